@@ -32,7 +32,7 @@
 extern "C" {
 #endif
 
-#define ACE_ABI_VERSION 5
+#define ACE_ABI_VERSION 6
 
 typedef enum {
   ACE_OK = 0,
@@ -252,6 +252,119 @@ size_t ace_tau_workspace_size(void);
 ace_status ace_tau_map(const float *scores, int64_t n_rows, int32_t k, int32_t m_min, const double *q,
                        int32_t n_q, float *tau, int64_t *m_q, int64_t *n_cand, void *workspace,
                        size_t workspace_bytes, void *stream);
+
+/*
+ * ---------------------------------------------------------------------------------------
+ * Operators around the layer: what a decoder that contains it computes next to it, in
+ * serving and in fine-tuning.  They follow the conventions above (device pointers, caller's
+ * buffers and stream, validation before any launch, deterministic results), with these
+ * differences: feature sizes are multiples of 16 bytes (8 bf16, 4 fp32 elements), arrays of
+ * them 16-byte aligned; int32 and fp32 arrays are 4-byte aligned.  Sums are fp32; each
+ * result is rounded once.  A result may not overlap an input unless its entry says so, nor
+ * another result.  Grids past 2^31 workgroups -> ACE_ERR_UNSUPPORTED.
+ *
+ * Rows in ragged groups: group e of N owns rows offsets[e] .. offsets[e + 1] - 1 of an S-row
+ * array, offsets DEVICE [N + 1] int32, ascending within 0 .. S (ace_moe_outputs.expert_offsets;
+ * the token offsets of a batch of requests); empty groups are fine.  The offsets are read on
+ * the device only.  Offsets that are not so give unspecified results, but no access outside
+ * the arrays.
+ */
+
+/*
+ * Matrix products grouped by expert with ragged sizes, over the experts' weights w [N, M, K]
+ * (nn.Linear layout: M outputs, K inputs), x [S, K] and dy [S, M] in group order:
+ *   ace_grouped_matmul          y[r]  = w[e] x[r]     for every row r of group e
+ *   ace_grouped_matmul_grad_x   dx[r] = w[e]^T dy[r]
+ *   ace_grouped_matmul_grad_w   dw[e] = sum over the rows r of e: dy[r] x[r]^T  (0 for an empty group)
+ * Rows of no group (before offsets[0], from offsets[N] on) keep what y or dx holds, or get
+ * zeros with ACE_ZERO_REST, and add nothing to dw.  Empty calls (S = 0) write nothing in the first
+ * two.  Limits (else ACE_ERR_UNSUPPORTED): N <= 4096, M and K <= 65536.
+ */
+enum { ACE_ZERO_REST = 1u << 0 };
+typedef struct {
+  int32_t S;      /* rows (0 is allowed) */
+  int32_t N;      /* groups */
+  int32_t M, K;   /* output and input features */
+  int32_t dtype;  /* ace_dtype of every array */
+  uint32_t flags; /* 0 or ACE_ZERO_REST */
+} ace_grouped_desc;
+ace_status ace_grouped_matmul(const ace_grouped_desc *desc, const void *x, const void *w, const int32_t *offsets,
+                              void *y, void *stream);
+ace_status ace_grouped_matmul_grad_x(const ace_grouped_desc *desc, const void *dy, const void *w,
+                                     const int32_t *offsets, void *dx, void *stream);
+ace_status ace_grouped_matmul_grad_w(const ace_grouped_desc *desc, const void *dy, const void *x,
+                                     const int32_t *offsets, void *dw, void *stream);
+
+/*
+ * The RMSNorms after a block and before the next one, fused with the block's gate and the
+ * residual scale.  With rms(v) = sqrt(mean(v^2) + eps):
+ *   u = y / rms(y) * w_post          (u = y without w_post)
+ *   h_out = res_scale * h + branch_scale * gate * u
+ *   n_out = h_out / rms(h_out) * w_pre, from h_out before its rounding   (not without w_pre)
+ * Without y: n_out is the norm of h, h_out is not written, and w_post, a gate or a res_scale
+ * other than 1 are refused; y or w_pre has to be there.  h_out and n_out may each be h or y itself.
+ * ace_block_norm_grad takes the gradients dh and dn of the two results (dh may be NULL: zero;
+ * dn exactly with w_pre), h = the h_out of the forward as stored (without y: the forward's h),
+ * the forward's y, weights and gate, and writes the gradients of the forward's h, y, w_post, w_pre
+ * and gate, each exactly where the operand is there.  h is needed with w_pre, y with w_post or a gate
+ * (any buffer otherwise; NULL y means a forward without y).  The gradients of h and y may each be one of
+ * dh, dn, h and y itself.  Sums over rows (w_post, w_pre, a gate per channel) are added in a fixed
+ * order; T = 0 gives zeros for them.
+ *   workspace  DEVICE scratch of ace_block_norm_grad_workspace_size(desc) bytes, 256-byte aligned.
+ * eps has to be positive.  Limit (else ACE_ERR_UNSUPPORTED): d <= 16384.
+ */
+typedef enum {
+  ACE_GATE_NONE = 0,
+  ACE_GATE_CHANNEL = 1, /* [d] */
+  ACE_GATE_TOKEN = 2,   /* [T] */
+  ACE_GATE_FULL = 3     /* [T, d] */
+} ace_gate_kind;
+typedef struct {
+  int32_t T, d;
+  int32_t dtype;     /* ace_dtype of every array */
+  int32_t gate_kind; /* ace_gate_kind */
+  float res_scale, branch_scale, eps;
+} ace_norm_desc;
+typedef struct {
+  const void *h;      /* [T, d] */
+  const void *y;      /* [T, d] or NULL */
+  const void *w_post; /* [d] or NULL */
+  const void *w_pre;  /* [d] or NULL */
+  const void *gate;   /* by gate_kind; NULL for ACE_GATE_NONE */
+} ace_norm_inputs;
+typedef struct {
+  void *h, *y, *w_post, *w_pre, *gate;
+} ace_norm_grads;
+ace_status ace_block_norm(const ace_norm_desc *desc, const ace_norm_inputs *in, void *h_out, void *n_out,
+                          void *stream);
+size_t ace_block_norm_grad_workspace_size(const ace_norm_desc *desc);
+ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs *in, const void *dh, const void *dn,
+                               const ace_norm_grads *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Low-rank adapters of many requests at once, beside a shared projection whose output is
+ * `base`: request i owns rows offsets[i] .. offsets[i + 1] - 1 and carries adapter[i],
+ *   out[r] = base[r] + scale[l] * b[l] (a[l] x[r])   with l = adapter[i].
+ * Rows of a request whose adapter number is outside 0 .. L - 1 (-1: none), and rows of no
+ * request, get out[r] = base[r].  out may be base itself (those rows then stay untouched).
+ *   base [S, d_out], x [S, d_in], a [L, rank, d_in], b [L, d_out, rank], out [S, d_out], dtype;
+ *   scale [L] fp32 or NULL (ones); offsets [R + 1] and adapter [R] int32 (adapter may be NULL when R = 0).
+ *   workspace  DEVICE scratch of ace_adapter_workspace_size(desc) bytes, 256-byte aligned.
+ * An adapter of lower rank is padded with zero rows of a.  Limits (else ACE_ERR_UNSUPPORTED): R <= 4096,
+ * rank <= 128, d_in and d_out <= 65536.
+ */
+typedef struct {
+  int32_t S;           /* rows (0 = nothing to do) */
+  int32_t R;           /* requests (0 is allowed) */
+  int32_t L;           /* adapters, at least 1 */
+  int32_t rank;
+  int32_t d_in, d_out;
+  int32_t dtype;       /* ace_dtype of base, x, a, b and out */
+} ace_adapter_desc;
+size_t ace_adapter_workspace_size(const ace_adapter_desc *desc);
+ace_status ace_adapter_add(const ace_adapter_desc *desc, const void *base, const void *x, const void *a, const void *b,
+                           const float *scale, const int32_t *offsets, const int32_t *adapter, void *out,
+                           void *workspace, size_t workspace_bytes, void *stream);
 
 /* Static, human-readable text of a status code (never NULL). */
 const char *ace_status_string(int status);

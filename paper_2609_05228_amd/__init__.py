@@ -9,6 +9,12 @@ arguments once, for loops that call the same layer again); `tau_map` turns the
 contribution scores of a score pass into the thresholds of requested skip
 ratios (App. C.1); and `build_tables` computes the offline GSP / RCR tables
 (Alg. 2, Alg. 3).
+
+Around the layer, for the decoder that contains it and for fine-tuning it:
+`grouped_matmul` (matrix products grouped by expert with ragged sizes) with its
+gradients, `block_norm` (the norms before and after a block with its gate and
+residual scale) with its gradient, and `adapter_add` (low-rank adapters of many
+requests beside a shared projection).
 """
 from ._lib import (  # noqa: F401
     ACE_BF16, ACE_ERR_HIP, ACE_ERR_INVALID_ARG, ACE_ERR_UNSUPPORTED, ACE_ERR_WORKSPACE, ACE_F32,
@@ -18,4 +24,7 @@ from ._lib import (  # noqa: F401
 )
 from .layer import (  # noqa: F401
     PreparedForward, build_tables, make_desc, moe_forward, prepare_forward, tau_map, workspace,
+)
+from .ops import (  # noqa: F401
+    adapter_add, block_norm, block_norm_grad, grouped_matmul, grouped_matmul_grad_w, grouped_matmul_grad_x,
 )

@@ -25,6 +25,7 @@ ACE_BF16 = 1
 ACE_SKIP_DISABLE = 1 << 0
 ACE_WRITE_SCORES = 1 << 1
 ACE_FUSION_SHIFT = 2
+ACE_ZERO_REST = 1 << 0
 # contribution rules (ace_fusion): ACE's max rule and the ablation variants
 FUSIONS = {"max": 0, "min": 1, "mean": 2, "gsp": 3, "rcr": 4, "score": 5}
 
@@ -46,6 +47,27 @@ class Weights(ctypes.Structure):
 class Outputs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in (
         "y", "topk_idx", "keep", "gates", "scores", "expert_counts", "expert_offsets", "perm")]
+
+
+class GroupedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("S", "N", "M", "K", "dtype")] + [("flags", ctypes.c_uint32)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "dtype", "gate_kind")] + [
+        (n, ctypes.c_float) for n in ("res_scale", "branch_scale", "eps")]
+
+
+class NormInputs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("h", "y", "w_post", "w_pre", "gate")]
+
+
+class NormGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("h", "y", "w_post", "w_pre", "gate")]
+
+
+class AdapterDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("S", "R", "L", "rank", "d_in", "d_out", "dtype")]
 
 
 class AceError(RuntimeError):
@@ -100,6 +122,22 @@ def lib() -> ctypes.CDLL:
                                   ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
                                   ctypes.c_void_p]
         L.ace_tau_map.restype = ctypes.c_int
+        vp = ctypes.c_void_p
+        for name in ("ace_grouped_matmul", "ace_grouped_matmul_grad_x", "ace_grouped_matmul_grad_w"):
+            fn = getattr(L, name)
+            fn.argtypes = [ctypes.POINTER(GroupedDesc), vp, vp, vp, vp, vp]
+            fn.restype = ctypes.c_int
+        L.ace_block_norm.argtypes = [ctypes.POINTER(NormDesc), ctypes.POINTER(NormInputs), vp, vp, vp]
+        L.ace_block_norm.restype = ctypes.c_int
+        L.ace_block_norm_grad_workspace_size.argtypes = [ctypes.POINTER(NormDesc)]
+        L.ace_block_norm_grad_workspace_size.restype = ctypes.c_size_t
+        L.ace_block_norm_grad.argtypes = [ctypes.POINTER(NormDesc), ctypes.POINTER(NormInputs), vp, vp,
+                                          ctypes.POINTER(NormGrads), vp, ctypes.c_size_t, vp]
+        L.ace_block_norm_grad.restype = ctypes.c_int
+        L.ace_adapter_workspace_size.argtypes = [ctypes.POINTER(AdapterDesc)]
+        L.ace_adapter_workspace_size.restype = ctypes.c_size_t
+        L.ace_adapter_add.argtypes = [ctypes.POINTER(AdapterDesc)] + [vp] * 8 + [vp, ctypes.c_size_t, vp]
+        L.ace_adapter_add.restype = ctypes.c_int
         _lib = L
     return _lib
 

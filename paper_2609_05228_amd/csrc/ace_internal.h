@@ -216,4 +216,47 @@ hipError_t launch_tau_map(const float *scores, long long n_rows, int k, int m_mi
                           float *tau, long long *m_q_out, long long *n_cand_out, void *workspace,
                           hipStream_t stream);
 
+// ---------------------------------------------------------------- operators around the layer
+// Grouped matrix products (grouped.hip).  rows: x (forward, [S, K]) or dy ([S, M]); other:
+// w [N, M, K] or, for the weights' gradient, x.  fill: zeros into the rows of no group.
+struct GroupedArgs {
+  const void *rows, *other;
+  void *out;
+  const int32_t *offsets;  // [N + 1]
+  int S, N, M, K;
+  int fill;
+};
+// each of these returns hipErrorInvalidValue, with nothing enqueued, for grids past 2^31 workgroups
+hipError_t launch_grouped_rows(const GroupedArgs &g, bool grad, bool bf16, hipStream_t stream);
+hipError_t launch_grouped_weights(const GroupedArgs &g, bool bf16, hipStream_t stream);
+
+// The norms before and after a block (block_norm.hip); null pointers: absent
+struct NormArgs {
+  const void *h, *y;  // residual stream before the block (forward) or after it (gradient), block output
+  const void *w_post, *w_pre, *gate;
+  int gate_kind;      // 0 none, 1 [d], 2 [T, 1], 3 [T, d]
+  int T, d;
+  float res_scale, branch_scale, eps;
+  void *out_h, *out_n;                  // forward
+  const void *dh, *dn;                  // gradient: in
+  void *g_h, *g_y, *g_post, *g_pre, *g_gate;  // and out
+  float *part;        // partial sums of the parameter gradients [params, blocks, d]
+  int blocks;
+};
+hipError_t launch_block_norm(const NormArgs &a, bool bf16, hipStream_t stream);
+hipError_t launch_block_norm_grad(const NormArgs &a, bool bf16, hipStream_t stream);
+int block_norm_grad_blocks(int T);  // workgroups of the gradient: rows of its partial sums
+
+// Low-rank adapters of many requests (adapter.hip)
+struct AdapterArgs {
+  const void *base, *x, *a, *b;  // [S, dout], [S, din], [L, r, din], [L, dout, r]
+  const float *scale;            // [L] or null
+  const int32_t *offsets, *adapter;  // [R + 1], [R]
+  void *out;                     // [S, dout], may be base
+  float *v;                      // [splits, S, r]
+  int S, R, L, r, din, dout, splits;
+};
+int adapter_splits(int S, int R, int din, bool bf16);
+hipError_t launch_adapter(const AdapterArgs &a, bool bf16, hipStream_t stream);
+
 }  // namespace ace

@@ -1,0 +1,250 @@
+"""torch-facing wrappers of the operators around the layer: matrix products grouped by
+expert with ragged sizes, the norms before and after a block fused with its gate and residual
+scale, and low-rank adapters of many requests at once.
+
+Like `moe_forward` they marshal device tensors into the C ABI of libace.so and enqueue on the
+current HIP stream of the tensors' device.  They record no autograd graph: the gradients are
+entry points of their own (`grouped_matmul_grad_x`, `grouped_matmul_grad_w`, `block_norm_grad`),
+and inputs that require a gradient are refused while autograd is on.  Workspaces come from
+torch's allocator with every call, so captured graphs share none.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import _lib
+from .layer import _DT
+
+_GATES = ("none", "channel", "token", "full")
+
+
+def _need(ok, msg):
+    if not ok:
+        raise ValueError(msg)
+
+
+def _check_all(dev, dtype, named):
+    """(name, tensor, shape, dtype or None for the call's): shapes, types, layout, device."""
+    grad = torch.is_grad_enabled()
+    for name, t, shape, dt in named:
+        if t.shape != shape:
+            raise ValueError(f"{name}: shape {tuple(t.shape)} != {tuple(shape)}")
+        if t.dtype != (dt or dtype):
+            raise ValueError(f"{name}: dtype {t.dtype} != {dt or dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, expected {dev}")
+        if grad and t.requires_grad:
+            raise ValueError(f"{name} requires a gradient: call under torch.no_grad() and use the *_grad functions")
+    if dev.type != "cuda":
+        raise ValueError(f"the tensors are on {dev}: a GPU is needed")
+
+
+def _dtype_of(name, t, dims):
+    _need(isinstance(t, torch.Tensor) and t.dim() == dims, f"{name} must be a tensor of {dims} dimensions")
+    _need(t.dtype in _DT, f"{name}: unsupported dtype {t.dtype}")
+    return t.dtype
+
+
+def _enqueue(dev, fn, *args):
+    """fn(*args, stream) on the current stream of dev, with dev current."""
+    if dev.index == torch.cuda.current_device():
+        st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if st != _lib.ACE_OK:
+        raise _lib.AceError(st, _lib.status_string(st))
+
+
+def _grouped(fn, rows, other, offsets, S, N, M, K, shape, names, shapes, out):
+    dtype, dev = rows.dtype, rows.device
+    named = [(names[0], rows, shapes[0], None), (names[1], other, shapes[1], None),
+             ("offsets", offsets, (N + 1,), torch.int32)]
+    flags = 0
+    if out is not None:
+        named.append(("out", out, shape, None))
+    _check_all(dev, dtype, named)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=dev)
+        flags = _lib.ACE_ZERO_REST
+    desc = _lib.GroupedDesc(S, N, M, K, _DT[dtype], flags)
+    _enqueue(dev, fn, desc, rows.data_ptr(), other.data_ptr(), offsets.data_ptr(), out.data_ptr())
+    return out
+
+
+def _groups_of(offsets):
+    _need(isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.shape[0] >= 2,
+          "offsets must hold at least one group: [N + 1] int32")
+    return offsets.shape[0] - 1
+
+
+def grouped_matmul(x, w, offsets, *, out=None):
+    """Products grouped by expert: y[r] = w[e] x[r] for the rows r of group e.
+
+    x        [S, K] bf16 or fp32 device tensor, rows in group order
+    w        [N, M, K] weights of the groups (nn.Linear layout)
+    offsets  [N + 1] int32: group e owns rows offsets[e] .. offsets[e + 1] - 1, ascending
+             (the `offsets` of `moe_forward`'s plan)
+    out      [S, M] or None.  Rows of no group stay as they are in `out`; a fresh result
+             holds zeros there.
+    K and M are multiples of 8 (fp32: 4).  Returns y [S, M]."""
+    _dtype_of("x", x, 2)
+    _dtype_of("w", w, 3)
+    N, M, K = w.shape
+    S = x.shape[0]
+    return _grouped(_lib.lib().ace_grouped_matmul, x, w, offsets, S, N, M, K, (S, M), ("x", "w"), ((S, K), (N, M, K)),
+                    out)
+
+
+def grouped_matmul_grad_x(dy, w, offsets, *, out=None):
+    """Gradient of `grouped_matmul` for its rows: dx[r] = w[e]^T dy[r].  dy [S, M]; the rest, and
+    rows of no group, as there.  Returns dx [S, K]."""
+    _dtype_of("dy", dy, 2)
+    _dtype_of("w", w, 3)
+    N, M, K = w.shape
+    S = dy.shape[0]
+    return _grouped(_lib.lib().ace_grouped_matmul_grad_x, dy, w, offsets, S, N, M, K, (S, K), ("dy", "w"),
+                    ((S, M), (N, M, K)), out)
+
+
+def grouped_matmul_grad_w(dy, x, offsets, *, out=None):
+    """Gradient of `grouped_matmul` for its weights: dw[e] = sum of dy[r] x[r]^T over the rows of
+    group e (zeros for an empty group).  dy [S, M], x [S, K], offsets [N + 1].  Returns dw [N, M, K]."""
+    _dtype_of("dy", dy, 2)
+    _dtype_of("x", x, 2)
+    N = _groups_of(offsets)
+    S, M = dy.shape
+    K = x.shape[1]
+    return _grouped(_lib.lib().ace_grouped_matmul_grad_w, dy, x, offsets, S, N, M, K, (N, M, K), ("dy", "x"),
+                    ((S, M), (S, K)), out)
+
+
+def _norm_call(rows, d, dtype, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, more):
+    """Check a block_norm call's tensors; (desc, inputs)."""
+    named = list(more)
+    for name, t in (("h", h), ("y", y)):
+        if t is not None:
+            named.append((name, t, (rows, d), None))
+    for name, t in (("w_post", w_post), ("w_pre", w_pre)):
+        if t is not None:
+            named.append((name, t, (d,), None))
+    kind = 0
+    if gate is not None:
+        kind = {(d,): 1, (rows, 1): 2, (rows, d): 3}.get(tuple(gate.shape), 0)
+        _need(kind, f"gate: shape {tuple(gate.shape)} is none of [d], [T, 1], [T, d]")
+        named.append(("gate", gate, gate.shape, None))
+    _need(y is not None or (w_post is None and gate is None and res_scale == 1.0),
+          "w_post, gate and res_scale need y")
+    _need(y is not None or w_pre is not None, "y or w_pre is required")
+    _check_all(named[0][1].device, dtype, named)
+    desc = _lib.NormDesc(rows, d, _DT[dtype], kind, res_scale, branch_scale, eps)
+    inp = _lib.NormInputs(*[None if t is None else t.data_ptr() for t in (h, y, w_post, w_pre, gate)])
+    return desc, inp
+
+
+def block_norm(h, y=None, *, w_post=None, w_pre=None, gate=None, res_scale=1.0, branch_scale=1.0, eps=1e-6, out=None):
+    """The norms after one block and before the next, with the block's gate and the residual scale:
+
+        u = y / rms(y) * w_post                         (y itself without w_post)
+        h' = res_scale * h + branch_scale * gate * u
+        n = h' / rms(h') * w_pre                        (not without w_pre)
+
+    h        [T, d] bf16 or fp32: the residual stream
+    y        [T, d]: the block's output (`moe_forward`'s y); None for the norm before the first block
+    w_post, w_pre  [d] or None
+    gate     [d], [T, 1] or [T, d], or None
+    out      dict that may hold "h" and "n" [T, d] (h or y themselves are fine)
+    d is a multiple of 8 (fp32: 4), at most 16384; eps > 0.  Returns dict(h=h'[, n]); without y, h' is h."""
+    dtype = _dtype_of("h", h, 2)
+    T, d = h.shape
+    out = {} if out is None else dict(out)
+    more = [(f"out['{k}']", out[k], (T, d), None) for k in ("h", "n") if k in out]
+    desc, inp = _norm_call(T, d, dtype, h, y, w_post, w_pre, gate, float(res_scale), float(branch_scale), float(eps),
+                           [("h", h, (T, d), None)] + more)
+    if y is None:
+        out["h"] = h
+    elif "h" not in out:
+        out["h"] = torch.empty_like(h)
+    if w_pre is None:
+        out.pop("n", None)
+    elif "n" not in out:
+        out["n"] = torch.empty_like(h)
+    _enqueue(h.device, _lib.lib().ace_block_norm, desc, inp, out["h"].data_ptr() if y is not None else None,
+             out["n"].data_ptr() if w_pre is not None else None)
+    return out
+
+
+def block_norm_grad(dh, dn, h, y=None, *, w_post=None, w_pre=None, gate=None, res_scale=1.0, branch_scale=1.0,
+                    eps=1e-6):
+    """Gradients of `block_norm`.
+
+    dh, dn   [T, d]: gradients of the results h' and n (dh None: zero; dn exactly with w_pre)
+    h        [T, d]: the forward's result h' (without y: its h); may be None without w_pre
+    y, weights, gate and scales as in the forward
+    Returns a dict of the gradients of h, and of y, w_post, w_pre and gate where there is one, in their
+    shapes and type.  Sums over the rows are fp32 in a fixed order."""
+    lead = dh if dh is not None else dn
+    _need(lead is not None, "dh or dn is required")
+    dtype = _dtype_of("dh" if dh is not None else "dn", lead, 2)
+    T, d = lead.shape
+    _need((dn is None) == (w_pre is None), "dn and w_pre go together")
+    _need(h is not None or w_pre is None, "h is required with w_pre")
+    more = [(n, t, (T, d), None) for n, t in (("dh", dh), ("dn", dn)) if t is not None]
+    desc, inp = _norm_call(T, d, dtype, h, y, w_post, w_pre, gate, float(res_scale), float(branch_scale), float(eps),
+                           more)
+    dev = lead.device
+    out = {"h": torch.empty_like(lead)}
+    for name, t in (("y", y), ("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
+        if t is not None:
+            out[name] = torch.empty_like(t)
+    grads = _lib.NormGrads(*[out[n].data_ptr() if n in out else None for n in ("h", "y", "w_post", "w_pre", "gate")])
+    lib = _lib.lib()
+    n = lib.ace_block_norm_grad_workspace_size(ctypes.byref(desc))
+    ws = torch.empty(max(n, 256), dtype=torch.uint8, device=dev)
+    _enqueue(dev, lib.ace_block_norm_grad, desc, inp, None if dh is None else dh.data_ptr(),
+             None if dn is None else dn.data_ptr(), grads, ws.data_ptr(), ws.numel())
+    return out
+
+
+def adapter_add(base, x, a, b, offsets, adapter, *, scale=None, out=None):
+    """Low-rank adapters of many requests beside a shared projection:
+    out[r] = base[r] + scale[l] * b[l] (a[l] x[r]), l = adapter[i] for the rows r of request i.
+
+    base     [S, d_out] bf16 or fp32: the shared projection's output
+    x        [S, d_in]: its input
+    a, b     [L, rank, d_in], [L, d_out, rank]: the adapters (lower ranks padded with zero rows of a)
+    offsets  [R + 1] int32: request i owns rows offsets[i] .. offsets[i + 1] - 1, ascending
+    adapter  [R] int32: adapter of each request, -1 for none
+    scale    [L] fp32 or None
+    out      [S, d_out] or None; `base` itself adds in place
+    Rows without an adapter, and rows of no request, are base's.  d_in, d_out and the rank (at most 128) are
+    multiples of 8 (fp32: 4).  Returns out."""
+    dtype = _dtype_of("x", x, 2)
+    _dtype_of("a", a, 3)
+    _dtype_of("b", b, 3)
+    S, d_in = x.shape
+    L, rank, _ = a.shape
+    d_out = b.shape[1]
+    R = (_groups_of(offsets) if isinstance(offsets, torch.Tensor) and offsets.shape != (1,) else 0)
+    dev = x.device
+    named = [("x", x, (S, d_in), None), ("base", base, (S, d_out), None), ("a", a, (L, rank, d_in), None),
+             ("b", b, (L, d_out, rank), None), ("offsets", offsets, (R + 1,), torch.int32),
+             ("adapter", adapter, (R,), torch.int32)]
+    if scale is not None:
+        named.append(("scale", scale, (L,), torch.float32))
+    if out is not None:
+        named.append(("out", out, (S, d_out), None))
+    _check_all(dev, dtype, named)
+    if out is None:
+        out = torch.empty_like(base)
+    desc = _lib.AdapterDesc(S, R, L, rank, d_in, d_out, _DT[dtype])
+    lib = _lib.lib()
+    ws = torch.empty(max(lib.ace_adapter_workspace_size(ctypes.byref(desc)), 256), dtype=torch.uint8, device=dev)
+    _enqueue(dev, lib.ace_adapter_add, desc, base.data_ptr(), x.data_ptr(), a.data_ptr(), b.data_ptr(),
+             None if scale is None else scale.data_ptr(), offsets.data_ptr(), adapter.data_ptr(), out.data_ptr(),
+             ws.data_ptr(), ws.numel())
+    return out

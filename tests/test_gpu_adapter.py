@@ -1,0 +1,146 @@
+"""Low-rank adapters of many requests against the definition in 64 bits."""
+import pytest
+import torch
+
+import ops_oracle as ref
+import paper_2609_05228_amd as ace
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+NAN = float("nan")
+
+# request sizes, adapters of the requests, rows before and behind, adapters, rank, d_in, d_out
+CASES = [
+    ([1], [0], 0, 0, 1, 8, 8, 8),
+    ([1, 1, 1, 1], [2, -1, 0, 2], 0, 0, 3, 16, 64, 64),
+    ([1] * 33, [i % 5 - 1 for i in range(33)], 0, 2, 4, 24, 136, 72),
+    ([5, 0, 17, 0, 3], [1, 0, -1, 7, 0], 2, 3, 2, 32, 264, 520),
+    ([100, 1, 65], [0, 1, 0], 0, 0, 2, 64, 520, 328),
+    ([16, 300, 48], [1, 1, 2], 1, 30, 3, 72, 1032, 264),
+    ([70], [0], 0, 0, 1, 128, 2056, 1032),
+    ([], [], 0, 9, 2, 16, 64, 64),
+    ([3] * 150, [i % 11 - 1 for i in range(150)], 0, 0, 10, 8, 72, 40),
+    ([200, 40], [-1, 5], 0, 0, 2, 16, 64, 64),
+]
+
+
+def make(sizes, ids, head, tail, L, rank, d_in, d_out, dtype):
+    """NaN in what no row may read: x of rows without an adapter, adapters of no request."""
+    gen = torch.Generator().manual_seed(len(sizes) + rank + d_in)
+    S = head + sum(sizes) + tail
+    offs = [head]
+    for n in sizes:
+        offs.append(offs[-1] + n)
+    base, x = torch.randn((S, d_out), generator=gen), torch.randn((S, d_in), generator=gen)
+    a, b = torch.randn((L, rank, d_in), generator=gen) * d_in ** -0.5, torch.randn((L, d_out, rank), generator=gen)
+    scale = torch.rand((L,), generator=gen) + 0.5
+    used = {i for i, n in zip(ids, sizes) if n}
+    for l in range(L):
+        if l not in used:
+            a[l], b[l], scale[l] = NAN, NAN, NAN
+    x[:head] = NAN
+    x[offs[-1]:] = NAN
+    for i, l in enumerate(ids):
+        if not 0 <= l < L:
+            x[offs[i]:offs[i + 1]] = NAN
+    dt = DT[dtype]
+    return (base.to(dt), x.to(dt), a.to(dt), b.to(dt), torch.tensor(offs, dtype=torch.int32),
+            torch.tensor(ids, dtype=torch.int32), scale)
+
+
+def check(got, args, scale, dtype):
+    base, x, a, b, offs, ids = args
+    want, mag = ref.adapter_add(base, x, a, b, offs, ids, scale)
+    # sums over d_in and the rank; in bf16 the inner product is held as two bf16 numbers: 2^-16 of
+    # it, 2^7 fp32 steps
+    terms = a.shape[2] + a.shape[1] + 4 + (128 if dtype == "bf16" else 0)
+    ref.close(got, want, mag, DT[dtype], terms, "out")
+    plain = torch.ones(base.shape[0], dtype=torch.bool)
+    for i, lo, hi in ref.groups(offs):
+        if 0 <= int(ids[i]) < a.shape[0]:
+            plain[lo:hi] = False
+    assert torch.equal(got.cpu()[plain], base[plain])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{len(c[0])}req_{sum(c[0])}r_rank{c[5]}_{c[6]}x{c[7]}")
+def test_against_the_definition(case, dtype):
+    *args, scale = make(*case, dtype)
+    d = [t.to(DEV) for t in args]
+    got = ace.adapter_add(*d, scale=scale.to(DEV))
+    torch.cuda.synchronize()
+    check(got, args, scale, dtype)
+    assert torch.equal(d[0].cpu(), args[0])
+    # in place: the same bits
+    assert ace.adapter_add(*d, scale=scale.to(DEV), out=d[0]) is d[0]
+    assert torch.equal(d[0], got)
+    # without scales
+    check(ace.adapter_add(args[0].to(DEV), *d[1:]), args, None, dtype)
+
+
+def test_no_rows():
+    *args, scale = make([], [], 0, 0, 1, 8, 64, 40, "bf16")
+    assert ace.adapter_add(*[t.to(DEV) for t in args]).shape == (0, 40)
+
+
+@pytest.mark.parametrize("offs", [[0, 9, 4, 40], [-5, 3, 90, 200], [40, 20, 10, 0]])
+def test_bad_offsets_stay_inside(offs):
+    *args, scale = make([20, 15, 5], [0, 1, 0], 0, 0, 2, 16, 64, 40, "bf16")
+    d = [t.to(DEV) for t in args]
+    d[4] = torch.tensor(offs, dtype=torch.int32, device=DEV)
+    pad = 64
+    buf = torch.full((40 * 40 + 2 * pad,), 5.0, dtype=torch.bfloat16, device=DEV)
+    ace.adapter_add(*d, out=buf[pad:-pad].view(40, 40))
+    torch.cuda.synchronize()
+    assert bool((buf[:pad] == 5).all()) and bool((buf[-pad:] == 5).all())
+
+
+def test_rows_past_four_gib():
+    S, n, w, r = (1 << 20) + 33, 40, 2048, 16
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    x = torch.zeros((S, w), dtype=torch.bfloat16, device=DEV)
+    base = torch.zeros_like(x)
+    x[-n:] = torch.randn((n, w), generator=gen, device=DEV).bfloat16()
+    a = (torch.randn((2, r, w), generator=gen, device=DEV) * w ** -0.5).bfloat16()
+    b = torch.randn((2, w, r), generator=gen, device=DEV).bfloat16()
+    offs = torch.tensor([0, S - n // 2, S], dtype=torch.int32, device=DEV)
+    ids = torch.tensor([1, 0], dtype=torch.int32, device=DEV)
+    got = ace.adapter_add(base, x, a, b, offs, ids)
+    torch.cuda.synchronize()
+    small = [base[-n:].cpu(), x[-n:].cpu(), a.cpu(), b.cpu(), torch.tensor([0, n // 2, n]), ids.cpu()]
+    check(got[-n:], small, None, "bf16")
+    assert not got[:-n].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_streams_graphs_and_repeats(dtype):
+    *args, scale = make([1, 1, 90, 1, 5], [0, 1, 1, -1, 2], 0, 0, 3, 16, 264, 136, dtype)
+    d = [t.to(DEV) for t in args]
+    sc = scale.to(DEV)
+    want = ace.adapter_add(*d, scale=sc)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = ace.adapter_add(*d, scale=sc)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = ace.adapter_add(*d, scale=sc)
+        graphs.append((g, got, torch.cuda.Stream()))
+    for _ in range(3):
+        for _, got, _ in graphs:
+            got.fill_(3)
+        torch.cuda.synchronize()
+        for g, _, s in graphs:
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for _, got, _ in graphs:
+            assert torch.equal(got, want)
+        assert torch.equal(ace.adapter_add(*d, scale=sc), want)

@@ -1,0 +1,211 @@
+"""Grouped matrix products and their gradients against the definition in 64 bits: ragged and
+empty groups, rows of no group, NaN wherever nothing may be read, offsets past 2^31."""
+import pytest
+import torch
+
+import ops_oracle as ref
+import paper_2609_05228_amd as ace
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+NAN = float("nan")
+
+# group sizes, rows before the first and behind the last group, M, K
+SHAPES = [
+    ([1], 0, 0, 8, 8),
+    ([1, 1, 1], 0, 1, 64, 64),
+    ([0, 3, 0, 0, 5, 0], 2, 4, 72, 136),
+    ([16, 17, 15, 33], 0, 0, 128, 64),
+    ([0, 0], 3, 0, 40, 24),
+    ([65, 1, 0, 130, 63], 1, 70, 136, 200),
+    ([257, 3, 256, 255], 0, 9, 264, 72),
+    ([300], 0, 0, 520, 328),
+    ([5] * 70 + [0] * 60 + [2] * 5, 0, 3, 48, 88),
+    ([700, 0, 1, 90], 0, 0, 32, 1032),
+    ([2, 0, 1], 0, 0, 1032, 2056),
+]
+
+
+def make(sizes, head, tail, M, K, dtype, seed=0):
+    """x, w, dy, offsets; NaN in the rows of no group and the weights of empty groups."""
+    gen = torch.Generator().manual_seed(seed + M + K + len(sizes))
+    S = head + sum(sizes) + tail
+    offs = [head]
+    for n in sizes:
+        offs.append(offs[-1] + n)
+    x = torch.randn((S, K), generator=gen).to(DT[dtype])
+    w = (torch.randn((len(sizes), M, K), generator=gen) * K ** -0.5).to(DT[dtype])
+    dy = torch.randn((S, M), generator=gen).to(DT[dtype])
+    for t in (x, dy):
+        t[:head] = NAN
+        t[offs[-1]:] = float("inf")
+    for e, n in enumerate(sizes):
+        if n == 0:
+            w[e] = NAN
+    return x, w, dy, torch.tensor(offs, dtype=torch.int32)
+
+
+def rest(offs, S):
+    m = torch.ones(S, dtype=torch.bool)
+    m[int(offs[0]):int(offs[-1])] = False
+    return m
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"{len(s[0])}g_{sum(s[0])}r_{s[3]}x{s[4]}")
+def test_against_the_definition(shape, dtype):
+    x, w, dy, offs = make(*shape, dtype)
+    S, M, K = x.shape[0], w.shape[1], w.shape[2]
+    gap = rest(offs, S)
+    d = [t.to(DEV) for t in (x, w, dy, offs)]
+    y = ace.grouped_matmul(d[0], d[1], d[3])
+    dx = ace.grouped_matmul_grad_x(d[2], d[1], d[3])
+    dw = ace.grouped_matmul_grad_w(d[2], d[0], d[3])
+    torch.cuda.synchronize()
+    want, mag = ref.grouped(x, w, offs)
+    ref.close(y, want, mag, DT[dtype], K, "y")
+    want, mag = ref.grouped(dy, w.transpose(1, 2), offs)
+    ref.close(dx, want, mag, DT[dtype], M, "dx")
+    want, mag = ref.grouped_grad_w(dy, x, offs)
+    ref.close(dw, want, mag, DT[dtype], max(max(shape[0]), 1), "dw")
+    assert not y[gap].any() and not dx[gap].any()
+    # into given buffers: rows of no group stay, the rest is the same bits
+    y2, dx2, dw2 = torch.full_like(y, 7), torch.full_like(dx, 7), torch.full_like(dw, NAN)
+    assert ace.grouped_matmul(d[0], d[1], d[3], out=y2) is y2
+    ace.grouped_matmul_grad_x(d[2], d[1], d[3], out=dx2)
+    ace.grouped_matmul_grad_w(d[2], d[0], d[3], out=dw2)
+    torch.cuda.synchronize()
+    assert bool((y2[gap] == 7).all()) and bool((dx2[gap] == 7).all())
+    assert torch.equal(y2[~gap], y[~gap]) and torch.equal(dx2[~gap], dx[~gap]) and torch.equal(dw2, dw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_rows(dtype):
+    x, w, dy, offs = make([0, 0, 0], 0, 0, 16, 24, dtype)
+    d = [t.to(DEV) for t in (x, w, dy, offs)]
+    assert ace.grouped_matmul(d[0], d[1], d[3]).shape == (0, 16)
+    assert ace.grouped_matmul_grad_x(d[2], d[1], d[3]).shape == (0, 24)
+    dw = ace.grouped_matmul_grad_w(d[2], d[0], d[3], out=torch.full((3, 16, 24), NAN, dtype=DT[dtype], device=DEV))
+    torch.cuda.synchronize()
+    assert not dw.any()
+
+
+def test_infinities_stay_in_their_rows():
+    """An infinity in a row reaches that row's products (and its group's gradient) alone."""
+    x, w, dy, offs = make([40, 30], 0, 0, 64, 64, "bf16")
+    x[3, 5] = float("inf")
+    d = [t.to(DEV) for t in (x, w, dy, offs)]
+    y = ace.grouped_matmul(d[0], d[1], d[3]).cpu()
+    dw = ace.grouped_matmul_grad_w(d[2], d[0], d[3]).cpu()
+    want, mag = ref.grouped(x, w, offs)
+    keep = torch.arange(70) != 3
+    ref.close(y[keep], want[keep], mag[keep], torch.bfloat16, 64, "y")
+    assert torch.equal(y[3].isinf(), want[3].isinf())
+    want, mag = ref.grouped_grad_w(dy, x, offs)
+    cols = torch.arange(64) != 5
+    ref.close(dw[:, :, cols], want[:, :, cols], mag[:, :, cols], torch.bfloat16, 40, "dw")
+    ref.close(dw[1], want[1], mag[1], torch.bfloat16, 40, "dw of the other group")
+
+
+@pytest.mark.parametrize("offs", [[0, 9, 4, 40], [-5, 3, 90, 200], [40, 20, 10, 0], [7, 7, 7, 2 ** 31 - 1],
+                                  [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1]])
+def test_bad_offsets_stay_inside(offs):
+    """Offsets that do not ascend or leave the array: unspecified results, no write outside."""
+    S, M, K = 40, 24, 16
+    x, w, dy, _ = make([S, 0, 0], 0, 0, M, K, "bf16")
+    w[1:] = 0
+    o = torch.tensor(offs, dtype=torch.int32, device=DEV)
+    d = [t.to(DEV) for t in (x, w, dy)]
+    pad = 64
+    for fn, a, b, shape in ((ace.grouped_matmul, d[0], d[1], (S, M)), (ace.grouped_matmul_grad_x, d[2], d[1], (S, K)),
+                            (ace.grouped_matmul_grad_w, d[2], d[0], (3, M, K))):
+        n = torch.Size(shape).numel()
+        buf = torch.full((n + 2 * pad,), 5.0, dtype=torch.bfloat16, device=DEV)
+        fn(a, b, o, out=buf[pad:pad + n].view(shape))
+        torch.cuda.synchronize()
+        assert bool((buf[:pad] == 5).all()) and bool((buf[-pad:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_past_two_gib(dtype):
+    """Rows whose byte offsets pass 2^32 (and element offsets 2^31): the last rows are right."""
+    K, M = 2048, 8
+    S = (1 << 20) + (1 << 19) + 37  # 1.6M rows x 2048
+    x = torch.zeros((S, K), dtype=DT[dtype], device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    n = 300
+    x[-n:] = torch.randn((n, K), generator=gen, device=DEV).to(DT[dtype])
+    x[:n] = torch.randn((n, K), generator=gen, device=DEV).to(DT[dtype])
+    w = torch.randn((2, M, K), generator=gen, device=DEV).to(DT[dtype])
+    offs = torch.tensor([0, S - 200, S], dtype=torch.int32, device=DEV)
+    y = ace.grouped_matmul(x, w, offs)
+    dy = torch.zeros((S, M), dtype=DT[dtype], device=DEV)
+    dy[-n:] = y[-n:]
+    dy[:n] = y[:n]
+    dx = ace.grouped_matmul_grad_x(dy, w, offs)
+    dw = ace.grouped_matmul_grad_w(dy, x, offs)
+    torch.cuda.synchronize()
+    # the rows that are not zero: n first ones and n last ones, of which 200 are the second group's
+    cut = torch.tensor([0, 2 * n - 200, 2 * n], dtype=torch.int32)
+    xs, dys = torch.cat([x[:n], x[-n:]]).cpu(), torch.cat([dy[:n], dy[-n:]]).cpu()
+    want, mag = ref.grouped(xs, w.cpu(), cut)
+    ref.close(torch.cat([y[:n], y[-n:]]), want, mag, DT[dtype], K, "y")
+    assert not y[n:-n].any() and not dx[n:-n].any()
+    want, mag = ref.grouped(dys, w.cpu().transpose(1, 2), cut)
+    ref.close(torch.cat([dx[:n], dx[-n:]]), want, mag, DT[dtype], M, "dx")
+    want, mag = ref.grouped_grad_w(dys, xs, cut)
+    ref.close(dw, want, mag, DT[dtype], 2 * n, "dw")
+
+
+def test_gradients_against_differences():
+    """<dy, y(x + t v)> changes with t as <dx, v> says, and the same for the weights (fp32; the
+    function is linear in each, so the difference is exact up to the operator's own rounding)."""
+    x, w, dy, offs = make([33, 0, 70, 9], 0, 0, 40, 96, "f32", seed=3)
+    w = torch.nan_to_num(w)
+    gen = torch.Generator().manual_seed(8)
+    v, u = torch.randn(x.shape, generator=gen), torch.randn(w.shape, generator=gen)
+    d = [t.to(DEV) for t in (x, w, dy, offs)]
+    dx = ace.grouped_matmul_grad_x(d[2], d[1], d[3]).cpu().double()
+    dw = ace.grouped_matmul_grad_w(d[2], d[0], d[3]).cpu().double()
+
+    def loss(a, b):
+        return float((dy.double() * ref.grouped(a, b, offs)[0]).sum())
+
+    h = 2.0 ** -10
+    for grad, dirn, f in ((dx, v, lambda s: loss(x.double() + s * v.double(), w)), (dw, u, lambda s: loss(x, w.double() + s * u.double()))):
+        diff = (f(h) - f(-h)) / (2 * h)
+        want = float((grad * dirn.double()).sum())
+        # each gradient element is off by at most 96 fp32 operations on its terms
+        tol = 2 * 96 * ref.F32 * float((grad.abs() * dirn.double().abs()).sum()) * 40
+        assert abs(diff - want) <= tol, (diff, want, tol)
+
+
+@pytest.mark.parametrize("fn", ["fwd", "grad_x", "grad_w"])
+def test_streams_graphs_and_repeats(fn):
+    """The same bits again, on another stream, and from a graph replayed between eager work."""
+    x, w, dy, offs = make([70, 0, 3, 200], 0, 5, 136, 264, "bf16")
+    x, dy = torch.nan_to_num(x, 0, 0, 0), torch.nan_to_num(dy, 0, 0, 0)
+    d = [t.to(DEV) for t in (x, torch.nan_to_num(w), dy, offs)]
+    a, b, f = {"fwd": (d[0], d[1], ace.grouped_matmul), "grad_x": (d[2], d[1], ace.grouped_matmul_grad_x),
+               "grad_w": (d[2], d[0], ace.grouped_matmul_grad_w)}[fn]
+    want = f(a, b, d[3])
+    torch.cuda.synchronize()
+    assert torch.equal(f(a, b, d[3]), want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = f(a, b, d[3])
+    side.synchronize()
+    assert torch.equal(got, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = f(a, b, d[3])
+    for _ in range(3):
+        got.fill_(9)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        assert torch.equal(f(a, b, d[3]), want)
