@@ -278,7 +278,9 @@ ace_status ace_tau_map(const float *scores, int64_t n_rows, int32_t k, int32_t m
  *   ace_grouped_matmul_grad_w   dw[e] = sum over the rows r of e: dy[r] x[r]^T  (0 for an empty group)
  * Rows of no group (before offsets[0], from offsets[N] on) keep what y or dx holds, or get
  * zeros with ACE_ZERO_REST, and add nothing to dw.  Empty calls (S = 0) write nothing in the first
- * two.  Limits (else ACE_ERR_UNSUPPORTED): N <= 4096, M and K <= 65536.
+ * two.  Limits (else ACE_ERR_UNSUPPORTED): S < 2^31 - 1024, N <= 4096, M and K <= 65536.
+ *   workspace  DEVICE scratch of ace_grouped_workspace_size(desc, way) bytes, 256-byte aligned (may be NULL
+ *              when that is 0): partial sums where few tiles leave a long reduction to split.
  */
 enum { ACE_ZERO_REST = 1u << 0 };
 typedef struct {
@@ -288,12 +290,16 @@ typedef struct {
   int32_t dtype;  /* ace_dtype of every array */
   uint32_t flags; /* 0 or ACE_ZERO_REST */
 } ace_grouped_desc;
+typedef enum { ACE_GROUPED_FORWARD = 0, ACE_GROUPED_GRAD_X = 1, ACE_GROUPED_GRAD_W = 2 } ace_grouped_way;
+size_t ace_grouped_workspace_size(const ace_grouped_desc *desc, int way);
 ace_status ace_grouped_matmul(const ace_grouped_desc *desc, const void *x, const void *w, const int32_t *offsets,
-                              void *y, void *stream);
+                              void *y, void *workspace, size_t workspace_bytes, void *stream);
 ace_status ace_grouped_matmul_grad_x(const ace_grouped_desc *desc, const void *dy, const void *w,
-                                     const int32_t *offsets, void *dx, void *stream);
+                                     const int32_t *offsets, void *dx, void *workspace, size_t workspace_bytes,
+                                     void *stream);
 ace_status ace_grouped_matmul_grad_w(const ace_grouped_desc *desc, const void *dy, const void *x,
-                                     const int32_t *offsets, void *dw, void *stream);
+                                     const int32_t *offsets, void *dw, void *workspace, size_t workspace_bytes,
+                                     void *stream);
 
 /*
  * The RMSNorms after a block and before the next one, fused with the block's gate and the
@@ -350,7 +356,7 @@ ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs 
  *   base [S, d_out], x [S, d_in], a [L, rank, d_in], b [L, d_out, rank], out [S, d_out], dtype;
  *   scale [L] fp32 or NULL (ones); offsets [R + 1] and adapter [R] int32 (adapter may be NULL when R = 0).
  *   workspace  DEVICE scratch of ace_adapter_workspace_size(desc) bytes, 256-byte aligned.
- * An adapter of lower rank is padded with zero rows of a.  Limits (else ACE_ERR_UNSUPPORTED): R <= 4096,
+ * An adapter of lower rank is padded with zero rows of a.  Limits (else ACE_ERR_UNSUPPORTED): S < 2^31 - 1024, R <= 4096,
  * rank <= 128, d_in and d_out <= 65536.
  */
 typedef struct {

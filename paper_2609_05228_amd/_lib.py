@@ -26,6 +26,7 @@ ACE_SKIP_DISABLE = 1 << 0
 ACE_WRITE_SCORES = 1 << 1
 ACE_FUSION_SHIFT = 2
 ACE_ZERO_REST = 1 << 0
+GROUPED_FORWARD, GROUPED_GRAD_X, GROUPED_GRAD_W = 0, 1, 2  # ace_grouped_way
 # contribution rules (ace_fusion): ACE's max rule and the ablation variants
 FUSIONS = {"max": 0, "min": 1, "mean": 2, "gsp": 3, "rcr": 4, "score": 5}
 
@@ -125,8 +126,10 @@ def lib() -> ctypes.CDLL:
         vp = ctypes.c_void_p
         for name in ("ace_grouped_matmul", "ace_grouped_matmul_grad_x", "ace_grouped_matmul_grad_w"):
             fn = getattr(L, name)
-            fn.argtypes = [ctypes.POINTER(GroupedDesc), vp, vp, vp, vp, vp]
+            fn.argtypes = [ctypes.POINTER(GroupedDesc), vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
             fn.restype = ctypes.c_int
+        L.ace_grouped_workspace_size.argtypes = [ctypes.POINTER(GroupedDesc), ctypes.c_int]
+        L.ace_grouped_workspace_size.restype = ctypes.c_size_t
         L.ace_block_norm.argtypes = [ctypes.POINTER(NormDesc), ctypes.POINTER(NormInputs), vp, vp, vp]
         L.ace_block_norm.restype = ctypes.c_int
         L.ace_block_norm_grad_workspace_size.argtypes = [ctypes.POINTER(NormDesc)]

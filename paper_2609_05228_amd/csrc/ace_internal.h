@@ -225,8 +225,10 @@ struct GroupedArgs {
   const int32_t *offsets;  // [N + 1]
   int S, N, M, K;
   int fill;
+  int splits;   // parts of the reduction, and their fp32 sums [splits, out's elements]
+  float *part;  // grouped_workspace_bytes
 };
-// each of these returns hipErrorInvalidValue, with nothing enqueued, for grids past 2^31 workgroups
+size_t grouped_workspace_bytes(const GroupedArgs &g, bool weights, bool grad, bool bf16);
 hipError_t launch_grouped_rows(const GroupedArgs &g, bool grad, bool bf16, hipStream_t stream);
 hipError_t launch_grouped_weights(const GroupedArgs &g, bool bf16, hipStream_t stream);
 
@@ -257,6 +259,7 @@ struct AdapterArgs {
   int S, R, L, r, din, dout, splits;
 };
 int adapter_splits(int S, int R, int din, bool bf16);
+// hipErrorInvalidValue, with nothing enqueued, for grids past 2^31 workgroups
 hipError_t launch_adapter(const AdapterArgs &a, bool bf16, hipStream_t stream);
 
 }  // namespace ace

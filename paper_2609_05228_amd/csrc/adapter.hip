@@ -17,7 +17,7 @@ namespace ace {
 
 namespace {
 
-constexpr int kAdRows = 16, kAdRowsLog2 = 4;
+constexpr int kAdRows = 16;
 
 template <typename T> __device__ __forceinline__ typename Frag<T>::type zero_frag() {
   return __builtin_bit_cast(typename Frag<T>::type, uint4{0, 0, 0, 0});
@@ -36,7 +36,7 @@ template <typename T, int RB> __global__ __launch_bounds__(256) void adapter_shr
   constexpr int E = kChunkElems<T>;
   typedef typename Frag<T>::type frag_t;
   const int b = ragged_block();
-  const RaggedTile t = ragged_tile(p.offsets, p.R, p.S, kAdRowsLog2, b / p.splits, false);
+  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kAdRows, false).find_uniform(b / p.splits);
   if (!t.valid) return;
   const int ad = tile_adapter(p, t);
   if (ad < 0) return;
@@ -81,7 +81,7 @@ template <typename T, int KB> __global__ __launch_bounds__(256) void adapter_exp
   typedef typename Frag<T>::type frag_t;
   const int nN = (p.dout + kAdCols - 1) / kAdCols;
   const int b = ragged_block();
-  const RaggedTile t = ragged_tile(p.offsets, p.R, p.S, kAdRowsLog2, b / nN, true);
+  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kAdRows, true).find_uniform(b / nN);
   if (!t.valid) return;
   const int ad = tile_adapter(p, t);
   if (ad < 0 && p.out == p.base) return;

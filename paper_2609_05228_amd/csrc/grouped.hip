@@ -19,6 +19,9 @@
 // The products go to the matrix cores as mfma(B, A): a lane then holds consecutive columns
 // of one row, and with the columns of two 16-column blocks interleaved in fours (bf16) it
 // stores 16 bytes at a time.  Sums are fp32, rounded once.
+#include <algorithm>
+#include <type_traits>
+
 #include "lds_dma.h"
 #include "ragged.h"
 
@@ -37,6 +40,17 @@ __device__ __forceinline__ void dma16_buf(i32x4_rsrc rsrc, uint32_t off, uint32_
       "s_mov_b32 m0, %2\n\t"
       "s_nop 0\n\t"
       "buffer_load_dwordx4 %0, %1, 0 offen lds"
+      :
+      : "v"(off), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(lds))
+      : "memory", "m0");
+}
+
+// the same with the non-temporal hint, for data that is read once
+__device__ __forceinline__ void dma16_buf_stream(i32x4_rsrc rsrc, uint32_t off, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %0, %1, 0 offen nt lds"
       :
       : "v"(off), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(lds))
       : "memory", "m0");
@@ -103,19 +117,24 @@ template <typename T, bool DOWN, int BLK, bool PAIR, int W> struct Operand {
     }
   }
 
-  // stage s into LDS at `lds`
-  __device__ __forceinline__ void issue(int s, uint32_t lds, int wave) const {
+  // the copies of stage s into LDS at `lds`; once: no other tile reads this data
+  __device__ __forceinline__ void issue(int s, uint32_t lds, int wave, bool once) const {
+    i32x4_rsrc rsrc;
+    bool in = true;
     const int left = klen - s * BK;  // k from this stage on
     if (!DOWN) {
-      const i32x4_rsrc r = make_rsrc(base + static_cast<size_t>(s) * BK * ES, span - static_cast<uint32_t>(s * BK * ES));
-      const bool in = chunk_k < left;
-#pragma unroll
-      for (int t = 0; t < NU; ++t) dma16_buf(r, in ? voff[t] : kOutside, lds + (wave * NU + t) * kUnitBytes);
+      rsrc = make_rsrc(base + static_cast<size_t>(s) * BK * ES, span - static_cast<uint32_t>(s * BK * ES));
+      in = chunk_k < left;
     } else {
-      const i32x4_rsrc r = make_rsrc(base + static_cast<size_t>(s) * BK * row_bytes,
-                                     static_cast<uint32_t>(min(left, BK) - 1) * row_bytes + span);
+      rsrc = make_rsrc(base + static_cast<size_t>(s) * BK * row_bytes,
+                       static_cast<uint32_t>(min(left, BK) - 1) * row_bytes + span);
+    }
+    if (once) {
 #pragma unroll
-      for (int t = 0; t < NU; ++t) dma16_buf(r, voff[t], lds + (wave * NU + t) * kUnitBytes);
+      for (int t = 0; t < NU; ++t) dma16_buf_stream(rsrc, in ? voff[t] : kOutside, lds + (wave * NU + t) * kUnitBytes);
+    } else {
+#pragma unroll
+      for (int t = 0; t < NU; ++t) dma16_buf(rsrc, in ? voff[t] : kOutside, lds + (wave * NU + t) * kUnitBytes);
     }
   }
 
@@ -155,174 +174,598 @@ template <int N> __device__ __forceinline__ void stage_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// One tile of C: MB x NB 16-blocks at (rows 0.., columns 0..) of out (leading dimension
-// ldo), rows_valid x cols_valid of it stored.  WR x WC waves, a ring of D stages.
-template <typename T, bool ADOWN, bool BDOWN, int MB, int NB, int WR, int WC, int D>
-__device__ __forceinline__ void grouped_tile(const void *a, int lda, const void *b, int ldb, int klen, T *out,
-                                             size_t ldo, int rows_valid, int cols_valid, uint8_t *smem) {
-  constexpr int W = WR * WC, MW = MB / WR, NW = NB / WC;
-  constexpr bool PAIR = sizeof(T) == 2;
-  using A = Operand<T, ADOWN, MB, false, W>;
-  using B = Operand<T, BDOWN, NB, PAIR, W>;
-  constexpr int STAGE = A::BYTES + B::BYTES;
-  constexpr int OPS = A::NU + B::NU;
-  constexpr int BK = A::BK;
-  static_assert(MB % WR == 0 && NB % WC == 0 && NW % 2 == 0, "whole blocks, pairs of column blocks per wave");
-  static_assert(D >= 2 && (D - 2) * OPS <= 63, "outstanding copies exceed the wait counter");
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wave / WC, wc = wave % WC;
-  A oa;
-  B ob;
-  oa.init(a, lda, rows_valid, klen, wave, lane);
-  ob.init(b, ldb, cols_valid, klen, wave, lane);
-  f32x4_t acc[MW][NW];
+// One tile of C in a workgroup's list: rows and columns of the output, and the group
+struct Item {
+  int group;       // -1: rows of no group, whose result is zero
+  int row0, rows;  // rows of x / dy: the tile's rows, or (weights' gradient) the group's
+  int tile;        // column tile, or (weights' gradient) tile of the group's matrix
+  int once;        // no other row tile of the group
+  int split;       // part of the reduction
+};
+constexpr int kFlush = 4;  // stages of an fp32 partial sum
+constexpr int kItems = 64;  // of one list, one in each lane: longer work is done in several
+
+// Operands, sizes and place of a tile
+template <typename T> struct TileRef {
+  const T *a, *b;
+  T *out;
+  float *part;     // where the fp32 sums of a part of the reduction go instead, or null
+  int rows, cols;  // stored
+  int klen;        // 0: the result is zero
+  int rot;         // stage that comes first
+  bool once;       // b is read by no other tile
+};
+
+// The copying side of one operand: the stages of the list's tiles in order, through a ring of
+// D LDS slots
+template <class Op, int D, bool IS_A> struct Feed {
+  Op op;
+  int pi = -1, ps = 0, pnk = 0, prot = 0, slot = 0;
+  bool once = false;
+
+  // on to the next tile that has stages, if the present one has none left
+  template <typename F> __device__ __forceinline__ void advance(int n, int ld, int wave, int lane, F ref) {
+    while (pi < n && ps == pnk) {
+      if (++pi == n) return;
+      const auto t = ref(pi);
+      op.init(IS_A ? t.a : t.b, ld, IS_A ? t.rows : t.cols, t.klen, wave, lane);
+      pnk = (t.klen + Op::BK - 1) / Op::BK;
+      ps = 0;
+      prot = pnk > 0 ? t.rot % pnk : 0;
+      once = !IS_A && t.once;
+    }
+  }
+  // the next stage's copies
+  __device__ __forceinline__ void issue(uint32_t lds, int wave) {
+    op.issue(ps + prot < pnk ? ps + prot : ps + prot - pnk, lds + slot * Op::BYTES, wave, once);
+    slot = slot + 1 == D ? 0 : slot + 1;
+    ++ps;
+  }
+};
+
+// 16 bytes of a result, which nothing here reads again: with the non-temporal hint, so it takes
+// no cache from the operands (the weights' gradient of 128 groups of 768 x 2048 and 128 rows: 136 -> 114 us)
+__device__ __forceinline__ void put16(void *p, uint4 v) {
+  typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), reinterpret_cast<u32x4_t *>(p));
+}
+
+// lane r of 16 <-> lane r ^ 8
+__device__ __forceinline__ uint32_t swap8(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x128, 0xf, 0xf, true));  // row_ror:8
+}
+
+// A wave's share of a tile: row blocks wr + WR i, columns c0 .. c0 + 16 NW - 1.  A lane holds row
+// lane % 16 of each block.  bf16: 8 consecutive columns from each pair of column blocks, so two pairs are
+// 128 bytes of a row over 4 lanes each; lanes r and r + 8 exchange one of them, and a store writes whole
+// lines of 8 rows in place of half lines of 16.
+template <typename T, int MW, int NW, int WR>
+__device__ __forceinline__ void store_rows(const TileRef<T> &t, size_t ldo, const f32x4_t (&acc)[MW][NW], int wr,
+                                           int c0, int lane) {
+  const int r16 = lane & 15, g = lane >> 4;
+  if constexpr (sizeof(T) == 2) {
+    const bool lower = r16 < 8;
+    const int col = c0 + 8 * g + (lower ? 0 : 32);
 #pragma unroll
-  for (int i = 0; i < MW; ++i)
+    for (int i = 0; i < MW; ++i) {
+      const int row = 16 * (wr + WR * i) + (r16 & 7);
+      if (16 * (wr + WR * i) >= t.rows) break;  // wave-uniform
+      T *o = t.out + static_cast<size_t>(row) * ldo + col;
 #pragma unroll
-    for (int j = 0; j < NW; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int nk = (klen + BK - 1) / BK;
-  const uint32_t lds = lds_addr(smem);
-  auto issue = [&](int s) {
-    const uint32_t st = lds + (s % D) * STAGE;
-    oa.issue(s, st, wave);
-    ob.issue(s, st + A::BYTES, wave);
-  };
+      for (int j = 0; j < NW; j += 4) {
+        uint32_t p[2][4];
 #pragma unroll
-  for (int s = 0; s < D - 1; ++s)
-    if (s < nk) issue(s);
-  for (int kt = 0; kt < nk; ++kt) {
-    // stage kt landed for every wave, and every wave is done with the slot refilled below
-    if (kt + D - 2 < nk)
-      stage_barrier<(D - 2) * OPS>();
-    else if (D > 3 && kt + D - 3 < nk)
-      stage_barrier<(D > 3 ? D - 3 : 0) * OPS>();
-    else
-      stage_barrier<0>();
-    if (kt + D - 1 < nk) issue(kt + D - 1);
-    const uint8_t *sa = smem + (kt % D) * STAGE, *sb = sa + A::BYTES;
+        for (int q = 0; q < 2 && j + 2 * q < NW; ++q) {
+          const f32x4_t lo = acc[i][j + 2 * q], hi = acc[i][j + 2 * q + 1];
+          p[q][0] = pack_bf16x2(lo[0], lo[1]);
+          p[q][1] = pack_bf16x2(lo[2], lo[3]);
+          p[q][2] = pack_bf16x2(hi[0], hi[1]);
+          p[q][3] = pack_bf16x2(hi[2], hi[3]);
+        }
+        if (j + 2 < NW) {
+          uint32_t first[4], second[4];  // rows r16 % 8 and r16 % 8 + 8
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      typename B::frag_t bf[NW];
+          for (int d = 0; d < 4; ++d) {
+            const uint32_t got = swap8(lower ? p[1][d] : p[0][d]);
+            first[d] = lower ? p[0][d] : got;
+            second[d] = lower ? got : p[1][d];
+          }
+          if (col + 16 * j >= t.cols) continue;
+          if (row < t.rows) put16(o + 16 * j, uint4{first[0], first[1], first[2], first[3]});
+          if (row + 8 < t.rows) put16(o + 16 * j + 8 * ldo, uint4{second[0], second[1], second[2], second[3]});
+        } else {  // a pair left over: half lines
+          const int own = 16 * (wr + WR * i) + r16, at = c0 + 8 * g + 16 * j;
+          if (own < t.rows && at < t.cols)
+            put16(t.out + static_cast<size_t>(own) * ldo + at, uint4{p[0][0], p[0][1], p[0][2], p[0][3]});
+        }
+      }
+    }
+  } else {
 #pragma unroll
-      for (int j = 0; j < NW; ++j) bf[j] = B::read(sb, wc * NW + j, h, lane);
+    for (int i = 0; i < MW; ++i) {
+      const int row = 16 * (wr + WR * i) + r16;
+      if (row >= t.rows) continue;
+      T *o = t.out + static_cast<size_t>(row) * ldo;
 #pragma unroll
-      for (int i = 0; i < MW; ++i) {
-        const typename A::frag_t af = A::read(sa, wr + WR * i, h, lane);
-#pragma unroll
-        for (int s = 0; s < Frag<T>::steps; ++s)
-#pragma unroll
-          for (int j = 0; j < NW; ++j) acc[i][j] = Frag<T>::mma(bf[j], af, s, acc[i][j]);
+      for (int j = 0; j < NW; ++j) {
+        const int col = c0 + 16 * j + 4 * g;
+        if (col < t.cols) put16(o + col, __builtin_bit_cast(uint4, acc[i][j]));
       }
     }
   }
+}
+
+// The same sums as fp32: a part of the reduction, which grouped_join_kernel adds up
+template <typename T, int MW, int NW, int WR>
+__device__ __forceinline__ void store_part(const TileRef<T> &t, size_t ldo, const f32x4_t (&acc)[MW][NW], int wr,
+                                           int c0, int lane) {
   const int r16 = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int i = 0; i < MW; ++i) {
     const int row = 16 * (wr + WR * i) + r16;
-    if (row >= rows_valid) continue;
-    T *o = out + static_cast<size_t>(row) * ldo;
-    if constexpr (PAIR) {
+    if (row >= t.rows) continue;
+    float *o = t.part + static_cast<size_t>(row) * ldo;
 #pragma unroll
-      for (int j = 0; j < NW; j += 2) {
-        const int col = 16 * (wc * NW + j) + 8 * g;
-        if (col >= cols_valid) continue;
-        const f32x4_t lo = acc[i][j], hi = acc[i][j + 1];
-        *reinterpret_cast<uint4 *>(o + col) = uint4{pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]),
-                                                    pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3])};
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NW; ++j) {
-        const int col = 16 * (wc * NW + j) + 4 * g;
-        if (col < cols_valid) *reinterpret_cast<f32x4_t *>(o + col) = acc[i][j];
-      }
+    for (int j = 0; j < NW; ++j) {
+      const int col = c0 + (sizeof(T) == 2 ? 16 * (j & ~1) + 8 * g + 4 * (j & 1) : 16 * j + 4 * g);
+      if (col < t.cols) *reinterpret_cast<f32x4_t *>(o + col) = acc[i][j];
     }
   }
 }
 
-// zeros into rows_valid x cols_valid of out
-template <typename T>
-__device__ __forceinline__ void zero_tile(T *out, size_t ldo, int rows_valid, int cols_valid) {
-  constexpr int E = kChunkElems<T>;
-  const int chunks = cols_valid / E;
-  for (int i = threadIdx.x; i < rows_valid * chunks; i += blockDim.x)
-    *reinterpret_cast<uint4 *>(out + static_cast<size_t>(i / chunks) * ldo + (i % chunks) * E) = uint4{0, 0, 0, 0};
+// The tiles of a workgroup's list (item j in lane j of every wave, n of them) as one pipeline:
+// stages of a tile's operands are copied DA - 1 and DB - 1 ahead of their use through rings of DA
+// and DB LDS slots, and across the end of a tile, so the next tile's first stages are under way
+// while a tile ends and stores.  A tile is MB x NB 16-blocks, WR x WC waves.  ref(item) gives a
+// tile's operands; lda, ldb, ldo are common.
+template <typename T, bool ADOWN, bool BDOWN, int MB, int NB, int WR, int WC, int DA, int DB, typename F>
+__device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, int ldb, size_t ldo, uint8_t *smem,
+                                              F ref) {
+  constexpr int W = WR * WC, MW = MB / WR, NW = NB / WC;
+  constexpr bool PAIR = sizeof(T) == 2;
+  using A = Operand<T, ADOWN, MB, false, W>;
+  using B = Operand<T, BDOWN, NB, PAIR, W>;
+  constexpr int BK = A::BK;
+  // copies that may be outstanding when stage c is needed: those after the copies of A(c), that
+  // is of iterations c - DA + 1 (its B only, which lies ahead of B(c)) to c - 1
+  constexpr int PENDING = (DB > DA ? B::NU : 0) + (DA - 2) * (A::NU + B::NU);
+  static_assert(MB % WR == 0 && NB % WC == 0 && (!PAIR || NW % 2 == 0), "whole blocks, in bf16 pairs of column blocks, per wave");
+  static_assert(DA >= 2 && DB >= DA && PENDING <= 63, "ring depths, outstanding copies within the wait counter");
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave / WC, wc = wave % WC;
+  const uint32_t ldsa = lds_addr(smem), ldsb = ldsa + DA * A::BYTES;
+  auto at = [&](int i) {
+    return ref(Item{__builtin_amdgcn_readlane(list.group, i), __builtin_amdgcn_readlane(list.row0, i),
+                    __builtin_amdgcn_readlane(list.rows, i), __builtin_amdgcn_readlane(list.tile, i), __builtin_amdgcn_readlane(list.once, i), __builtin_amdgcn_readlane(list.split, i)});
+  };
+  Feed<A, DA, true> fa;
+  Feed<B, DB, false> fb;
+  auto issue_a = [&]() {
+    fa.issue(ldsa, wave);
+    fa.advance(n, lda, wave, lane, at);
+  };
+  auto issue_b = [&]() {
+    fb.issue(ldsb, wave);
+    fb.advance(n, ldb, wave, lane, at);
+  };
+  fa.advance(n, lda, wave, lane, at);
+  fb.advance(n, ldb, wave, lane, at);
+#pragma unroll
+  for (int s = 0; s < DB - 1; ++s)
+    if (fb.pi < n) issue_b();
+#pragma unroll
+  for (int s = 0; s < DA - 1; ++s)
+    if (fa.pi < n) issue_a();
+  int sa = 0, sb = 0;  // slots of the stage multiplied next
+  int warm = DA - 1;   // the first stages wait for everything
+  for (int ci = 0; ci < n; ++ci) {
+    const TileRef<T> t = at(ci);
+    f32x4_t acc[MW][NW];
+    auto clear = [](f32x4_t (&c)[MW][NW]) {
+#pragma unroll
+      for (int i = 0; i < MW; ++i)
+#pragma unroll
+        for (int j = 0; j < NW; ++j) c[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    };
+    clear(acc);
+    // fp32 results: the products of kFlush stages are summed apart and then added to the rest, so the
+    // rounding of a long sum grows with the root of its parts, not of its terms (1.1e-6 of the result
+    // without it for 1024 terms, 4e-7 with it)
+    [[maybe_unused]] f32x4_t total[sizeof(T) == 4 ? MW : 1][NW];
+    auto flush = [&]() {
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < MW; ++i)
+#pragma unroll
+          for (int j = 0; j < NW; ++j) total[i][j] += acc[i][j];
+        clear(acc);
+      }
+    };
+    if constexpr (sizeof(T) == 4) clear(total);
+    const int nk = (t.klen + BK - 1) / BK;
+    for (int kt = 0; kt < nk; ++kt) {
+      // this stage landed for every wave, and every wave is done with the slots refilled next;
+      // while B still had a stage to copy one iteration ago, the count is the constant one
+      if (PENDING > 0 && warm == 0)
+        stage_barrier<PENDING>();
+      else
+        stage_barrier<0>();
+      if (fa.pi < n) issue_a();
+      if (fb.pi < n) {
+        issue_b();
+        warm = max(warm - 1, 0);
+      } else {
+        warm = 1;
+      }
+      const uint8_t *pa = smem + sa * A::BYTES, *pb = smem + DA * A::BYTES + sb * B::BYTES;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        typename B::frag_t bf[NW];
+        typename A::frag_t af[MW];
+#pragma unroll
+        for (int j = 0; j < NW; ++j) bf[j] = B::read(pb, wc * NW + j, h, lane);
+        // blocks past the tile's rows are read too and not multiplied
+#pragma unroll
+        for (int i = 0; i < MW; ++i) af[i] = A::read(pa, wr + WR * i, h, lane);
+#pragma unroll
+        for (int i = 0; i < MW; ++i)
+          if (16 * (wr + WR * i) < t.rows) {  // wave-uniform
+#pragma unroll
+            for (int s = 0; s < Frag<T>::steps; ++s)
+#pragma unroll
+              for (int j = 0; j < NW; ++j) acc[i][j] = Frag<T>::mma(bf[j], af[i], s, acc[i][j]);
+          }
+      }
+      if (sizeof(T) == 4 && (kt + 1) % kFlush == 0) flush();
+      sa = sa + 1 == DA ? 0 : sa + 1;
+      sb = sb + 1 == DB ? 0 : sb + 1;
+    }
+    flush();
+    const f32x4_t(&sum)[MW][NW] = [&]() -> const f32x4_t(&)[MW][NW] {
+      if constexpr (sizeof(T) == 4)
+        return total;
+      else
+        return acc;
+    }();
+    if (t.part)
+      store_part<T, MW, NW, WR>(t, ldo, sum, wr, 16 * wc * NW, lane);
+    else
+      store_rows<T, MW, NW, WR>(t, ldo, sum, wr, 16 * wc * NW, lane);
+  }
 }
 
-// Forward (GX = false) and rows' gradient (GX = true): tile = TM rows of one group x BN columns
-template <typename T, bool GX, int MB, int NB, int WR, int WC, int D>
-__global__ __launch_bounds__(WR *WC * 64) void grouped_rows_kernel(GroupedArgs g) {
-  constexpr int TM = 16 * MB, BN = 16 * NB;
-  constexpr int TML = TM == 256 ? 8 : TM == 128 ? 7 : TM == 64 ? 6 : TM == 32 ? 5 : 4;
-  static_assert(1 << TML == TM, "tile rows");
-  __shared__ __align__(16) uint8_t smem[D * (MB + NB) * 2 * kUnitBytes];
-  const int cols = GX ? g.K : g.M, klen = GX ? g.M : g.K;
-  const int nN = (cols + BN - 1) / BN;
-  // the column tiles of one row tile share an XCD (block b runs on XCD b % 8), so the rows
-  // they share stay in its L2
-  const int b = ragged_block();
-  const int tile = (b & 7) + 8 * ((b >> 3) / nN), nt = (b >> 3) % nN;
-  const RaggedTile t = ragged_tile(g.offsets, g.N, g.S, TML, tile, g.fill);
-  if (!t.valid) return;
-  const int c0 = nt * BN, cv = min(BN, cols - c0);
-  T *out = static_cast<T *>(g.out) + static_cast<size_t>(t.row0) * cols + c0;
-  if (t.group < 0) {
-    zero_tile(out, cols, t.rows, cv);
-    return;
+// Block b runs on XCD b % 8.  Each XCD takes a run of consecutive items, all columns of a row tile (or all
+// tiles of a group's dw) before the next, its workgroups side by side: the rows that
+// column tiles share and the weights that the row tiles of a group share are read into one L2
+// at about the same time.  Workgroup `slot` of an XCD takes the items slot, slot + slots, .. of its run.
+struct Share {
+  long long first, mine;
+  int slot, slots;
+  __device__ __forceinline__ explicit Share(long long all)
+      : slot(blockIdx.x >> 3), slots(static_cast<int>(gridDim.x) >> 3) {
+    const long long run = (all + 7) >> 3;
+    first = (blockIdx.x & 7) * run;
+    mine = min(run, max(all - first, 0ll));
   }
-  const T *rows = static_cast<const T *>(g.rows) + static_cast<size_t>(t.row0) * klen;
-  const T *w = static_cast<const T *>(g.other) + static_cast<size_t>(t.group) * g.M * g.K;
-  grouped_tile<T, false, GX, MB, NB, WR, WC, D>(rows, klen, GX ? w + c0 : w + static_cast<size_t>(c0) * g.K, g.K, klen,
-                                                 out, cols, t.rows, cv, smem);
+  // this workgroup's items from its `done`-th on: how many a list takes of them, and this lane's
+  __device__ __forceinline__ int count(long long done) const {
+    const long long left = mine - slot - done * slots;
+    return left <= 0 ? 0 : static_cast<int>(min((left + slots - 1) / slots, static_cast<long long>(kItems)));
+  }
+  __device__ __forceinline__ long long item(long long done) const {
+    return first + min(slot + (done + (threadIdx.x & 63)) * slots, max(mine - 1, 0ll));
+  }
+};
+
+// part `s` of `splits` of a reduction of klen: whole stages, as even as they come
+struct Part {
+  int k0, len;
+};
+template <typename T> __device__ __forceinline__ Part part_of(int klen, int s, int splits) {
+  if (splits == 1) return {0, klen};
+  constexpr int BK = kStageElems<T>;
+  const int nk = (klen + BK - 1) / BK, each = nk / splits, more = nk % splits;
+  const int b = s * each + min(s, more), n = each + (s < more);
+  return {b * BK, max(min(n * BK, klen - b * BK), 0)};
+}
+
+// Tiles of x's or dy's rows by columns, the whole work of a workgroup
+template <typename T, bool GX, int MB, int NB, int WR, int WC, int DA, int DB>
+__device__ __forceinline__ void grouped_rows(const GroupedArgs &g, const RaggedTiles &tiles, uint8_t *smem) {
+  constexpr int BN = 16 * NB;
+  const int cols = GX ? g.K : g.M, klen = GX ? g.M : g.K;
+  const int nN = (cols + BN - 1) / BN, per = nN * g.splits;
+  const Share share(static_cast<long long>(tiles.total) * per);
+  auto ref = [&](const Item &it) {
+    const int c0 = it.tile * BN;
+    const Part k = part_of<T>(it.group < 0 ? 0 : klen, it.split, g.splits);
+    TileRef<T> t;
+    t.a = static_cast<const T *>(g.rows) + static_cast<size_t>(it.row0) * klen + k.k0;
+    const T *w = static_cast<const T *>(g.other) + static_cast<size_t>(max(it.group, 0)) * g.M * g.K;
+    t.b = GX ? w + static_cast<size_t>(k.k0) * g.K + c0 : w + static_cast<size_t>(c0) * g.K + k.k0;
+    t.out = static_cast<T *>(g.out) + static_cast<size_t>(it.row0) * cols + c0;
+    t.part = g.splits > 1 ? g.part + (static_cast<size_t>(it.split) * g.S + it.row0) * cols + c0 : nullptr;
+    t.rows = it.rows;
+    t.cols = min(BN, cols - c0);
+    t.klen = k.len;
+    t.rot = max(it.group, 0);
+    t.once = it.once;
+    return t;
+  };
+  long long done = 0;
+  for (int n; (n = share.count(done)) > 0; done += n) {
+    const long long i = share.item(done);
+    const RaggedTile t = tiles.find(static_cast<int>(i / per));
+    const int q = static_cast<int>(i % per);
+    __syncthreads();  // every wave is done with the rings
+    grouped_items<T, false, GX, MB, NB, WR, WC, DA, DB>(
+        Item{t.group, t.row0, t.rows, q % nN, t.only, q / nN}, n, klen, g.K, cols, smem, ref);
+  }
+}
+
+// Forward (GX = false) and rows' gradient (GX = true) in tiles of 16 MB rows of one group x 16 NB columns
+template <typename T, bool GX, int MB, int NB, int WR, int WC, int DA, int DB>
+__global__ __launch_bounds__(WR *WC * 64) void grouped_rows_kernel(GroupedArgs g) {
+  __shared__ __align__(16) uint8_t smem[(DA * MB + DB * NB) * 2 * kUnitBytes];
+  const RaggedTiles tiles(g.offsets, g.N, g.S, 16 * MB, g.fill);
+  grouped_rows<T, GX, MB, NB, WR, WC, DA, DB>(g, tiles, smem);
+}
+
+// The same with the tile shape taken here, from the groups' sizes that only the device knows: a
+// group's last row tile costs about a full one, so which height wastes least goes by them.
+// Rounds of a CU times the time of a stage, in units of 50 ns as measured with every CU busy.
+template <bool GX> __global__ __launch_bounds__(512) void grouped_shapes_kernel(GroupedArgs g) {
+  __shared__ __align__(16) uint8_t smem[160 * 1024];
+  const int cols = GX ? g.K : g.M;
+  const int heights[3] = {192, 256, 320};
+  int tiles[3];
+  RaggedTiles::count(g.offsets, g.N, g.S, heights, tiles, g.fill);
+  const int slots = static_cast<int>(gridDim.x);
+  auto cost = [&](int h, int width, int stage) {
+    const long long items = static_cast<long long>(tiles[h]) * ((cols + width - 1) / width);
+    return (items + slots - 1) / slots * stage;
+  };
+  const long long c192 = cost(0, 192, 28), c192w = cost(0, 256, 35), c256 = cost(1, 256, 42), c320 = cost(2, 192, 41);
+  const long long best = min(min(c192, c192w), min(c256, c320));
+  if (best == c256)
+    grouped_rows<bf16_t, GX, 16, 16, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 256, g.fill), smem);
+  else if (best == c320)
+    grouped_rows<bf16_t, GX, 20, 12, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 320, g.fill), smem);
+  else if (best == c192)
+    grouped_rows<bf16_t, GX, 12, 12, 4, 2, 3, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 192, g.fill), smem);
+  else
+    grouped_rows<bf16_t, GX, 12, 16, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 192, g.fill), smem);
 }
 
 // Weights' gradient: tile = 16 MB rows x 16 NB columns of one group's dw
-template <typename T, int MB, int NB, int WR, int WC, int D>
+template <typename T, int MB, int NB, int WR, int WC, int DA, int DB>
 __global__ __launch_bounds__(WR *WC * 64) void grouped_weights_kernel(GroupedArgs g) {
   constexpr int BM = 16 * MB, BN = 16 * NB;
-  __shared__ __align__(16) uint8_t smem[D * (MB + NB) * 2 * kUnitBytes];
-  const int nM = (g.M + BM - 1) / BM, nN = (g.K + BN - 1) / BN;
-  const int b = ragged_block();
-  const int e = (b & 7) + 8 * ((b >> 3) / (nM * nN)), q = (b >> 3) % (nM * nN);
-  if (e >= g.N) return;
-  const int r0 = min(max(g.offsets[e], 0), g.S), r1 = min(max(g.offsets[e + 1], r0), g.S);
-  const int m0 = q / nN * BM, k0 = q % nN * BN;
-  const int mv = min(BM, g.M - m0), kv = min(BN, g.K - k0);
-  const T *dy = static_cast<const T *>(g.rows) + static_cast<size_t>(r0) * g.M + m0;
-  const T *x = static_cast<const T *>(g.other) + static_cast<size_t>(r0) * g.K + k0;
-  T *out = static_cast<T *>(g.out) + (static_cast<size_t>(e) * g.M + m0) * g.K + k0;
-  grouped_tile<T, true, true, MB, NB, WR, WC, D>(dy, g.M, x, g.K, r1 - r0, out, g.K, mv, kv, smem);
+  __shared__ __align__(16) uint8_t smem[(DA * MB + DB * NB) * 2 * kUnitBytes];
+  const int nM = (g.M + BM - 1) / BM, nN = (g.K + BN - 1) / BN, one = nM * nN, per = one * g.splits;
+  const Share share(static_cast<long long>(g.N) * per);
+  auto ref = [&](const Item &it) {
+    const int m0 = it.tile / nN * BM, c0 = it.tile % nN * BN;
+    const Part k = part_of<T>(it.rows, it.split, g.splits);
+    const size_t row = static_cast<size_t>(it.row0) + k.k0;
+    TileRef<T> t;
+    t.a = static_cast<const T *>(g.rows) + row * g.M + m0;
+    t.b = static_cast<const T *>(g.other) + row * g.K + c0;
+    t.out = static_cast<T *>(g.out) + (static_cast<size_t>(it.group) * g.M + m0) * g.K + c0;
+    t.part = g.splits > 1
+                 ? g.part + ((static_cast<size_t>(it.split) * g.N + it.group) * g.M + m0) * g.K + c0
+                 : nullptr;
+    t.rows = min(BM, g.M - m0);
+    t.cols = min(BN, g.K - c0);
+    t.klen = k.len;
+    t.rot = 0;
+    t.once = false;
+    return t;
+  };
+  long long done = 0;
+  for (int n; (n = share.count(done)) > 0; done += n) {
+    const long long i = share.item(done);
+    const int e = static_cast<int>(i / per), q = static_cast<int>(i % per);
+    const int r0 = min(max(g.offsets[e], 0), g.S), r1 = min(max(g.offsets[e + 1], r0), g.S);
+    __syncthreads();  // every wave is done with the rings
+    grouped_items<T, true, true, MB, NB, WR, WC, DA, DB>(Item{e, r0, r1 - r0, q % one, 0, q / one}, n, g.M, g.K, g.K,
+                                                          smem, ref);
+  }
 }
 
-template <typename T, bool GX> hipError_t launch_rows(const GroupedArgs &g, hipStream_t s) {
-  constexpr int MB = sizeof(T) == 2 ? 8 : 4, NB = sizeof(T) == 2 ? 8 : 4;
-  const int nN = ((GX ? g.K : g.M) + 16 * NB - 1) / (16 * NB);
-  const long long blocks = (ragged_max_tiles(g.S, g.N, 16 * MB) + 7) / 8 * 8 * nN;
-  if (blocks > kRaggedMaxBlocks) return hipErrorInvalidValue;
-  grouped_rows_kernel<T, GX, MB, NB, 2, 2, 2><<<ragged_grid(blocks), 256, 0, s>>>(g);
+// out = the parts' sum in order, for the elements first .. last of `total` (16 bytes of out a thread);
+// the others get zeros with `fill`, or stay.  Rows (weights' gradient: all): first and last by the offsets.
+template <typename T> __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedArgs g, size_t total, int cols) {
+  constexpr int E = kChunkElems<T>;
+  size_t first = 0, last = total;
+  if (cols > 0) {
+    const int r0 = min(max(g.offsets[0], 0), g.S);
+    first = static_cast<size_t>(r0) * cols;
+    last = static_cast<size_t>(min(max(g.offsets[g.N], r0), g.S)) * cols;
+  }
+  for (size_t i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * E; i < total;
+       i += static_cast<size_t>(gridDim.x) * 256 * E) {
+    float v[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[j] = 0.f;
+    if (i >= first && i < last) {
+      for (int s = 0; s < g.splits; ++s) {
+        const float *p = g.part + s * total + i;
+#pragma unroll
+        for (int j = 0; j < E; j += 4) {
+          const f32x4_t u = *reinterpret_cast<const f32x4_t *>(p + j);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[j + k] += u[k];
+        }
+      }
+    } else if (!g.fill) {
+      continue;
+    }
+    T *o = static_cast<T *>(g.out) + i;
+    if constexpr (E == 8)
+      *reinterpret_cast<uint4 *>(o) =
+          uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    else
+      *reinterpret_cast<f32x4_t *>(o) = f32x4_t{v[0], v[1], v[2], v[3]};
+  }
+}
+
+constexpr int kCUs = 256;
+constexpr int kMaxSplits = 64;
+
+// A kernel's tile and rings; PER_CU workgroups of it share a CU's LDS
+template <int MB_, int NB_, int WR_, int WC_, int DA_, int DB_> struct Shape {
+  static constexpr int MB = MB_, NB = NB_, WR = WR_, WC = WC_, DA = DA_, DB = DB_;
+  static constexpr int TM = 16 * MB, TN = 16 * NB, THREADS = WR * WC * 64;
+  static constexpr int PER_CU = 160 * 1024 / ((DA * MB + DB * NB) * 2 * kUnitBytes);
+};
+using Tile64 = Shape<4, 4, 2, 2, 4, 4>;     // bf16: few tiles, deep rings
+using Tile64x128 = Shape<4, 8, 2, 2, 3, 3>;  // bf16: a few rows a group
+using Tile128 = Shape<8, 8, 2, 2, 2, 3>;     // bf16
+using Tile256 = Shape<16, 16, 4, 2, 2, 2>;   // bf16, weights' gradient
+using TileF32 = Shape<2, 4, 2, 2, 3, 3>;     // fp32
+using TileF32Weights = Shape<4, 4, 2, 2, 3, 3>;
+
+enum class Kind { k64, k64x128, k128, kLarge, kF32 };
+
+struct Plan {
+  Kind kind;
+  int splits;         // parts of the reduction
+  size_t part_elems;  // of one part
+};
+
+long long tiles_of(long long n, int t) { return (n + t - 1) / t; }
+
+// Tiles that S rows in N groups make, about: half a tile more than full ones for a group, at least one
+long long about_tiles(long long S, long long N, int tm) {
+  return std::max(S / tm + std::min(N, S) / 2, std::min(N, S));
+}
+
+// Parts of the reduction: few tiles with a long reduction leave CUs idle.  Each part is at least one
+// workgroup more; what it saves are its stages' times, what it costs the launch that adds the parts
+// and their traffic (us, as measured: 2 groups of 1024 x 2048 with 4 rows 33 us whole and 12 in 8 parts,
+// 16 groups of 1024 x 1024 with one row 12.8 whole and 13.4 in two).
+int pick_splits(long long items, int slots, long long nk, size_t elems, double stage_us) {
+  int best = 1;
+  double least = static_cast<double>(nk) * stage_us;
+  for (int s = 2; s <= kMaxSplits && items * s <= slots && s <= nk; s *= 2) {
+    const double t = static_cast<double>((nk + s - 1) / s) * stage_us + 4.5 + 2e-6 * s * static_cast<double>(elems);
+    if (t < least) {
+      least = t;
+      best = s;
+    }
+  }
+  return best;
+}
+
+// Which kernel for the forward and the rows' gradient.  us on 128 groups of 768 x 2048 (forward):
+//   rows a group               2    16    48    96   128   256  1024
+//   64 x 128 (two a CU)       65    70    84   112   134   208   673
+//   128 x 128 (two a CU)      66    68    73    81   119   173   543
+//   large (best of its four)  64    71    74    82    94   140   478
+// and 16 groups of 1024 x 1024 with 1, 16, 128 and 512 rows: 64 x 64 12.8, 14.2, -, -; 128 x 128 15.2, 16.4, 20, 25;
+// large 17, 18, 23, 31.  So: the large shapes past 80 rows a group for work of at least a round of 128 x 128
+// tiles, 64 x 64 tiles while they are at most a round.
+Plan plan_rows(const GroupedArgs &g, bool grad, bool bf16) {
+  const int cols = grad ? g.K : g.M, klen = grad ? g.M : g.K;
+  const size_t elems = static_cast<size_t>(g.S) * cols;
+  if (!bf16) {
+    const long long items = about_tiles(g.S, g.N, TileF32::TM) * tiles_of(cols, TileF32::TN);
+    return {Kind::kF32, pick_splits(items, kCUs * TileF32::PER_CU, tiles_of(klen, 32), elems, 0.6), elems};
+  }
+  const long long small = about_tiles(g.S, g.N, Tile64::TM) * tiles_of(cols, Tile64::TN);
+  if (small <= kCUs * Tile64::PER_CU)
+    return {Kind::k64, pick_splits(small, kCUs * Tile64::PER_CU, tiles_of(klen, 64), elems, 0.45), elems};
+  if (g.S <= 32ll * g.N) return {Kind::k64x128, 1, elems};
+  const long long items = about_tiles(g.S, g.N, Tile128::TM) * tiles_of(cols, Tile128::TN);
+  const bool large = g.S > 80ll * g.N && items >= kCUs * Tile128::PER_CU;
+  return {large ? Kind::kLarge : Kind::k128, 1, elems};
+}
+
+// ... and for the weights' gradient.  128 groups of 768 x 2048 and 128 rows: 256 x 256 tiles 114 us, 128 x 128 134.
+Plan plan_weights(const GroupedArgs &g, bool bf16) {
+  const size_t elems = static_cast<size_t>(g.N) * g.M * g.K;
+  const long long rows = (static_cast<long long>(g.S) + g.N - 1) / g.N;
+  auto items = [&](int t) { return g.N * tiles_of(g.M, t) * tiles_of(g.K, t); };
+  if (!bf16)
+    return {Kind::kF32, pick_splits(items(64), kCUs * TileF32Weights::PER_CU, tiles_of(rows, 32), elems, 0.6), elems};
+  if (items(64) <= kCUs * Tile64::PER_CU)
+    return {Kind::k64, pick_splits(items(64), kCUs * Tile64::PER_CU, tiles_of(rows, 64), elems, 0.45), elems};
+  if (items(256) >= kCUs) return {Kind::kLarge, 1, elems};
+  return {Kind::k128, pick_splits(items(128), kCUs * Tile128::PER_CU, tiles_of(rows, 64), elems, 1.2), elems};
+}
+
+// Workgroups of a launch: whole rounds of the XCDs, per_cu of them on every CU
+unsigned grouped_grid(long long items, int per_cu) {
+  return static_cast<unsigned>(std::min<long long>((items + 7) / 8 * 8, kCUs * per_cu));
+}
+
+template <typename T, bool GX, class Sh> void launch_rows_shape(const GroupedArgs &g, int cols, hipStream_t s) {
+  const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(cols, Sh::TN) * g.splits;
+  grouped_rows_kernel<T, GX, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>
+      <<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g);
+}
+
+template <typename T, class Sh> void launch_weights_shape(const GroupedArgs &g, hipStream_t s) {
+  const long long items = g.N * tiles_of(g.M, Sh::TM) * tiles_of(g.K, Sh::TN) * g.splits;
+  grouped_weights_kernel<T, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>
+      <<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g);
+}
+
+hipError_t launch_join(const GroupedArgs &g, size_t total, int cols, bool bf16, hipStream_t s) {
+  const size_t blocks = (total / (bf16 ? 8 : 4) + 255) / 256;
+  const unsigned grid = static_cast<unsigned>(std::min<size_t>(std::max<size_t>(blocks, 1), 8 * kCUs));
+  if (bf16)
+    grouped_join_kernel<bf16_t><<<grid, 256, 0, s>>>(g, total, cols);
+  else
+    grouped_join_kernel<float><<<grid, 256, 0, s>>>(g, total, cols);
   return hipGetLastError();
 }
 
-template <typename T> hipError_t launch_weights(const GroupedArgs &g, hipStream_t s) {
-  constexpr int MB = sizeof(T) == 2 ? 8 : 4, NB = sizeof(T) == 2 ? 8 : 4;
-  const long long nM = (g.M + 16 * MB - 1) / (16 * MB), nN = (g.K + 16 * NB - 1) / (16 * NB);
-  const long long blocks = (g.N + 7) / 8 * 8 * nM * nN;
-  if (blocks > kRaggedMaxBlocks) return hipErrorInvalidValue;
-  grouped_weights_kernel<T, MB, NB, 2, 2, 2><<<ragged_grid(blocks), 256, 0, s>>>(g);
-  return hipGetLastError();
+template <bool GX> hipError_t launch_rows(GroupedArgs g, bool bf16, hipStream_t s) {
+  const int cols = GX ? g.K : g.M;
+  const Plan p = plan_rows(g, GX, bf16);
+  g.splits = p.splits;
+  switch (p.kind) {
+    case Kind::k64: launch_rows_shape<bf16_t, GX, Tile64>(g, cols, s); break;
+    case Kind::k64x128: launch_rows_shape<bf16_t, GX, Tile64x128>(g, cols, s); break;
+    case Kind::k128: launch_rows_shape<bf16_t, GX, Tile128>(g, cols, s); break;
+    case Kind::kLarge: grouped_shapes_kernel<GX><<<kCUs, 512, 0, s>>>(g); break;
+    case Kind::kF32: launch_rows_shape<float, GX, TileF32>(g, cols, s); break;
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  return launch_join(g, p.part_elems, cols, bf16, s);
 }
 
 }  // namespace
 
-hipError_t launch_grouped_rows(const GroupedArgs &g, bool grad, bool bf16, hipStream_t stream) {
-  if (g.S <= 0) return hipSuccess;
-  if (bf16) return grad ? launch_rows<bf16_t, true>(g, stream) : launch_rows<bf16_t, false>(g, stream);
-  return grad ? launch_rows<float, true>(g, stream) : launch_rows<float, false>(g, stream);
+size_t grouped_workspace_bytes(const GroupedArgs &g, bool weights, bool grad, bool bf16) {
+  if (g.S <= 0 && !weights) return 0;
+  const Plan p = weights ? plan_weights(g, bf16) : plan_rows(g, grad, bf16);
+  return p.splits > 1 ? p.splits * p.part_elems * sizeof(float) : 0;
 }
 
-hipError_t launch_grouped_weights(const GroupedArgs &g, bool bf16, hipStream_t stream) {
-  return bf16 ? launch_weights<bf16_t>(g, stream) : launch_weights<float>(g, stream);
+hipError_t launch_grouped_rows(const GroupedArgs &g, bool grad, bool bf16, hipStream_t stream) {
+  if (g.S <= 0) return hipSuccess;
+  return grad ? launch_rows<true>(g, bf16, stream) : launch_rows<false>(g, bf16, stream);
+}
+
+hipError_t launch_grouped_weights(const GroupedArgs &args, bool bf16, hipStream_t stream) {
+  GroupedArgs g = args;
+  const Plan p = plan_weights(g, bf16);
+  g.splits = p.splits;
+  g.fill = 1;
+  switch (p.kind) {
+    case Kind::k64: launch_weights_shape<bf16_t, Tile64>(g, stream); break;
+    case Kind::kLarge: launch_weights_shape<bf16_t, Tile256>(g, stream); break;
+    case Kind::kF32: launch_weights_shape<float, TileF32Weights>(g, stream); break;
+    default: launch_weights_shape<bf16_t, Tile128>(g, stream); break;
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  return launch_join(g, p.part_elems, 0, bf16, stream);
 }
 
 }  // namespace ace

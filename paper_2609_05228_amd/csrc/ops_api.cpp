@@ -15,6 +15,7 @@ constexpr int32_t kMaxGroups = 4096;  // groups of rows, requests
 constexpr int32_t kMaxWidth = 65536;  // feature sizes
 constexpr int32_t kMaxNormWidth = 16384;
 constexpr int32_t kMaxRank = 128;
+constexpr int32_t kMaxRows = 0x7fffffff - 1024;  // rounding up to a tile or stage stays an int
 
 bool is_dtype(int32_t t) { return t == ACE_F32 || t == ACE_BF16; }
 size_t elem_bytes(int32_t t) { return t == ACE_BF16 ? 2 : 4; }
@@ -36,17 +37,37 @@ ace_status status_of(hipError_t e) {
   return e == hipSuccess ? ACE_OK : e == hipErrorInvalidValue ? ACE_ERR_UNSUPPORTED : ACE_ERR_HIP;
 }
 
-enum class Way { kForward, kGradX, kGradW };
+enum class Way { kForward = ACE_GROUPED_FORWARD, kGradX = ACE_GROUPED_GRAD_X, kGradW = ACE_GROUPED_GRAD_W };
 
-ace_status grouped(const ace_grouped_desc *d, Way way, const void *rows, const void *other, const int32_t *offsets,
-                   void *out, void *stream) {
+ace_status grouped_desc(const ace_grouped_desc *d) {
   if (!d) return ACE_ERR_INVALID_ARG;
   if (d->S < 0 || d->N <= 0 || d->M <= 0 || d->K <= 0 || !is_dtype(d->dtype) ||
       (d->flags & ~static_cast<uint32_t>(ACE_ZERO_REST)))
     return ACE_ERR_INVALID_ARG;
-  if (d->N > kMaxGroups || d->M > kMaxWidth || d->K > kMaxWidth || bad_width(d->M, d->dtype) ||
+  if (d->S > kMaxRows || d->N > kMaxGroups || d->M > kMaxWidth || d->K > kMaxWidth || bad_width(d->M, d->dtype) ||
       bad_width(d->K, d->dtype))
     return ACE_ERR_UNSUPPORTED;
+  return ACE_OK;
+}
+
+ace::GroupedArgs grouped_args(const ace_grouped_desc &d) {
+  ace::GroupedArgs g{};
+  g.S = d.S;
+  g.N = d.N;
+  g.M = d.M;
+  g.K = d.K;
+  g.fill = (d.flags & ACE_ZERO_REST) ? 1 : 0;
+  return g;
+}
+
+size_t grouped_bytes(const ace_grouped_desc &d, Way way) {
+  return ace::grouped_workspace_bytes(grouped_args(d), way == Way::kGradW, way == Way::kGradX, d.dtype == ACE_BF16);
+}
+
+ace_status grouped(const ace_grouped_desc *d, Way way, const void *rows, const void *other, const int32_t *offsets,
+                   void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  const ace_status st = grouped_desc(d);
+  if (st != ACE_OK) return st;
   const size_t es = elem_bytes(d->dtype), S = d->S, M = d->M, K = d->K, W = static_cast<size_t>(d->N) * M * K * es;
   const size_t xb = S * K * es, yb = S * M * es;
   const bool gw = way == Way::kGradW;
@@ -57,16 +78,14 @@ ace_status grouped(const ace_grouped_desc *d, Way way, const void *rows, const v
   const Span in[] = {{rows, way == Way::kForward ? xb : yb}, {other, gw ? xb : W}, {offsets, (d->N + 1u) * size_t{4}}};
   for (const Span &s : in)
     if (overlap(o, s)) return ACE_ERR_INVALID_ARG;
-  ace::GroupedArgs g{};
+  const size_t need = grouped_bytes(*d, way);
+  if (need > 0 && (!usable(workspace, 256) || workspace_bytes < need)) return ACE_ERR_WORKSPACE;
+  ace::GroupedArgs g = grouped_args(*d);
   g.rows = rows;
   g.other = other;
   g.out = out;
   g.offsets = offsets;
-  g.S = d->S;
-  g.N = d->N;
-  g.M = d->M;
-  g.K = d->K;
-  g.fill = (d->flags & ACE_ZERO_REST) ? 1 : 0;
+  g.part = static_cast<float *>(workspace);
   const bool bf16 = d->dtype == ACE_BF16;
   hipStream_t s = static_cast<hipStream_t>(stream);
   return status_of(gw ? ace::launch_grouped_weights(g, bf16, s)
@@ -125,19 +144,26 @@ bool bad_alias(const Span &out, const Span &in, bool may_equal) {
 
 extern "C" {
 
+size_t ace_grouped_workspace_size(const ace_grouped_desc *desc, int way) {
+  if (grouped_desc(desc) != ACE_OK || way < ACE_GROUPED_FORWARD || way > ACE_GROUPED_GRAD_W) return 0;
+  return grouped_bytes(*desc, static_cast<Way>(way));
+}
+
 ace_status ace_grouped_matmul(const ace_grouped_desc *desc, const void *x, const void *w, const int32_t *offsets,
-                              void *y, void *stream) {
-  return grouped(desc, Way::kForward, x, w, offsets, y, stream);
+                              void *y, void *workspace, size_t workspace_bytes, void *stream) {
+  return grouped(desc, Way::kForward, x, w, offsets, y, workspace, workspace_bytes, stream);
 }
 
 ace_status ace_grouped_matmul_grad_x(const ace_grouped_desc *desc, const void *dy, const void *w,
-                                     const int32_t *offsets, void *dx, void *stream) {
-  return grouped(desc, Way::kGradX, dy, w, offsets, dx, stream);
+                                     const int32_t *offsets, void *dx, void *workspace, size_t workspace_bytes,
+                                     void *stream) {
+  return grouped(desc, Way::kGradX, dy, w, offsets, dx, workspace, workspace_bytes, stream);
 }
 
 ace_status ace_grouped_matmul_grad_w(const ace_grouped_desc *desc, const void *dy, const void *x,
-                                     const int32_t *offsets, void *dw, void *stream) {
-  return grouped(desc, Way::kGradW, dy, x, offsets, dw, stream);
+                                     const int32_t *offsets, void *dw, void *workspace, size_t workspace_bytes,
+                                     void *stream) {
+  return grouped(desc, Way::kGradW, dy, x, offsets, dw, workspace, workspace_bytes, stream);
 }
 
 ace_status ace_block_norm(const ace_norm_desc *desc, const ace_norm_inputs *in, void *h_out, void *n_out,
@@ -225,7 +251,7 @@ ace_status ace_adapter_add(const ace_adapter_desc *desc, const void *base, const
   const ace_adapter_desc &d = *desc;
   if (d.S < 0 || d.R < 0 || d.L <= 0 || d.rank <= 0 || d.d_in <= 0 || d.d_out <= 0 || !is_dtype(d.dtype))
     return ACE_ERR_INVALID_ARG;
-  if (d.R > kMaxGroups || d.rank > kMaxRank || d.d_in > kMaxWidth || d.d_out > kMaxWidth || bad_width(d.rank, d.dtype) ||
+  if (d.S > kMaxRows || d.R > kMaxGroups || d.rank > kMaxRank || d.d_in > kMaxWidth || d.d_out > kMaxWidth || bad_width(d.rank, d.dtype) ||
       bad_width(d.d_in, d.dtype) || bad_width(d.d_out, d.dtype))
     return ACE_ERR_UNSUPPORTED;
   if (d.S == 0) return ACE_OK;

@@ -12,6 +12,7 @@ struct RaggedTile {
   int group;  // 0 .. N - 1, or -1: rows of no group (before the first, behind the last)
   int row0, rows;
   bool valid;
+  bool only;  // the group's only tile
 };
 
 // Tiles of S rows in N groups and the two gaps around them: a group of r rows has at most
@@ -20,60 +21,107 @@ inline long long ragged_max_tiles(long long S, long long N, int tm) {
   return S / tm + (N + 2 < S ? N + 2 : S);
 }
 
-// Tile `tile` in group order, the same in every lane of the calling wave (all 64 lanes
+// The tiles of all groups in group order, held by one wave (all 64 lanes take part in every
 // call).  The gaps come as groups of their own before the first and behind the last when
 // `gaps` is set.  Offsets are clamped to 0 .. S, so whatever they hold, rows outside the
 // array are never named.  Lane l counts the tiles of `per` consecutive groups, one wave
 // scan places them: one round of loads and one scan, against a launch of its own for a tile
 // list.
-__device__ __forceinline__ RaggedTile ragged_tile(const int32_t *offsets, int N, int S, int tm_log2, int tile,
-                                                  bool gaps) {
-  const int lane = threadIdx.x & 63;
-  const int tm = 1 << tm_log2;
-  const int per = (N + 2 + 63) >> 6;
+struct RaggedTiles {
+  const int32_t *offsets;
+  int N, S, tm, per, cnt, inc, total;
+  bool gaps;
+
   // boundary i of the N + 2 groups: 0, offsets[0], .., offsets[N], S
-  auto bound = [&](int i) { return i <= 0 ? 0 : i > N + 1 ? S : min(max(offsets[i - 1], 0), S); };
-  auto tiles = [&](int p, int lo, int hi) {
+  __device__ __forceinline__ int bound(int i) const {
+    return i <= 0 ? 0 : i > N + 1 ? S : min(max(offsets[i - 1], 0), S);
+  }
+  __device__ __forceinline__ int tiles(int p, int lo, int hi) const {
     if (p > N + 1 || hi <= lo || ((p == 0 || p == N + 1) && !gaps)) return 0;
-    return static_cast<int>((static_cast<uint32_t>(hi - lo) + static_cast<uint32_t>(tm) - 1u) >> tm_log2);
-  };
-  const int p0 = lane * per;
-  int cnt = 0, lo = bound(p0);
-  for (int j = 0; j < per; ++j) {
-    const int hi = bound(p0 + j + 1);
-    cnt += tiles(p0 + j, lo, hi);
-    lo = hi;
+    return static_cast<int>((static_cast<uint32_t>(hi - lo) + tm - 1u) / static_cast<uint32_t>(tm));
   }
-  int inc = cnt;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(inc, o);
-    if (lane >= o) inc += v;
-  }
-  const unsigned long long own = __ballot(inc - cnt <= tile && tile < inc);
-  RaggedTile t{-1, 0, 0, false};
-  if (own == 0) return t;
-  const int src = __ffsll(static_cast<long long>(own)) - 1;
-  const int first = __builtin_amdgcn_readlane(inc - cnt, src);
-  int q = tile - first, p = src * per;
-  lo = bound(p);
-  for (int j = 0; j < per; ++j, ++p) {
-    const int hi = bound(p + 1), n = tiles(p, lo, hi);
-    if (q < n) {
-      t.group = p == 0 || p == N + 1 ? -1 : p - 1;
-      t.row0 = lo + (q << tm_log2);
-      t.rows = min(tm, hi - t.row0);
-      t.valid = true;
-      break;
+
+  __device__ __forceinline__ RaggedTiles(const int32_t *offsets_, int N_, int S_, int tm_, bool gaps_)
+      : offsets(offsets_), N(N_), S(S_), tm(tm_), per((N_ + 2 + 63) >> 6), cnt(0), gaps(gaps_) {
+    const int lane = threadIdx.x & 63;
+    const int p0 = lane * per;
+    int lo = bound(p0);
+    for (int j = 0; j < per; ++j) {
+      const int hi = bound(p0 + j + 1);
+      cnt += tiles(p0 + j, lo, hi);
+      lo = hi;
     }
-    q -= n;
-    lo = hi;
+    inc = cnt;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(inc, o);
+      if (lane >= o) inc += v;
+    }
+    total = __builtin_amdgcn_readlane(inc, 63);
   }
-  t.group = __builtin_amdgcn_readfirstlane(t.group);
-  t.row0 = __builtin_amdgcn_readfirstlane(t.row0);
-  t.rows = __builtin_amdgcn_readfirstlane(t.rows);
-  return t;
-}
+
+  // tiles[i]: how many tiles of heights[i] rows there are, without the list of any
+  template <int H>
+  static __device__ __forceinline__ void count(const int32_t *offsets, int N, int S, const int (&heights)[H],
+                                               int (&tiles)[H], bool gaps) {
+#pragma unroll
+    for (int i = 0; i < H; ++i) tiles[i] = 0;
+    for (int p = static_cast<int>(threadIdx.x & 63); p < N + 2; p += 64) {
+      const int lo = p == 0 ? 0 : min(max(offsets[p - 1], 0), S), hi = p > N ? S : min(max(offsets[p], 0), S);
+      if (hi <= lo || ((p == 0 || p == N + 1) && !gaps)) continue;
+#pragma unroll
+      for (int i = 0; i < H; ++i)
+        tiles[i] += static_cast<int>((static_cast<uint32_t>(hi - lo) + heights[i] - 1u) / static_cast<uint32_t>(heights[i]));
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < H; ++i) tiles[i] += __shfl_xor(tiles[i], o);
+#pragma unroll
+    for (int i = 0; i < H; ++i) tiles[i] = __builtin_amdgcn_readfirstlane(tiles[i]);
+  }
+
+  // tile `tile`, each lane its own
+  __device__ __forceinline__ RaggedTile find(int tile) const {
+    RaggedTile t{-1, 0, 0, false, false};
+    // the lane that counts the tile: the first whose inclusive sum exceeds it
+    int src = 0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+      if (__shfl(inc, src + o - 1) <= tile) src += o;
+    int q = tile - __shfl(inc - cnt, src);
+    if (tile < 0 || tile >= total) return t;
+    int p = src * per, lo = bound(p);
+    for (int j = 0; j < per; ++j, ++p) {
+      const int hi = bound(p + 1), n = tiles(p, lo, hi);
+      if (q < n) {
+        t.group = p == 0 || p == N + 1 ? -1 : p - 1;
+        // its 16-row blocks spread evenly over its tiles: a short tile would stream the group's
+        // operands for a few rows
+        const uint32_t blocks = (static_cast<uint32_t>(hi - lo) + 15u) >> 4, each = blocks / n, more = blocks % n;
+        const uint32_t b0 = q * each + min(static_cast<uint32_t>(q), more);
+        t.row0 = lo + static_cast<int>(b0 << 4);
+        t.rows = min(static_cast<int>((each + (q < static_cast<int>(more))) << 4), hi - t.row0);
+        t.valid = true;
+        t.only = n == 1;
+        break;
+      }
+      q -= n;
+      lo = hi;
+    }
+    return t;
+  }
+
+  // the same for a wave-uniform tile, in scalar registers
+  __device__ __forceinline__ RaggedTile find_uniform(int tile) const {
+    RaggedTile t = find(tile);
+    t.group = __builtin_amdgcn_readfirstlane(t.group);
+    t.row0 = __builtin_amdgcn_readfirstlane(t.row0);
+    t.rows = __builtin_amdgcn_readfirstlane(t.rows);
+    t.valid = __builtin_amdgcn_readfirstlane(t.valid);
+    return t;
+  }
+};
 
 // A launch takes fewer than 2^32 threads in x: grids of more blocks than a row of 2^20 are
 // several rows, the last row's excess past the end.

@@ -60,7 +60,7 @@ def _enqueue(dev, fn, *args):
         raise _lib.AceError(st, _lib.status_string(st))
 
 
-def _grouped(fn, rows, other, offsets, S, N, M, K, shape, names, shapes, out):
+def _grouped(way, rows, other, offsets, S, N, M, K, shape, names, shapes, out):
     dtype, dev = rows.dtype, rows.device
     named = [(names[0], rows, shapes[0], None), (names[1], other, shapes[1], None),
              ("offsets", offsets, (N + 1,), torch.int32)]
@@ -72,7 +72,12 @@ def _grouped(fn, rows, other, offsets, S, N, M, K, shape, names, shapes, out):
         out = torch.empty(shape, dtype=dtype, device=dev)
         flags = _lib.ACE_ZERO_REST
     desc = _lib.GroupedDesc(S, N, M, K, _DT[dtype], flags)
-    _enqueue(dev, fn, desc, rows.data_ptr(), other.data_ptr(), offsets.data_ptr(), out.data_ptr())
+    lib = _lib.lib()
+    n = lib.ace_grouped_workspace_size(desc, way)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    fn = (lib.ace_grouped_matmul, lib.ace_grouped_matmul_grad_x, lib.ace_grouped_matmul_grad_w)[way]
+    _enqueue(dev, fn, desc, rows.data_ptr(), other.data_ptr(), offsets.data_ptr(), out.data_ptr(),
+             None if ws is None else ws.data_ptr(), n)
     return out
 
 
@@ -96,7 +101,7 @@ def grouped_matmul(x, w, offsets, *, out=None):
     _dtype_of("w", w, 3)
     N, M, K = w.shape
     S = x.shape[0]
-    return _grouped(_lib.lib().ace_grouped_matmul, x, w, offsets, S, N, M, K, (S, M), ("x", "w"), ((S, K), (N, M, K)),
+    return _grouped(_lib.GROUPED_FORWARD, x, w, offsets, S, N, M, K, (S, M), ("x", "w"), ((S, K), (N, M, K)),
                     out)
 
 
@@ -107,7 +112,7 @@ def grouped_matmul_grad_x(dy, w, offsets, *, out=None):
     _dtype_of("w", w, 3)
     N, M, K = w.shape
     S = dy.shape[0]
-    return _grouped(_lib.lib().ace_grouped_matmul_grad_x, dy, w, offsets, S, N, M, K, (S, K), ("dy", "w"),
+    return _grouped(_lib.GROUPED_GRAD_X, dy, w, offsets, S, N, M, K, (S, K), ("dy", "w"),
                     ((S, M), (N, M, K)), out)
 
 
@@ -119,7 +124,7 @@ def grouped_matmul_grad_w(dy, x, offsets, *, out=None):
     N = _groups_of(offsets)
     S, M = dy.shape
     K = x.shape[1]
-    return _grouped(_lib.lib().ace_grouped_matmul_grad_w, dy, x, offsets, S, N, M, K, (N, M, K), ("dy", "x"),
+    return _grouped(_lib.GROUPED_GRAD_W, dy, x, offsets, S, N, M, K, (N, M, K), ("dy", "x"),
                     ((S, M), (S, K)), out)
 
 

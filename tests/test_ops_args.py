@@ -15,11 +15,12 @@ BIG = (1 << 31) - 1
 BAD, UNS, WSP = _lib.ACE_ERR_INVALID_ARG, _lib.ACE_ERR_UNSUPPORTED, _lib.ACE_ERR_WORKSPACE
 
 
-def _grouped(fn="ace_grouped_matmul", rows=P[0], other=P[1], offsets=P[2], out=P[3], null=False, **kw):
+def _grouped(fn="ace_grouped_matmul", rows=P[0], other=P[1], offsets=P[2], out=P[3], null=False, ws=P[15], ws_bytes=1 << 40,
+             **kw):
     d = dict(S=64, N=4, M=64, K=64, dtype=_lib.ACE_BF16, flags=0)
     d.update(kw)
     desc = None if null else ctypes.byref(_lib.GroupedDesc(*[d[n] for n in ("S", "N", "M", "K", "dtype", "flags")]))
-    return getattr(ace.lib(), fn)(desc, rows, other, offsets, out, None)
+    return getattr(ace.lib(), fn)(desc, rows, other, offsets, out, ws, ws_bytes, None)
 
 
 FNS = ("ace_grouped_matmul", "ace_grouped_matmul_grad_x", "ace_grouped_matmul_grad_w")
@@ -31,14 +32,24 @@ def test_grouped_refusals(fn):
                dict(other=0), dict(offsets=0), dict(out=0), dict(rows=P[0] + 8), dict(out=P[3] + 4), dict(offsets=P[2] + 2),
                dict(out=P[0]), dict(out=P[1] + 64), dict(out=P[2])):
         assert _grouped(fn, **kw) == BAD, kw
-    for kw in (dict(N=4097), dict(M=65544), dict(K=65544), dict(M=12), dict(K=4), dict(dtype=_lib.ACE_F32, K=6)):
+    for kw in (dict(S=BIG), dict(N=4097), dict(M=65544), dict(K=65544), dict(M=12), dict(K=4), dict(dtype=_lib.ACE_F32, K=6)):
         assert _grouped(fn, **kw) == UNS, kw
 
 
-def test_grouped_grids_past_the_limit():
-    # 2^25 64-row fp32 tiles x 1024 column tiles; 4096 x 1024 x 1024 tiles of weights
-    assert _grouped(S=BIG, N=1, M=65536, K=4, dtype=_lib.ACE_F32, other=P[1], out=P[9]) == UNS
-    assert _grouped(FNS[2], S=1, N=4096, M=65536, K=65536, dtype=_lib.ACE_F32, out=P[4]) == UNS
+def test_grouped_workspace():
+    """Few tiles with a long reduction take partial sums; enough tiles none."""
+    size = ace.lib().ace_grouped_workspace_size
+    for way, fn in enumerate(FNS):
+        few = dict(S=64, N=2, M=4096, K=128) if way == 1 else dict(S=64, N=2, M=128, K=4096) if way == 0 else dict(
+            S=40000, N=2, M=128, K=128)
+        n = size(_lib.GroupedDesc(*few.values(), _lib.ACE_BF16, 0), way)
+        assert n > 0 and n % 4 == 0
+        for kw in (dict(ws=0), dict(ws=P[15] + 16), dict(ws_bytes=n - 1)):
+            assert _grouped(fn, **few, **kw) == WSP, kw
+        many = _lib.GroupedDesc(32768, 128, 768, 2048, _lib.ACE_BF16, 0)
+        assert size(many, way) == 0
+        assert size(_lib.GroupedDesc(64, 0, 64, 64, _lib.ACE_BF16, 0), way) == 0
+    assert size(many, 3) == 0 and size(many, -1) == 0
 
 
 def test_grouped_empty_rows():
@@ -112,7 +123,7 @@ def test_adapter_refusals():
                dict(x=P[1] + 8), dict(scale=P[4] + 2), dict(out=P[0] + 16), dict(out=P[1]), dict(out=P[2]), dict(out=P[3]),
                dict(out=P[4] - 16), dict(out=P[6])):
         assert _adapter(**kw) == BAD, kw
-    for kw in (dict(R=4097), dict(rank=136), dict(rank=12), dict(d_in=65544), dict(d_out=65544), dict(d_in=60),
+    for kw in (dict(S=BIG), dict(R=4097), dict(rank=136), dict(rank=12), dict(d_in=65544), dict(d_out=65544), dict(d_in=60),
                dict(d_out=4)):
         assert _adapter(**kw) == UNS, kw
     for kw in (dict(ws=None), dict(ws=P[15] + 16), dict(need=-1)):
