@@ -247,7 +247,7 @@ struct NormArgs {
 };
 hipError_t launch_block_norm(const NormArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_block_norm_grad(const NormArgs &a, bool bf16, hipStream_t stream);
-int block_norm_grad_blocks(int T);  // workgroups of the gradient: rows of its partial sums
+int block_norm_grad_blocks(int T, int d, bool bf16);  // workgroups of the gradient: rows of its partial sums
 
 // Low-rank adapters of many requests (adapter.hip)
 struct AdapterArgs {

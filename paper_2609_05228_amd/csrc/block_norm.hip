@@ -14,7 +14,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "ace_internal.h"
+#include "lds_dma.h"
 
 namespace ace {
 
@@ -22,8 +22,7 @@ namespace {
 
 template <typename T> constexpr int kVec = 16 / static_cast<int>(sizeof(T));  // elements of a 16-byte access
 
-template <typename T> __device__ __forceinline__ void load_vec(const T *p, float *f) {
-  const uint4 v = *reinterpret_cast<const uint4 *>(p);
+template <typename T> __device__ __forceinline__ void unpack(const uint4 &v, float *f) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -36,6 +35,10 @@ template <typename T> __device__ __forceinline__ void load_vec(const T *p, float
   }
 }
 
+template <typename T> __device__ __forceinline__ void load_vec(const T *p, float *f) {
+  unpack<T>(*reinterpret_cast<const uint4 *>(p), f);
+}
+
 template <typename T> __device__ __forceinline__ void store_vec(T *p, const float *f) {
   uint4 v;
   if constexpr (sizeof(T) == 2)
@@ -45,6 +48,26 @@ template <typename T> __device__ __forceinline__ void store_vec(T *p, const floa
   *reinterpret_cast<uint4 *>(p) = v;
 }
 
+// Sum over a wave in a fixed order, the same in every lane: within rows of 16 lanes by DPP, then across
+// the rows (a lane exchange through LDS takes several times as long)
+template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, true));
+}
+// over N = 1, 2, 4, 8 or 16 neighbouring lanes, in each of them
+template <int N> __device__ __forceinline__ float lanes_sum(float v) {
+  if constexpr (N > 1) v = dpp_add<0xb1, 0xf>(v);   // lanes 1 apart
+  if constexpr (N > 2) v = dpp_add<0x4e, 0xf>(v);   // 2 apart
+  if constexpr (N > 4) v = dpp_add<0x141, 0xf>(v);  // mirrored in 8
+  if constexpr (N > 8) v = dpp_add<0x140, 0xf>(v);  // mirrored in 16
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = lanes_sum<16>(v);
+  v = dpp_add<0x142, 0xa>(v);  // rows 1 and 3 add the row before
+  v = dpp_add<0x143, 0xc>(v);  // rows 2 and 3 add row 1's: lane 63 holds all
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
 // Sums over the workgroup, the same in every thread, in a fixed order.  Successive calls
 // alternate between two LDS slots, so one barrier per call is enough.
 template <int NT, int N> struct BlockSum {
@@ -52,9 +75,7 @@ template <int NT, int N> struct BlockSum {
   int par = 0;
   __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o);
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
     if constexpr (NT > 64) {
       const int wave = threadIdx.x >> 6;
       if ((threadIdx.x & 63) == 0)
@@ -62,12 +83,7 @@ template <int NT, int N> struct BlockSum {
         for (int i = 0; i < N; ++i) red[par][i][wave] = v[i];
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < NT / 64; ++w) s += red[par][i][w];
-        v[i] = s;
-      }
+      for (int i = 0; i < N; ++i) v[i] = lanes_sum<NT / 64>(red[par][i][threadIdx.x % (NT / 64)]);
       par ^= 1;
     }
   }
@@ -140,123 +156,221 @@ template <typename T, int NT, int CH> __global__ __launch_bounds__(NT) void bloc
   }
 }
 
-// The parameter gradients are sums over rows: each workgroup takes the rows blockIdx.x,
-// blockIdx.x + gridDim.x, .. and keeps its threads' columns of the sums in registers, then
-// writes them to part [w_pre, w_post, gate [d]][gridDim.x][d], which param_sum_kernel adds in
-// a fixed order (no atomics: equal calls give equal bits).
-template <typename T, int NT, int CH> __global__ __launch_bounds__(NT) void block_norm_grad_kernel(NormArgs a) {
+// Sums over the NT threads of each of a workgroup's RG rows, the same in each of them, in a fixed
+// order; as BlockSum, with one barrier of the workgroup, none where a row is one wave's.
+template <int NT, int RG, int N> struct RowSum {
+  float (*red)[RG][N][NT / 64];
+  int par = 0;
+  __device__ __forceinline__ void operator()(float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (NT > 64) {
+      const int grp = threadIdx.x / NT, wave = (threadIdx.x % NT) >> 6;
+      if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) red[par][grp][i][wave] = v[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = lanes_sum<NT / 64>(red[par][grp][i][threadIdx.x % (NT / 64)]);
+      par ^= 1;
+    }
+  }
+};
+
+// A workgroup takes RG rows at a time (NT threads each).  While it works on them, held in registers as
+// stored and widened where used, the next ones are copied into LDS (each thread its own 16 bytes of
+// each operand, so a wave waits for its own copies only); weights and a gate per channel lie in LDS too, so
+// that no other load has to be waited for.
+// The parameter gradients are sums over rows: a thread keeps its columns' sums of its rows in registers,
+// the RG rows' are added through LDS at the end, and each workgroup writes one line of part
+// [w_pre, w_post, gate [d]][gridDim.x][d], which param_sum_kernel adds in a fixed order (no atomics:
+// equal calls give equal bits).  RG rows at a time keep these lines few.
+// Bound by HBM and the fp32 pipes alike: some 30 operations an element, 12 of the 19 us that the memory
+// takes for 4096 rows of 2048 (bf16).
+template <typename T, int NT, int CH, int RG>
+__global__ __launch_bounds__(NT *RG) void block_norm_grad_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
-  __shared__ float red3[2][3][NT / 64], red2[2][2][NT / 64];
-  BlockSum<NT, 3> sum3{red3};
-  BlockSum<NT, 2> sum2{red2};
+  constexpr bool AHEAD = CH == 1;  // longer rows would not fit LDS
+  __shared__ float red3[2][RG][3][NT / 64], red2[2][RG][2][NT / 64];
+  __shared__ f32x4_t join[RG > 1 ? RG - 1 : 1][RG > 1 ? NT * V / 4 : 1];
+  __shared__ uint4 params[3][AHEAD ? NT : 1];                    // w_pre, w_post, gate [d]
+  __shared__ uint4 ahead[AHEAD ? NT * RG / 64 : 1][4][64];       // a wave's h, dn, y, dh
+  RowSum<NT, RG, 3> sum3{red3};
+  RowSum<NT, RG, 2> sum2{red2};
   const float inv_d = 1.f / static_cast<float>(a.d);
+  const int tid = threadIdx.x % NT, grp = threadIdx.x / NT;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   float pre[CH][V], post[CH][V], gc[CH][V];
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
     for (int i = 0; i < V; ++i) pre[c][i] = post[c][i] = gc[c][i] = 0.f;
   const bool need_y = a.y && (a.w_post || a.gate_kind);
-  for (int row = blockIdx.x; row < a.T; row += gridDim.x) {
+  const void *src[4] = {a.dn ? a.h : nullptr, a.dn, need_y ? a.y : nullptr, a.dh};
+  const uint4 zero{0, 0, 0, 0};
+  const uint32_t one = sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u;
+  // chunk c of a parameter: ones where there is none
+  auto fetch_param = [&](int k, int c) {
+    const int col = (c * NT + tid) * V;
+    const void *p = k == 0 ? a.w_pre : k == 1 ? a.w_post : a.gate_kind == 1 ? a.gate : nullptr;
+    return p && col < a.d ? *reinterpret_cast<const uint4 *>(static_cast<const T *>(p) + col) : uint4{one, one, one, one};
+  };
+  auto param = [&](int k, int c, float *f) {
+    if constexpr (AHEAD)
+      unpack<T>(params[k][tid], f);
+    else
+      unpack<T>(fetch_param(k, c), f);
+  };
+  const bool wide = tid * V < a.d;
+  const uint32_t slot = lds_addr(ahead[AHEAD ? wave : 0]);
+  auto copy = [&](int row) {
+    if (row < a.T && wide)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (src[k]) dma16(static_cast<const T *>(src[k]) + static_cast<size_t>(row) * a.d + tid * V, slot + k * 1024);
+  };
+  const int step = static_cast<int>(gridDim.x) * RG;
+  if constexpr (AHEAD) {
+    copy(blockIdx.x * RG + grp);
+    if (grp == 0)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) params[k][tid] = fetch_param(k, 0);
+    __syncthreads();
+  }
+  // stores of a wave after the copies that it waits for: at least these (a wave's memory operations finish
+  // in order)
+  const int behind = 1 + (a.y != nullptr) + (a.gate_kind == 3);
+  bool first = true;
+  for (int row0 = blockIdx.x * RG; row0 < a.T; row0 += step) {
+    const int row = row0 + grp;
+    const bool there = row < a.T;
     const size_t ro = static_cast<size_t>(row) * a.d;
-    float h[CH][V], y[CH][V], p[CH][V], t[CH][V];
+    uint4 cur[4][CH];  // h, dn, y, dh
+    if constexpr (AHEAD) {
+      if (first || !there)
+        wait_vmcnt_in<0, 0>(0);
+      else
+        wait_vmcnt_in<1, 3>(behind);
+      first = false;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) cur[k][0] = there && wide && src[k] ? ahead[wave][k][lane] : zero;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next copies overwrite it
+#pragma unroll
+      for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(cur[k][0].x), "+v"(cur[k][0].y), "+v"(cur[k][0].z), "+v"(cur[k][0].w));
+      if (step < a.T - row0) copy(row + step);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const int col = (c * NT + tid) * V;
+          cur[k][c] = there && col < a.d && src[k] ? *reinterpret_cast<const uint4 *>(static_cast<const T *>(src[k]) + ro + col) : zero;
+        }
+    }
     float s3[3] = {0.f, 0.f, 0.f};  // sum h'^2, sum p h', sum y^2
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int col = (c * NT + threadIdx.x) * V;
-#pragma unroll
-      for (int i = 0; i < V; ++i) h[c][i] = y[c][i] = p[c][i] = t[c][i] = 0.f;
-      if (col < a.d) {
-        if (a.dn) {
-          load_vec(static_cast<const T *>(a.h) + ro + col, h[c]);
-          load_vec(static_cast<const T *>(a.dn) + ro + col, p[c]);
-        }
-        if (need_y) load_vec(static_cast<const T *>(a.y) + ro + col, y[c]);
-        if (a.dh) load_vec(static_cast<const T *>(a.dh) + ro + col, t[c]);
-      }
-      if (a.dn && col < a.d) {
-        float w[V];
-        load_vec(static_cast<const T *>(a.w_pre) + col, w);
-#pragma unroll
-        for (int i = 0; i < V; ++i) s3[1] += p[c][i] * w[i] * h[c][i];
-      }
+      float h[V], p[V], y[V], w[V];
+      unpack<T>(cur[0][c], h);
+      unpack<T>(cur[1][c], p);
+      unpack<T>(cur[2][c], y);
+      param(0, c, w);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        s3[0] += h[c][i] * h[c][i];
-        s3[2] += y[c][i] * y[c][i];
+        s3[0] += h[i] * h[i];
+        s3[1] += p[i] * w[i] * h[i];
+        s3[2] += y[i] * y[i];
       }
     }
     sum3(s3);
     const float r = 1.f / sqrtf(s3[0] * inv_d + a.eps);
-    const float m = s3[1] * inv_d * r * r;
+    const float mr = s3[1] * inv_d * r * r * r;
     const float s = a.w_post ? 1.f / sqrtf(s3[2] * inv_d + a.eps) : 1.f;
-    const float gt = gate_of_row<T>(a, row);
-    float s2[2] = {0.f, 0.f};  // sum q y, sum db u
+    const float gt = there ? a.branch_scale * gate_of_row<T>(a, row) : 0.f;
+    float q[CH][V];
+    float s2[2] = {0.f, 0.f};  // sum q y, sum t u
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int col = (c * NT + threadIdx.x) * V;
-      if (col >= a.d) continue;
-      if (a.dn) {
-        float w[V];
-        load_vec(static_cast<const T *>(a.w_pre) + col, w);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          pre[c][i] += p[c][i] * (h[c][i] * r);
-          t[c][i] += r * (p[c][i] * w[i] - h[c][i] * m);
-        }
-      }
-      float o[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) o[i] = a.res_scale * t[c][i];
-      store_vec(static_cast<T *>(a.g_h) + ro + col, o);
-      if (!a.y) continue;
-      float w[V], g[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) w[i] = g[i] = 1.f;
-      if (a.w_post) load_vec(static_cast<const T *>(a.w_post) + col, w);
-      if (a.gate_kind == 1) load_vec(static_cast<const T *>(a.gate) + col, g);
-      if (a.gate_kind == 3) load_vec(static_cast<const T *>(a.gate) + ro + col, g);
+      const int col = (c * NT + tid) * V;
+      const bool in = there && col < a.d;
+      float h[V], p[V], y[V], t[V], w[V], o[V];
+      unpack<T>(cur[0][c], h);
+      unpack<T>(cur[1][c], p);
+      unpack<T>(cur[2][c], y);
+      unpack<T>(cur[3][c], t);
+      param(0, c, w);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float db = a.branch_scale * t[c][i], yn = y[c][i] * s, du = db * (g[i] * gt);
-        o[i] = db * (yn * w[i]);
+        const float pr = p[i] * r;
+        pre[c][i] += pr * h[i];
+        t[i] += pr * w[i] - h[i] * mr;
+        o[i] = a.res_scale * t[i];
+      }
+      if (in) store_vec(static_cast<T *>(a.g_h) + ro + col, o);
+      if (!a.y) continue;
+      float g[V];
+      param(1, c, w);
+      param(2, c, g);
+      if (a.gate_kind == 3 && in) load_vec(static_cast<const T *>(a.gate) + ro + col, g);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float tyn = t[i] * (y[i] * s), gg = g[i] * gt;
+        o[i] = tyn * w[i];
         gc[c][i] += o[i];
         s2[1] += o[i];
-        post[c][i] += du * yn;
-        t[c][i] = du * w[i];
-        s2[0] += t[c][i] * y[c][i];
+        post[c][i] += tyn * gg;
+        q[c][i] = t[i] * gg * w[i];
+        s2[0] += q[c][i] * y[i];
       }
-      if (a.gate_kind == 3) store_vec(static_cast<T *>(a.g_gate) + ro + col, o);
+      if (a.gate_kind == 3 && in) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] *= a.branch_scale;
+        store_vec(static_cast<T *>(a.g_gate) + ro + col, o);
+      }
     }
     if (!a.y) continue;
     if (a.w_post || a.gate_kind == 2) sum2(s2);
-    if (a.gate_kind == 2 && threadIdx.x == 0) static_cast<T *>(a.g_gate)[row] = Elem<T>::from_f32(s2[1]);
-    const float k = a.w_post ? s2[0] * inv_d * s * s : 0.f;
+    if (a.gate_kind == 2 && tid == 0 && there)
+      static_cast<T *>(a.g_gate)[row] = Elem<T>::from_f32(a.branch_scale * s2[1]);
+    const float k = a.w_post ? s2[0] * inv_d * s * s * s : 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int col = (c * NT + threadIdx.x) * V;
-      if (col >= a.d) continue;
-      float o[V];
+      const int col = (c * NT + tid) * V;
+      float y[V], o[V];
+      unpack<T>(cur[2][c], y);
 #pragma unroll
-      for (int i = 0; i < V; ++i) o[i] = s * (t[c][i] - y[c][i] * k);
-      store_vec(static_cast<T *>(a.g_y) + ro + col, o);
+      for (int i = 0; i < V; ++i) o[i] = s * q[c][i] - y[i] * k;
+      if (there && col < a.d) store_vec(static_cast<T *>(a.g_y) + ro + col, o);
     }
   }
   float *part = a.part;
-  auto put = [&](const float (&acc)[CH][V]) {
+  auto put = [&](float (&acc)[CH][V], float scale) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int col = (c * NT + threadIdx.x) * V;
-      if (col >= a.d) continue;
+      if constexpr (RG > 1) {
+        __syncthreads();
+        if (grp > 0)
+#pragma unroll
+          for (int i = 0; i < V; i += 4)
+            join[grp - 1][tid * (V / 4) + i / 4] = f32x4_t{acc[c][i], acc[c][i + 1], acc[c][i + 2], acc[c][i + 3]};
+        __syncthreads();
+      }
+      const int col = (c * NT + tid) * V;
+      if (grp > 0 || col >= a.d) continue;
       float *o = part + static_cast<size_t>(blockIdx.x) * a.d + col;
 #pragma unroll
-      for (int i = 0; i < V; i += 4)
-        *reinterpret_cast<f32x4_t *>(o + i) = f32x4_t{acc[c][i], acc[c][i + 1], acc[c][i + 2], acc[c][i + 3]};
+      for (int i = 0; i < V; i += 4) {
+        f32x4_t v = {acc[c][i], acc[c][i + 1], acc[c][i + 2], acc[c][i + 3]};
+        if constexpr (RG > 1)
+          for (int k = 0; k < RG - 1; ++k) v += join[k][tid * (V / 4) + i / 4];
+        *reinterpret_cast<f32x4_t *>(o + i) = v * scale;
+      }
     }
     part += static_cast<size_t>(gridDim.x) * a.d;
   };
-  if (a.g_pre) put(pre);
-  if (a.g_post) put(post);
-  if (a.gate_kind == 1) put(gc);
+  if (a.g_pre) put(pre, 1.f);
+  if (a.g_post) put(post, 1.f);
+  if (a.gate_kind == 1) put(gc, a.branch_scale);
 }
 
 // Sums of `blocks` partial rows: 64 columns per workgroup, 16 waves take every 16th row
@@ -286,6 +400,15 @@ template <typename T> __global__ __launch_bounds__(1024) void param_sum_kernel(N
 }
 
 constexpr int kNormBlocks = 2048;
+constexpr int kGradBlocks = 256;  // a workgroup a CU
+
+// Threads of a gradient workgroup: 1024, or 512 where those would not fill the CUs once (bf16: 117 rows of 384
+// 10.8 us with 1024 and 8.4 with 512, 1574 rows of 200 11.6 and 9.8; 4096 rows of 2048 29 and 32, 10819 of 1296 63 and 77)
+int grad_threads(int T, int nt) {
+  const int small = std::max(nt, 512);
+  return static_cast<long long>(T) <= static_cast<long long>(kGradBlocks) * (1024 / nt) ? small : 1024;
+}
+
 
 // the smallest workgroup whose threads hold a row of d in one access each, else 1024
 // threads with two or four
@@ -314,14 +437,26 @@ template <typename T> void launch_fwd(const NormArgs &a, hipStream_t s) {
 }
 
 template <typename T> void launch_grad(const NormArgs &a, hipStream_t s) {
-  by_width<T>(a.d, [&](auto nt, auto ch) { block_norm_grad_kernel<T, nt(), ch()><<<a.blocks, nt(), 0, s>>>(a); });
+  by_width<T>(a.d, [&](auto nt, auto ch) {
+    constexpr int NT = nt(), SMALL = std::max(NT, 512);
+    if (grad_threads(a.T, NT) == SMALL)
+      block_norm_grad_kernel<T, NT, ch(), SMALL / NT><<<a.blocks, SMALL, 0, s>>>(a);
+    else
+      block_norm_grad_kernel<T, NT, ch(), 1024 / NT><<<a.blocks, 1024, 0, s>>>(a);
+  });
   const int n = (a.g_pre != nullptr) + (a.g_post != nullptr) + (a.gate_kind == 1);
   if (n > 0) param_sum_kernel<T><<<dim3((a.d + 63) / 64, n), 1024, 0, s>>>(a);
 }
 
 }  // namespace
 
-int block_norm_grad_blocks(int T) { return T < 1 ? 1 : T < 512 ? T : 512; }
+int block_norm_grad_blocks(int T, int d, bool bf16) {
+  const int v = bf16 ? 8 : 4;
+  int nt = 64;
+  while (nt < 1024 && d > nt * v) nt *= 2;
+  const int threads = grad_threads(T, nt), rows = threads / nt;  // of a workgroup at a time
+  return std::min((std::max(T, 1) - 1) / rows + 1, threads < 1024 ? 2 * kGradBlocks : kGradBlocks);
+}
 
 hipError_t launch_block_norm(const NormArgs &a, bool bf16, hipStream_t stream) {
   if (a.T <= 0) return hipSuccess;

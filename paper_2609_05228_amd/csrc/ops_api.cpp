@@ -191,7 +191,7 @@ ace_status ace_block_norm(const ace_norm_desc *desc, const ace_norm_inputs *in, 
 
 size_t ace_block_norm_grad_workspace_size(const ace_norm_desc *desc) {
   if (!desc || desc->T < 0 || desc->d <= 0) return 0;
-  return static_cast<size_t>(ace::block_norm_grad_blocks(desc->T)) * desc->d * 3 * sizeof(float);
+  return static_cast<size_t>(ace::block_norm_grad_blocks(desc->T, desc->d, desc->dtype == ACE_BF16)) * desc->d * 3 * sizeof(float);
 }
 
 ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs *in, const void *dh, const void *dn,
@@ -234,7 +234,7 @@ ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs 
   a.g_pre = out->w_pre;
   a.g_gate = out->gate;
   a.part = static_cast<float *>(workspace);
-  a.blocks = ace::block_norm_grad_blocks(d.T);
+  a.blocks = ace::block_norm_grad_blocks(d.T, d.d, d.dtype == ACE_BF16);
   return status_of(ace::launch_block_norm_grad(a, d.dtype == ACE_BF16, static_cast<hipStream_t>(stream)));
 }
 
