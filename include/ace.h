@@ -355,7 +355,8 @@ ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs 
  * request, get out[r] = base[r].  out may be base itself (those rows then stay untouched).
  *   base [S, d_out], x [S, d_in], a [L, rank, d_in], b [L, d_out, rank], out [S, d_out], dtype;
  *   scale [L] fp32 or NULL (ones); offsets [R + 1] and adapter [R] int32 (adapter may be NULL when R = 0).
- *   workspace  DEVICE scratch of ace_adapter_workspace_size(desc) bytes, 256-byte aligned.
+ *   workspace  DEVICE scratch of ace_adapter_workspace_size(desc) bytes, 256-byte aligned (may be NULL when
+ *              that is 0: small batches).
  * An adapter of lower rank is padded with zero rows of a.  Limits (else ACE_ERR_UNSUPPORTED): S < 2^31 - 1024, R <= 4096,
  * rank <= 128, d_in and d_out <= 65536.
  */

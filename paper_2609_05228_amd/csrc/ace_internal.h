@@ -257,7 +257,9 @@ struct AdapterArgs {
   void *out;                     // [S, dout], may be base
   float *v;                      // [splits, S, r]
   int S, R, L, r, din, dout, splits;
+  int chunks;                    // shares of the columns (small batches)
 };
+// parts of the inner product's partial sums; 0: none are kept
 int adapter_splits(int S, int R, int din, bool bf16);
 // hipErrorInvalidValue, with nothing enqueued, for grids past 2^31 workgroups
 hipError_t launch_adapter(const AdapterArgs &a, bool bf16, hipStream_t stream);

@@ -2,12 +2,16 @@
 // that carries adapter a gets
 //   out[r] = base[r] + scale_a B_a v,   v = A_a x[r]
 // and every other row gets base[r].  A_a [rank, din], B_a [dout, rank].
-// Two launches: v has to be whole before any of it is used.  The first multiplies 16 rows of
-// one request by A_a, din split over the waves of a workgroup and, where there are few rows,
-// over workgroups (partial sums [splits][S][rank], fp32); the second adds the splits in order and
-// multiplies by B_a.  Operands go from memory straight into the matrix cores' registers: each is
-// used by one wave.  v stays exact to 16 bits in bf16 calls: it is multiplied as the sum of two
-// bf16 numbers (a single rounding of v to 8 bits would cost as much as that of the output).
+//
+// v has to be whole before any of it is used.  Many rows: two launches, the first multiplies tiles of 64
+// rows of one request by A_a, din split over the waves of a workgroup and over workgroups (partial
+// sums [splits][S][rank], fp32), the second adds the splits in order and multiplies by B_a.  Few rows, where a
+// launch costs as much as the work (decoding): one launch, each workgroup computes v of 16 rows
+// for itself and multiplies it by its share of B_a's rows.
+// Operands go from memory straight into the matrix cores' registers: a wave reads each fragment
+// of A_a and B_a once and uses it for every row of its tile, so staging them would save nothing.
+// v stays exact to 16 bits in bf16 calls: it is multiplied as the sum of two bf16 numbers (a
+// single rounding of v to 8 bits would cost as much as that of the output).
 #include <algorithm>
 
 #include "lds_dma.h"
@@ -17,11 +21,18 @@ namespace ace {
 
 namespace {
 
-constexpr int kAdRows = 16;
+constexpr int kRowBlock = 16;
+constexpr int kTileRows = 64;    // of the two launches
+constexpr int kExpandWaves = 8;  // 64 columns each
+constexpr int kCUs = 256;
 
-template <typename T> __device__ __forceinline__ typename Frag<T>::type zero_frag() {
-  return __builtin_bit_cast(typename Frag<T>::type, uint4{0, 0, 0, 0});
+template <typename T> using frag_of = typename Frag<T>::type;
+template <typename T> __device__ __forceinline__ frag_of<T> zero_frag() {
+  return __builtin_bit_cast(frag_of<T>, uint4{0, 0, 0, 0});
 }
+template <typename T> constexpr int kStepK = 64 / static_cast<int>(sizeof(T));  // k of a pair of fragments
+// pairs of fragments that hold a rank of 16 RB
+template <typename T, int RB> constexpr int kRankSteps = (16 * RB + kStepK<T> - 1) / kStepK<T>;
 
 // adapter of a tile, or -1
 __device__ __forceinline__ int tile_adapter(const AdapterArgs &p, const RaggedTile &t) {
@@ -30,167 +41,334 @@ __device__ __forceinline__ int tile_adapter(const AdapterArgs &p, const RaggedTi
   return a >= 0 && a < p.L ? a : -1;
 }
 
-// RB: 16-wide blocks of the rank
-template <typename T, int RB> __global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterArgs p) {
-  constexpr int KS = 64 / sizeof(T);  // k of one fragment pair
+// acc[i][c] += rows 16 i .. of x times rows 16 c .. of A over k = first, first + step, .. (a fragment
+// pair each): lane holds rank 16 c + 4 g + q of row 16 i + lane % 16.  Rows past the tile repeat its last.
+template <typename T, int RT, int RB>
+__device__ __forceinline__ void shrink(const AdapterArgs &p, const RaggedTile &t, int ad, int first, int step,
+                                       f32x4_t (&acc)[RT][RB]) {
   constexpr int E = kChunkElems<T>;
-  typedef typename Frag<T>::type frag_t;
+  const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+  const T *x[RT], *w[RB];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+    x[i] = static_cast<const T *>(p.x) + static_cast<size_t>(t.row0 + min(16 * i + r16, t.rows - 1)) * p.din;
+#pragma unroll
+  for (int c = 0; c < RB; ++c)
+    w[c] = static_cast<const T *>(p.a) + (static_cast<size_t>(ad) * p.r + min(16 * c + r16, p.r - 1)) * p.din;
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int c = 0; c < RB; ++c) acc[i][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll(RT == 1 ? 4 : 2)
+  for (int k0 = first; k0 < p.din; k0 += step) {
+    const int k = k0 + E * g;
+    const bool in = k < p.din;
+    frag_of<T> xf[RT], wf[RB];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) xf[i] = in ? *reinterpret_cast<const frag_of<T> *>(x[i] + k) : zero_frag<T>();
+#pragma unroll
+    for (int c = 0; c < RB; ++c) wf[c] = in ? *reinterpret_cast<const frag_of<T> *>(w[c] + k) : zero_frag<T>();
+#pragma unroll
+    for (int s = 0; s < Frag<T>::steps; ++s)
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int c = 0; c < RB; ++c) acc[i][c] = Frag<T>::mma(wf[c], xf[i], s, acc[i][c]);
+  }
+}
+
+// A lane's E values of v as fragments: bf16 the value rounded and the rest of it, fp32 itself
+template <typename T> struct VFrag {
+  frag_of<T> hi, lo;
+  __device__ __forceinline__ void set(const float *f) {
+    if constexpr (sizeof(T) == 2) {
+      uint32_t h[4], l[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+        l[i] = pack_bf16x2(f[2 * i] - __uint_as_float(h[i] << 16), f[2 * i + 1] - __uint_as_float(h[i] & 0xffff0000u));
+      }
+      hi = __builtin_bit_cast(frag_of<T>, uint4{h[0], h[1], h[2], h[3]});
+      lo = __builtin_bit_cast(frag_of<T>, uint4{l[0], l[1], l[2], l[3]});
+    } else {
+      hi = __builtin_bit_cast(
+          frag_of<T>, uint4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
+    }
+  }
+};
+
+// 64 columns of B_a from c0, as fragments.  bf16: the columns of two 16-column blocks interleaved in fours,
+// so that a lane's results are 8 consecutive columns (see grouped.hip)
+template <typename T, int KB> struct Columns {
+  static constexpr bool PAIR = sizeof(T) == 2;
+  static constexpr int E = kChunkElems<T>;
+  frag_of<T> w[KB][4];
+  int c0;
+  __device__ __forceinline__ void load(const AdapterArgs &p, int ad, int c0_) {
+    c0 = c0_;
+    const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+    const T *b = static_cast<const T *>(p.b) + static_cast<size_t>(ad) * p.dout * p.r;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int col = min(c0 + (PAIR ? 32 * (c >> 1) + 8 * (r16 >> 2) + 4 * (c & 1) + (r16 & 3) : 16 * c + r16), p.dout - 1);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const int k = kb * kStepK<T> + E * g;
+        w[kb][c] = k < p.r ? *reinterpret_cast<const frag_of<T> *>(b + static_cast<size_t>(col) * p.r + k) : zero_frag<T>();
+      }
+    }
+  }
+  static constexpr int STEP = PAIR ? 2 : 1;
+  static constexpr int PIECES = 4 / STEP;  // of 16 bytes of a row in a lane
+  __device__ __forceinline__ int col(int i) const { return c0 + 16 * STEP * i + E * static_cast<int>((threadIdx.x & 63) >> 4); }
+
+  // base's 16 columns-pieces of a row
+  __device__ __forceinline__ void base_of(const AdapterArgs &p, size_t row, bool there, uint4 (&v)[PIECES]) const {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+      v[i] = there && col(i) < p.dout ? *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.base) + row * p.dout + col(i))
+                                      : uint4{0, 0, 0, 0};
+  }
+  // out = base + B v for the row of this lane
+  __device__ __forceinline__ void finish(const AdapterArgs &p, const VFrag<T> (&v)[KB], size_t row, bool there,
+                                         uint4 (&bv)[PIECES]) const {
+    f32x4_t acc[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int s = 0; s < Frag<T>::steps; ++s) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] = Frag<T>::mma(w[kb][c], v[kb].hi, s, acc[c]);
+        if constexpr (PAIR)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c] = Frag<T>::mma(w[kb][c], v[kb].lo, s, acc[c]);
+      }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      if constexpr (PAIR) {
+        uint32_t b[4] = {bv[i].x, bv[i].y, bv[i].z, bv[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4_t &d = acc[2 * i + (j >> 1)];
+          b[j] = pack_bf16x2(__uint_as_float(b[j] << 16) + d[2 * (j & 1)],
+                             __uint_as_float(b[j] & 0xffff0000u) + d[2 * (j & 1) + 1]);
+        }
+        bv[i] = uint4{b[0], b[1], b[2], b[3]};
+      } else {
+        bv[i] = __builtin_bit_cast(uint4, __builtin_bit_cast(f32x4_t, bv[i]) + acc[i]);
+      }
+    }
+    put(p, row, there, bv);
+  }
+  __device__ __forceinline__ void put(const AdapterArgs &p, size_t row, bool there, const uint4 (&v)[PIECES]) const {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+      if (there && col(i) < p.dout) *reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + row * p.dout + col(i)) = v[i];
+  }
+};
+
+// ---------------------------------------------------------------- many rows
+template <typename T, int RB> __global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterArgs p) {
+  constexpr int RT = kTileRows / kRowBlock;
   const int b = ragged_block();
-  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kAdRows, false).find_uniform(b / p.splits);
+  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kTileRows, false).find_uniform(b / p.splits);
   if (!t.valid) return;
   const int ad = tile_adapter(p, t);
   if (ad < 0) return;
   const int split = b % p.splits;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
-  const T *x = static_cast<const T *>(p.x) + static_cast<size_t>(t.row0 + min(r16, t.rows - 1)) * p.din;
-  const T *w = static_cast<const T *>(p.a) + static_cast<size_t>(ad) * p.r * p.din;
-  f32x4_t acc[RB];
+  f32x4_t acc[RT][RB];
+  shrink<T, RT, RB>(p, t, ad, (split * 4 + wave) * kStepK<T>, 4 * p.splits * kStepK<T>, acc);
+  // the waves' sums, one row block after the other: wave i adds block i's in wave order
+  __shared__ f32x4_t red[4][RT][RB][64];
 #pragma unroll
-  for (int c = 0; c < RB; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int step = 4 * p.splits * KS;
-#pragma unroll 4
-  for (int k = (split * 4 + wave) * KS + E * g; k - E * g < p.din; k += step) {
-    const bool in = k < p.din;
-    const frag_t xf = in ? *reinterpret_cast<const frag_t *>(x + k) : zero_frag<T>();
+  for (int i = 0; i < RT; ++i)
 #pragma unroll
-    for (int c = 0; c < RB; ++c) {
-      const int row = min(16 * c + r16, p.r - 1);
-      const frag_t wf = in ? *reinterpret_cast<const frag_t *>(w + static_cast<size_t>(row) * p.din + k) : zero_frag<T>();
-#pragma unroll
-      for (int s = 0; s < Frag<T>::steps; ++s) acc[c] = Frag<T>::mma(wf, xf, s, acc[c]);
-    }
-  }
-  __shared__ f32x4_t red[4][RB][64];
-#pragma unroll
-  for (int c = 0; c < RB; ++c) red[wave][c][lane] = acc[c];
+    for (int c = 0; c < RB; ++c) red[wave][i][c][lane] = acc[i][c];
   __syncthreads();
-  if (r16 >= t.rows) return;
-  float *v = p.v + (static_cast<size_t>(split) * p.S + t.row0 + r16) * p.r;
-  for (int c = wave; c < RB; c += 4) {
+  const int row = 16 * wave + r16;
+  if (row >= t.rows) return;
+  float *v = p.v + (static_cast<size_t>(split) * p.S + t.row0 + row) * p.r;
+#pragma unroll
+  for (int c = 0; c < RB; ++c) {
     const int col = 16 * c + 4 * g;
-    if (col < p.r) *reinterpret_cast<f32x4_t *>(v + col) = red[0][c][lane] + red[1][c][lane] + red[2][c][lane] + red[3][c][lane];
+    if (col < p.r)
+      *reinterpret_cast<f32x4_t *>(v + col) =
+          red[0][wave][c][lane] + red[1][wave][c][lane] + red[2][wave][c][lane] + red[3][wave][c][lane];
   }
 }
 
-constexpr int kAdCols = 256;  // output columns of a workgroup: 64 per wave
-
-template <typename T, int KB> __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs p) {
-  constexpr int KS = 64 / sizeof(T);
+// Tile = 64 rows x 512 columns, 64 a wave: B_a's fragments are read once for the four row blocks
+template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_kernel(AdapterArgs p) {
   constexpr int E = kChunkElems<T>;
-  constexpr bool PAIR = sizeof(T) == 2;
-  typedef typename Frag<T>::type frag_t;
-  const int nN = (p.dout + kAdCols - 1) / kAdCols;
+  constexpr int W = 64 * kExpandWaves;
+  const int nN = (p.dout + W - 1) / W;
   const int b = ragged_block();
-  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kAdRows, true).find_uniform(b / nN);
+  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kTileRows, p.out != p.base).find_uniform(b / nN);
+  if (!t.valid) return;
+  const int ad = tile_adapter(p, t);
+  if (ad < 0 && p.out == p.base) return;
+  const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+  const int c0 = (b % nN) * W + static_cast<int>(threadIdx.x >> 6) * 64;
+  if (c0 >= p.dout) return;
+  using Cols = Columns<T, KB>;
+  Cols w;
+  w.c0 = c0;
+  const int blocks = (t.rows + 15) >> 4;
+  uint4 bv[Cols::PIECES], next[Cols::PIECES];
+  auto row_of = [&](int i) { return static_cast<size_t>(t.row0) + 16 * i + r16; };
+  w.base_of(p, row_of(0), r16 < t.rows, bv);
+  if (ad < 0) {
+    for (int i = 0; i < blocks; ++i) {
+      const bool there = 16 * i + r16 < t.rows;
+      if (i > 0) w.base_of(p, row_of(i), there, bv);
+      w.put(p, row_of(i), there, bv);
+    }
+    return;
+  }
+  w.load(p, ad, c0);
+  const float sc = p.scale ? p.scale[ad] : 1.f;
+  for (int i = 0; i < blocks; ++i) {
+    const int row = min(16 * i + r16, t.rows - 1);
+    const float *v = p.v + static_cast<size_t>(t.row0 + row) * p.r;
+    VFrag<T> vf[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int k = kb * kStepK<T> + E * g;
+      float f[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) f[j] = 0.f;
+      if (k < p.r)
+        for (int s = 0; s < p.splits; ++s) {
+          const float *q = v + static_cast<size_t>(s) * p.S * p.r + k;
+#pragma unroll
+          for (int j = 0; j < E; j += 4) {
+            const f32x4_t u = *reinterpret_cast<const f32x4_t *>(q + j);
+#pragma unroll
+            for (int l = 0; l < 4; ++l) f[j + l] += u[l];
+          }
+        }
+#pragma unroll
+      for (int j = 0; j < E; ++j) f[j] *= sc;
+      vf[kb].set(f);
+    }
+    // the next block's rows of base are under way while this one's are finished
+    if (i + 1 < blocks) w.base_of(p, row_of(i + 1), 16 * (i + 1) + r16 < t.rows, next);
+    w.finish(p, vf, row_of(i), 16 * i + r16 < t.rows, bv);
+#pragma unroll
+    for (int j = 0; j < Cols::PIECES; ++j) bv[j] = next[j];
+  }
+}
+
+// ---------------------------------------------------------------- few rows
+constexpr int kSmallWaves = 8;
+
+// Tile = 16 rows x one of p.chunks shares of the columns; din split over the waves
+template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) void adapter_small_kernel(AdapterArgs p) {
+  constexpr int E = kChunkElems<T>, KB = kRankSteps<T, RB>;
+  const int b = ragged_block();
+  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kRowBlock, p.out != p.base).find_uniform(b / p.chunks);
   if (!t.valid) return;
   const int ad = tile_adapter(p, t);
   if (ad < 0 && p.out == p.base) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
-  const int c0 = (b % nN) * kAdCols + wave * 64;
-  f32x4_t acc[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  if (ad >= 0) {
-    const float sc = p.scale ? p.scale[ad] : 1.f;
-    const float *v = p.v + static_cast<size_t>(t.row0 + min(r16, t.rows - 1)) * p.r;
-    const T *w = static_cast<const T *>(p.b) + static_cast<size_t>(ad) * p.dout * p.r;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int k = kb * KS + E * g;
-      const bool in = k < p.r;
-      float f[E];
-#pragma unroll
-      for (int i = 0; i < E; ++i) f[i] = 0.f;
-      if (in)
-        for (int s = 0; s < p.splits; ++s) {
-          const float *q = v + static_cast<size_t>(s) * p.S * p.r + k;
-#pragma unroll
-          for (int i = 0; i < E; i += 4) {
-            const f32x4_t u = *reinterpret_cast<const f32x4_t *>(q + i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[i + j] += u[j];
-          }
-        }
-      frag_t hi, lo;
-#pragma unroll
-      for (int i = 0; i < E; ++i) f[i] *= sc;
-      if constexpr (PAIR) {
-        uint32_t h4[4], l4[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h4[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
-          l4[i] = pack_bf16x2(f[2 * i] - __uint_as_float(h4[i] << 16), f[2 * i + 1] - __uint_as_float(h4[i] & 0xffff0000u));
-        }
-        hi = __builtin_bit_cast(frag_t, uint4{h4[0], h4[1], h4[2], h4[3]});
-        lo = __builtin_bit_cast(frag_t, uint4{l4[0], l4[1], l4[2], l4[3]});
-      } else {
-        hi = __builtin_bit_cast(frag_t, uint4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
-      }
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int col = min(PAIR ? c0 + 32 * (c >> 1) + 8 * (r16 >> 2) + 4 * (c & 1) + (r16 & 3) : c0 + 16 * c + r16, p.dout - 1);
-        const frag_t wf = in ? *reinterpret_cast<const frag_t *>(w + static_cast<size_t>(col) * p.r + k) : zero_frag<T>();
-#pragma unroll
-        for (int s = 0; s < Frag<T>::steps; ++s) acc[c] = Frag<T>::mma(wf, hi, s, acc[c]);
-        if constexpr (PAIR) acc[c] = Frag<T>::mma(wf, lo, 0, acc[c]);
-      }
+  const int groups = (p.dout + 63) >> 6, each = (groups + p.chunks - 1) / p.chunks;  // 64-column groups
+  const int g0 = (b % p.chunks) * each, g1 = min(g0 + each, groups);
+  const size_t row = static_cast<size_t>(t.row0) + r16;
+  const bool there = r16 < t.rows;
+  using Cols = Columns<T, KB>;
+  Cols w;
+  uint4 bv[Cols::PIECES];
+  if (ad < 0) {
+    for (int q = g0 + wave; q < g1; q += kSmallWaves) {
+      w.c0 = 64 * q;
+      w.base_of(p, row, there, bv);
+      w.put(p, row, there, bv);
     }
+    return;
   }
-  if (r16 >= t.rows) return;
-  const size_t ro = static_cast<size_t>(t.row0 + r16) * p.dout;
-  const T *base = static_cast<const T *>(p.base) + ro;
-  T *out = static_cast<T *>(p.out) + ro;
+  // the first column group's operands are under way while v is computed
+  if (g0 + wave < g1) {
+    w.load(p, ad, 64 * (g0 + wave));
+    w.base_of(p, row, there, bv);
+  }
+  __shared__ f32x4_t red[kSmallWaves][RB][64];
+  __shared__ f32x4_t vs[16][RB * 4 + 1];
+  f32x4_t acc[1][RB];
+  shrink<T, 1, RB>(p, t, ad, wave * kStepK<T>, kSmallWaves * kStepK<T>, acc);
 #pragma unroll
-  for (int c = 0; c < 4; c += PAIR ? 2 : 1) {
-    const int col = c0 + 16 * c + E * g;
-    if (col >= p.dout) continue;
-    uint4 bv = *reinterpret_cast<const uint4 *>(base + col);
-    if (ad >= 0) {
-      if constexpr (PAIR) {
-        uint32_t *bw = reinterpret_cast<uint32_t *>(&bv);
+  for (int c = 0; c < RB; ++c) red[wave][c][lane] = acc[0][c];
+  __syncthreads();
+  const float sc = p.scale ? p.scale[ad] : 1.f;
+  for (int c = wave; c < RB; c += kSmallWaves) {
+    f32x4_t s = red[0][c][lane];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4_t &d = acc[c + (i >> 1)];
-          bw[i] = pack_bf16x2(__uint_as_float(bw[i] << 16) + d[2 * (i & 1)], __uint_as_float(bw[i] & 0xffff0000u) + d[2 * (i & 1) + 1]);
-        }
-      } else {
-        const f32x4_t s = __builtin_bit_cast(f32x4_t, bv) + acc[c];
-        bv = __builtin_bit_cast(uint4, s);
-      }
+    for (int i = 1; i < kSmallWaves; ++i) s += red[i][c][lane];
+    vs[r16][4 * c + g] = s * sc;
+  }
+  __syncthreads();
+  VFrag<T> vf[KB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const int k = kb * kStepK<T> + E * g;
+    float f[E];
+#pragma unroll
+    for (int j = 0; j < E; j += 4) {
+      const f32x4_t u = k < p.r ? vs[r16][k / 4 + j / 4] : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int l = 0; l < 4; ++l) f[j + l] = u[l];
     }
-    *reinterpret_cast<uint4 *>(out + col) = bv;
+    vf[kb].set(f);
+  }
+  for (int q = g0 + wave; q < g1; q += kSmallWaves) {
+    if (q != g0 + wave) {
+      w.load(p, ad, 64 * q);
+      w.base_of(p, row, there, bv);
+    }
+    w.finish(p, vf, row, there, bv);
   }
 }
 
-template <typename T, int RB> hipError_t launch_rank(const AdapterArgs &p, hipStream_t s) {
-  constexpr int KB = (16 * RB * static_cast<int>(sizeof(T)) + 63) / 64;
-  const long long tiles = ragged_max_tiles(p.S, p.R, kAdRows);
-  const long long shrink = tiles * p.splits, expand = tiles * ((p.dout + kAdCols - 1) / kAdCols);
+// One launch up to kSmallTiles 16-row tiles, their columns in shares that fill the CUs
+constexpr int kSmallTiles = 256;
+bool is_small(int S, int R) { return ragged_max_tiles(S, R, kRowBlock) <= kSmallTiles; }
+
+template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t s) {
+  if (is_small(p.S, p.R)) {
+    const long long tiles = ragged_max_tiles(p.S, p.R, kRowBlock);
+    const long long groups = (p.dout + 63) / 64, most = (groups + kSmallWaves - 1) / kSmallWaves;
+    p.chunks = static_cast<int>(std::max(1ll, std::min(most, 2 * kCUs / tiles)));
+    adapter_small_kernel<T, RB><<<ragged_grid(tiles * p.chunks), 64 * kSmallWaves, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  const long long tiles = ragged_max_tiles(p.S, p.R, kTileRows);
+  const long long shrink = tiles * p.splits, expand = tiles * ((p.dout + 64 * kExpandWaves - 1) / (64 * kExpandWaves));
   if (std::max(shrink, expand) > kRaggedMaxBlocks) return hipErrorInvalidValue;
   adapter_shrink_kernel<T, RB><<<ragged_grid(shrink), 256, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  adapter_expand_kernel<T, KB><<<ragged_grid(expand), 256, 0, s>>>(p);
+  adapter_expand_kernel<T, kRankSteps<T, RB>><<<ragged_grid(expand), 64 * kExpandWaves, 0, s>>>(p);
   return hipGetLastError();
 }
 
 template <typename T> hipError_t launch_t(const AdapterArgs &p, hipStream_t s) {
-  if (p.r <= 16)
-    return launch_rank<T, 1>(p, s);
-  if (p.r <= 32)
-    return launch_rank<T, 2>(p, s);
-  if (p.r <= 64)
-    return launch_rank<T, 4>(p, s);
+  if (p.r <= 16) return launch_rank<T, 1>(p, s);
+  if (p.r <= 32) return launch_rank<T, 2>(p, s);
+  if (p.r <= 64) return launch_rank<T, 4>(p, s);
   return launch_rank<T, 8>(p, s);
 }
 
 }  // namespace
 
 int adapter_splits(int S, int R, int din, bool bf16) {
-  const long long tiles = ragged_max_tiles(S, R, kAdRows);
-  const int ks = bf16 ? 32 : 16;
+  if (is_small(S, R)) return 0;
+  const long long tiles = ragged_max_tiles(S, R, kTileRows);
+  const int step = bf16 ? kStepK<bf16_t> : kStepK<float>;
   int n = 1;
-  while (n < 8 && tiles * n * 2 <= 512 && din / ks >= 8 * 2 * n) n *= 2;
+  // two workgroups a CU, at least four steps for each of a workgroup's four waves
+  while (n < 8 && tiles * n * 2 <= 2 * kCUs && din >= 4 * 4 * 2 * n * step) n *= 2;
   return n;
 }
 

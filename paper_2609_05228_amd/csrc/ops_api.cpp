@@ -265,7 +265,8 @@ ace_status ace_adapter_add(const ace_adapter_desc *desc, const void *base, const
                       {offsets, 4 * (d.R + size_t{1})}, {adapter, 4 * static_cast<size_t>(d.R)}};
   for (const Span &s : ins)
     if (overlap(o, s)) return ACE_ERR_INVALID_ARG;
-  if (!usable(workspace, 256) || workspace_bytes < ace_adapter_workspace_size(desc)) return ACE_ERR_WORKSPACE;
+  const size_t need = ace_adapter_workspace_size(desc);
+  if (need > 0 && (!usable(workspace, 256) || workspace_bytes < need)) return ACE_ERR_WORKSPACE;
   ace::AdapterArgs p{};
   p.base = base;
   p.x = x;

@@ -248,8 +248,9 @@ def adapter_add(base, x, a, b, offsets, adapter, *, scale=None, out=None):
         out = torch.empty_like(base)
     desc = _lib.AdapterDesc(S, R, L, rank, d_in, d_out, _DT[dtype])
     lib = _lib.lib()
-    ws = torch.empty(max(lib.ace_adapter_workspace_size(ctypes.byref(desc)), 256), dtype=torch.uint8, device=dev)
+    n = lib.ace_adapter_workspace_size(desc)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
     _enqueue(dev, lib.ace_adapter_add, desc, base.data_ptr(), x.data_ptr(), a.data_ptr(), b.data_ptr(),
              None if scale is None else scale.data_ptr(), offsets.data_ptr(), adapter.data_ptr(), out.data_ptr(),
-             ws.data_ptr(), ws.numel())
+             None if ws is None else ws.data_ptr(), n)
     return out

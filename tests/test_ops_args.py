@@ -127,7 +127,7 @@ def test_adapter_refusals():
                dict(d_out=4)):
         assert _adapter(**kw) == UNS, kw
     for kw in (dict(ws=None), dict(ws=P[15] + 16), dict(need=-1)):
-        assert _adapter(**kw) == WSP, kw
+        assert _adapter(S=8192, **kw) == WSP, kw
     assert _adapter(S=0, base=None, x=None, out=None) == _lib.ACE_OK
 
 
