@@ -13,6 +13,7 @@
 // v stays exact to 16 bits in bf16 calls: it is multiplied as the sum of two bf16 numbers (a
 // single rounding of v to 8 bits would cost as much as that of the output).
 #include <algorithm>
+#include <type_traits>
 
 #include "lds_dma.h"
 #include "ragged.h"
@@ -23,7 +24,8 @@ namespace {
 
 constexpr int kRowBlock = 16;
 constexpr int kTileRows = 64;    // of the two launches
-constexpr int kExpandWaves = 8;  // 64 columns each
+constexpr int kExpandWaves = 4;  // 64 columns each
+constexpr int kMaxParts = 16;    // partial sums of v
 constexpr int kCUs = 256;
 
 template <typename T> using frag_of = typename Frag<T>::type;
@@ -59,21 +61,32 @@ __device__ __forceinline__ void shrink(const AdapterArgs &p, const RaggedTile &t
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int c = 0; c < RB; ++c) acc[i][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll(RT == 1 ? 4 : 2)
-  for (int k0 = first; k0 < p.din; k0 += step) {
-    const int k = k0 + E * g;
-    const bool in = k < p.din;
-    frag_of<T> xf[RT], wf[RB];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) xf[i] = in ? *reinterpret_cast<const frag_of<T> *>(x[i] + k) : zero_frag<T>();
-#pragma unroll
-    for (int c = 0; c < RB; ++c) wf[c] = in ? *reinterpret_cast<const frag_of<T> *>(w[c] + k) : zero_frag<T>();
+  frag_of<T> xf[RT], wf[RB];
+  auto multiply = [&]() {
 #pragma unroll
     for (int s = 0; s < Frag<T>::steps; ++s)
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int c = 0; c < RB; ++c) acc[i][c] = Frag<T>::mma(wf[c], xf[i], s, acc[i][c]);
+  };
+  int k0 = first;
+#pragma unroll(RT == 1 ? 4 : 2)
+  for (; k0 + kStepK<T> <= p.din; k0 += step) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) xf[i] = *reinterpret_cast<const frag_of<T> *>(x[i] + k0 + E * g);
+#pragma unroll
+    for (int c = 0; c < RB; ++c) wf[c] = *reinterpret_cast<const frag_of<T> *>(w[c] + k0 + E * g);
+    multiply();
+  }
+  if (k0 < p.din) {  // din ends inside the step: zeros behind the end, in both operands
+    const int k = k0 + E * g;
+    const bool in = k < p.din;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) xf[i] = in ? *reinterpret_cast<const frag_of<T> *>(x[i] + k) : zero_frag<T>();
+#pragma unroll
+    for (int c = 0; c < RB; ++c) wf[c] = in ? *reinterpret_cast<const frag_of<T> *>(w[c] + k) : zero_frag<T>();
+    multiply();
   }
 }
 
@@ -97,6 +110,26 @@ template <typename T> struct VFrag {
   }
 };
 
+// Rows of v in LDS, 16-byte quads: odd strides, so that 16 rows' reads go to different banks
+template <typename T, int KB> constexpr int kVStride = KB * kStepK<T> / 4 + 1;
+template <typename T, int KB>
+__device__ __forceinline__ void read_v(const f32x4_t *vs, int row, int r, VFrag<T> (&vf)[KB]) {
+  constexpr int E = kChunkElems<T>;
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const int k = kb * kStepK<T> + E * g;
+    float f[E];
+#pragma unroll
+    for (int j = 0; j < E; j += 4) {
+      const f32x4_t u = k < r ? vs[row * kVStride<T, KB> + k / 4 + j / 4] : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int l = 0; l < 4; ++l) f[j + l] = u[l];
+    }
+    vf[kb].set(f);
+  }
+}
+
 // 64 columns of B_a from c0, as fragments.  bf16: the columns of two 16-column blocks interleaved in fours,
 // so that a lane's results are 8 consecutive columns (see grouped.hip)
 template <typename T, int KB> struct Columns {
@@ -114,7 +147,9 @@ template <typename T, int KB> struct Columns {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         const int k = kb * kStepK<T> + E * g;
-        w[kb][c] = k < p.r ? *reinterpret_cast<const frag_of<T> *>(b + static_cast<size_t>(col) * p.r + k) : zero_frag<T>();
+        // loaded in any case and replaced behind the end of the rank, so that no load is a branch of its own
+        const frag_of<T> f = *reinterpret_cast<const frag_of<T> *>(b + static_cast<size_t>(col) * p.r + min(k, p.r - E));
+        w[kb][c] = k < p.r ? f : zero_frag<T>();
       }
     }
   }
@@ -169,6 +204,16 @@ template <typename T, int KB> struct Columns {
   }
 };
 
+// Share `chunk` of p.chunks of the 64-column groups of the output
+struct Groups {
+  int first, last;
+  __device__ __forceinline__ Groups(const AdapterArgs &p, int chunk) {
+    const int groups = (p.dout + 63) >> 6, each = (groups + p.chunks - 1) / p.chunks;
+    first = chunk * each;
+    last = min(first + each, groups);
+  }
+};
+
 // ---------------------------------------------------------------- many rows
 template <typename T, int RB> __global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterArgs p) {
   constexpr int RT = kTileRows / kRowBlock;
@@ -179,86 +224,101 @@ template <typename T, int RB> __global__ __launch_bounds__(256) void adapter_shr
   if (ad < 0) return;
   const int split = b % p.splits;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
-  f32x4_t acc[RT][RB];
-  shrink<T, RT, RB>(p, t, ad, (split * 4 + wave) * kStepK<T>, 4 * p.splits * kStepK<T>, acc);
-  // the waves' sums, one row block after the other: wave i adds block i's in wave order
-  __shared__ f32x4_t red[4][RT][RB][64];
+  __shared__ f32x4_t red[4][RB][64];
+  // with as many row blocks as the tile has (1, 2 or all)
+  auto run = [&](auto rt) {
+    f32x4_t acc[rt()][RB];
+    shrink<T, rt(), RB>(p, t, ad, (split * 4 + wave) * kStepK<T>, 4 * p.splits * kStepK<T>, acc);
+    // the waves' sums: row block i's are added by wave i in wave order
 #pragma unroll
-  for (int i = 0; i < RT; ++i)
+    for (int i = 0; i < rt(); ++i) {
+      if (i > 0) __syncthreads();
 #pragma unroll
-    for (int c = 0; c < RB; ++c) red[wave][i][c][lane] = acc[i][c];
-  __syncthreads();
-  const int row = 16 * wave + r16;
-  if (row >= t.rows) return;
-  float *v = p.v + (static_cast<size_t>(split) * p.S + t.row0 + row) * p.r;
+      for (int c = 0; c < RB; ++c) red[wave][c][lane] = acc[i][c];
+      __syncthreads();
+      const int row = 16 * i + r16;
+      if (wave != i || row >= t.rows) continue;
+      float *v = p.v + (static_cast<size_t>(split) * p.S + t.row0 + row) * p.r;
 #pragma unroll
-  for (int c = 0; c < RB; ++c) {
-    const int col = 16 * c + 4 * g;
-    if (col < p.r)
-      *reinterpret_cast<f32x4_t *>(v + col) =
-          red[0][wave][c][lane] + red[1][wave][c][lane] + red[2][wave][c][lane] + red[3][wave][c][lane];
-  }
+      for (int c = 0; c < RB; ++c) {
+        const int col = 16 * c + 4 * g;
+        if (col < p.r)
+          *reinterpret_cast<f32x4_t *>(v + col) = red[0][c][lane] + red[1][c][lane] + red[2][c][lane] + red[3][c][lane];
+      }
+    }
+  };
+  if (t.rows <= 16)
+    run(std::integral_constant<int, 1>{});
+  else if (t.rows <= 32)
+    run(std::integral_constant<int, 2>{});
+  else
+    run(std::integral_constant<int, RT>{});
 }
 
-// Tile = 64 rows x 512 columns, 64 a wave: B_a's fragments are read once for the four row blocks
+// Tile = 64 rows x one of p.chunks shares of the columns, 64 of them a wave at a time: B_a's fragments
+// are read once for the four row blocks
 template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_kernel(AdapterArgs p) {
-  constexpr int E = kChunkElems<T>;
-  constexpr int W = 64 * kExpandWaves;
-  const int nN = (p.dout + W - 1) / W;
   const int b = ragged_block();
-  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kTileRows, p.out != p.base).find_uniform(b / nN);
+  const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kTileRows, p.out != p.base).find_uniform(b / p.chunks);
   if (!t.valid) return;
   const int ad = tile_adapter(p, t);
   if (ad < 0 && p.out == p.base) return;
-  const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
-  const int c0 = (b % nN) * W + static_cast<int>(threadIdx.x >> 6) * 64;
-  if (c0 >= p.dout) return;
+  const int r16 = threadIdx.x & 15, wave = threadIdx.x >> 6;
+  const Groups cols(p, b % p.chunks);
   using Cols = Columns<T, KB>;
   Cols w;
-  w.c0 = c0;
-  const int blocks = (t.rows + 15) >> 4;
   uint4 bv[Cols::PIECES], next[Cols::PIECES];
+  const int blocks = (t.rows + 15) >> 4;
   auto row_of = [&](int i) { return static_cast<size_t>(t.row0) + 16 * i + r16; };
-  w.base_of(p, row_of(0), r16 < t.rows, bv);
+  auto there = [&](int i) { return 16 * i + r16 < t.rows; };
   if (ad < 0) {
-    for (int i = 0; i < blocks; ++i) {
-      const bool there = 16 * i + r16 < t.rows;
-      if (i > 0) w.base_of(p, row_of(i), there, bv);
-      w.put(p, row_of(i), there, bv);
+    for (int q = cols.first + wave; q < cols.last; q += kExpandWaves) {
+      w.c0 = 64 * q;
+      for (int i = 0; i < blocks; ++i) {
+        w.base_of(p, row_of(i), there(i), bv);
+        w.put(p, row_of(i), there(i), bv);
+      }
     }
     return;
   }
-  w.load(p, ad, c0);
+  // v of the tile's rows: the parts added in order, times the scale, once for all waves
+  __shared__ f32x4_t vs[kTileRows * kVStride<T, KB>];
   const float sc = p.scale ? p.scale[ad] : 1.f;
-  for (int i = 0; i < blocks; ++i) {
-    const int row = min(16 * i + r16, t.rows - 1);
-    const float *v = p.v + static_cast<size_t>(t.row0 + row) * p.r;
-    VFrag<T> vf[KB];
+  const int quads = p.r >> 2;
+  for (int i = threadIdx.x; i < t.rows * quads; i += 64 * kExpandWaves) {
+    const int row = i / quads, q = i % quads;
+    const float *v = p.v + static_cast<size_t>(t.row0 + row) * p.r + 4 * q;
+    f32x4_t sum = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < p.splits; s0 += 4) {  // four loads in flight
+      f32x4_t u[4];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int k = kb * kStepK<T> + E * g;
-      float f[E];
+      for (int s = 0; s < 4; ++s)
+        u[s] = *reinterpret_cast<const f32x4_t *>(v + static_cast<size_t>(min(s0 + s, p.splits - 1)) * p.S * p.r);
 #pragma unroll
-      for (int j = 0; j < E; ++j) f[j] = 0.f;
-      if (k < p.r)
-        for (int s = 0; s < p.splits; ++s) {
-          const float *q = v + static_cast<size_t>(s) * p.S * p.r + k;
-#pragma unroll
-          for (int j = 0; j < E; j += 4) {
-            const f32x4_t u = *reinterpret_cast<const f32x4_t *>(q + j);
-#pragma unroll
-            for (int l = 0; l < 4; ++l) f[j + l] += u[l];
-          }
-        }
-#pragma unroll
-      for (int j = 0; j < E; ++j) f[j] *= sc;
-      vf[kb].set(f);
+      for (int s = 0; s < 4; ++s)
+        if (s0 + s < p.splits) sum += u[s];
     }
-    // the next block's rows of base are under way while this one's are finished
-    if (i + 1 < blocks) w.base_of(p, row_of(i + 1), 16 * (i + 1) + r16 < t.rows, next);
-    w.finish(p, vf, row_of(i), 16 * i + r16 < t.rows, bv);
+    vs[row * kVStride<T, KB> + q] = sum * sc;
+  }
+  if (cols.first + wave < cols.last) {  // under way while the waves meet
+    w.load(p, ad, 64 * (cols.first + wave));
+    w.base_of(p, row_of(0), there(0), bv);
+  }
+  __syncthreads();
+  for (int q = cols.first + wave; q < cols.last; q += kExpandWaves) {
+    if (q != cols.first + wave) {
+      w.load(p, ad, 64 * q);
+      w.base_of(p, row_of(0), there(0), bv);
+    }
+    for (int i = 0; i < blocks; ++i) {
+      VFrag<T> vf[KB];
+      read_v<T, KB>(vs, 16 * i + r16, p.r, vf);
+      // the next block's rows of base are under way while this one's are finished
+      if (i + 1 < blocks) w.base_of(p, row_of(i + 1), there(i + 1), next);
+      w.finish(p, vf, row_of(i), there(i), bv);
 #pragma unroll
-    for (int j = 0; j < Cols::PIECES; ++j) bv[j] = next[j];
+      for (int j = 0; j < Cols::PIECES; ++j) bv[j] = next[j];
+    }
   }
 }
 
@@ -267,15 +327,15 @@ constexpr int kSmallWaves = 8;
 
 // Tile = 16 rows x one of p.chunks shares of the columns; din split over the waves
 template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) void adapter_small_kernel(AdapterArgs p) {
-  constexpr int E = kChunkElems<T>, KB = kRankSteps<T, RB>;
+  constexpr int KB = kRankSteps<T, RB>;
   const int b = ragged_block();
   const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kRowBlock, p.out != p.base).find_uniform(b / p.chunks);
   if (!t.valid) return;
   const int ad = tile_adapter(p, t);
   if (ad < 0 && p.out == p.base) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
-  const int groups = (p.dout + 63) >> 6, each = (groups + p.chunks - 1) / p.chunks;  // 64-column groups
-  const int g0 = (b % p.chunks) * each, g1 = min(g0 + each, groups);
+  const Groups cols(p, b % p.chunks);
+  const int g0 = cols.first, g1 = cols.last;
   const size_t row = static_cast<size_t>(t.row0) + r16;
   const bool there = r16 < t.rows;
   using Cols = Columns<T, KB>;
@@ -295,7 +355,7 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
     w.base_of(p, row, there, bv);
   }
   __shared__ f32x4_t red[kSmallWaves][RB][64];
-  __shared__ f32x4_t vs[16][RB * 4 + 1];
+  __shared__ f32x4_t vs[kRowBlock * kVStride<T, KB>];
   f32x4_t acc[1][RB];
   shrink<T, 1, RB>(p, t, ad, wave * kStepK<T>, kSmallWaves * kStepK<T>, acc);
 #pragma unroll
@@ -306,22 +366,11 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
     f32x4_t s = red[0][c][lane];
 #pragma unroll
     for (int i = 1; i < kSmallWaves; ++i) s += red[i][c][lane];
-    vs[r16][4 * c + g] = s * sc;
+    if (4 * c + g < KB * kStepK<T> / 4) vs[r16 * kVStride<T, KB> + 4 * c + g] = s * sc;
   }
   __syncthreads();
   VFrag<T> vf[KB];
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb) {
-    const int k = kb * kStepK<T> + E * g;
-    float f[E];
-#pragma unroll
-    for (int j = 0; j < E; j += 4) {
-      const f32x4_t u = k < p.r ? vs[r16][k / 4 + j / 4] : f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int l = 0; l < 4; ++l) f[j + l] = u[l];
-    }
-    vf[kb].set(f);
-  }
+  read_v<T, KB>(vs, r16, p.r, vf);
   for (int q = g0 + wave; q < g1; q += kSmallWaves) {
     if (q != g0 + wave) {
       w.load(p, ad, 64 * q);
@@ -331,12 +380,17 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
   }
 }
 
-// One launch up to kSmallTiles 16-row tiles, their columns in shares that fill the CUs
+// One launch for up to kSmallTiles 16-row tiles, their columns in shares that fill the CUs, unless computing v
+// in each share takes longer than another launch: past 512 KB of A_a in bf16, 256 KB in fp32,
+// whose products take 16 times as long.
 constexpr int kSmallTiles = 256;
-bool is_small(int S, int R) { return ragged_max_tiles(S, R, kRowBlock) <= kSmallTiles; }
+bool is_small(int S, int R, int r, int din, bool bf16) {
+  const long long bytes = static_cast<long long>((r + 15) / 16 * 16) * din * (bf16 ? 2 : 4);
+  return ragged_max_tiles(S, R, kRowBlock) <= kSmallTiles && bytes <= (bf16 ? 512 : 256) << 10;
+}
 
 template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t s) {
-  if (is_small(p.S, p.R)) {
+  if (is_small(p.S, p.R, p.r, p.din, sizeof(T) == 2)) {
     const long long tiles = ragged_max_tiles(p.S, p.R, kRowBlock);
     const long long groups = (p.dout + 63) / 64, most = (groups + kSmallWaves - 1) / kSmallWaves;
     p.chunks = static_cast<int>(std::max(1ll, std::min(most, 2 * kCUs / tiles)));
@@ -344,7 +398,11 @@ template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t 
     return hipGetLastError();
   }
   const long long tiles = ragged_max_tiles(p.S, p.R, kTileRows);
-  const long long shrink = tiles * p.splits, expand = tiles * ((p.dout + 64 * kExpandWaves - 1) / (64 * kExpandWaves));
+  // column shares: eight workgroups a CU, where there are more tiles fewer, longer ones (1225 rows of 504 requests,
+  // 3280 columns: 57 us with a workgroup for every 256 columns)
+  const long long most = (p.dout + 64 * kExpandWaves - 1) / (64 * kExpandWaves);
+  p.chunks = static_cast<int>(std::min(most, (8 * kCUs + tiles - 1) / tiles));
+  const long long shrink = tiles * p.splits, expand = tiles * p.chunks;
   if (std::max(shrink, expand) > kRaggedMaxBlocks) return hipErrorInvalidValue;
   adapter_shrink_kernel<T, RB><<<ragged_grid(shrink), 256, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
@@ -356,19 +414,21 @@ template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t 
 template <typename T> hipError_t launch_t(const AdapterArgs &p, hipStream_t s) {
   if (p.r <= 16) return launch_rank<T, 1>(p, s);
   if (p.r <= 32) return launch_rank<T, 2>(p, s);
+  if (p.r <= 48) return launch_rank<T, 3>(p, s);
   if (p.r <= 64) return launch_rank<T, 4>(p, s);
+  if (p.r <= 96) return launch_rank<T, 6>(p, s);
   return launch_rank<T, 8>(p, s);
 }
 
 }  // namespace
 
-int adapter_splits(int S, int R, int din, bool bf16) {
-  if (is_small(S, R)) return 0;
+int adapter_splits(int S, int R, int r, int din, bool bf16) {
+  if (is_small(S, R, r, din, bf16)) return 0;
   const long long tiles = ragged_max_tiles(S, R, kTileRows);
   const int step = bf16 ? kStepK<bf16_t> : kStepK<float>;
   int n = 1;
-  // two workgroups a CU, at least four steps for each of a workgroup's four waves
-  while (n < 8 && tiles * n * 2 <= 2 * kCUs && din >= 4 * 4 * 2 * n * step) n *= 2;
+  // four workgroups a CU, at least four steps for each of a workgroup's four waves
+  while (n < kMaxParts && tiles * n * 2 <= 4 * kCUs && din >= 4 * 4 * 2 * n * step) n *= 2;
   return n;
 }
 

@@ -46,6 +46,7 @@ struct RaggedTiles {
     const int lane = threadIdx.x & 63;
     const int p0 = lane * per;
     int lo = bound(p0);
+#pragma unroll 4  // the loads of four groups in flight together, here and below
     for (int j = 0; j < per; ++j) {
       const int hi = bound(p0 + j + 1);
       cnt += tiles(p0 + j, lo, hi);
@@ -91,24 +92,33 @@ struct RaggedTiles {
       if (__shfl(inc, src + o - 1) <= tile) src += o;
     int q = tile - __shfl(inc - cnt, src);
     if (tile < 0 || tile >= total) return t;
-    int p = src * per, lo = bound(p);
-    for (int j = 0; j < per; ++j, ++p) {
-      const int hi = bound(p + 1), n = tiles(p, lo, hi);
-      if (q < n) {
-        t.group = p == 0 || p == N + 1 ? -1 : p - 1;
-        // its 16-row blocks spread evenly over its tiles: a short tile would stream the group's
-        // operands for a few rows
-        const uint32_t blocks = (static_cast<uint32_t>(hi - lo) + 15u) >> 4, each = blocks / n, more = blocks % n;
-        const uint32_t b0 = q * each + min(static_cast<uint32_t>(q), more);
-        t.row0 = lo + static_cast<int>(b0 << 4);
-        t.rows = min(static_cast<int>((each + (q < static_cast<int>(more))) << 4), hi - t.row0);
-        t.valid = true;
-        t.only = n == 1;
-        break;
+    const int p0 = src * per;
+    int lo = bound(p0), from = 0, to = 0, n = 0;
+#pragma unroll 4
+    for (int j = 0; j < per; ++j) {
+      const int hi = bound(p0 + j + 1), m = tiles(p0 + j, lo, hi);
+      if (n == 0) {  // not found yet
+        if (q < m) {
+          t.group = p0 + j;
+          from = lo;
+          to = hi;
+          n = m;
+        } else {
+          q -= m;
+        }
       }
-      q -= n;
       lo = hi;
     }
+    if (n == 0) return t;
+    t.group = t.group == 0 || t.group == N + 1 ? -1 : t.group - 1;
+    // the group's 16-row blocks spread evenly over its tiles: a short tile would stream the group's
+    // operands for a few rows
+    const uint32_t blocks = (static_cast<uint32_t>(to - from) + 15u) >> 4, each = blocks / n, more = blocks % n;
+    const uint32_t b0 = q * each + min(static_cast<uint32_t>(q), more);
+    t.row0 = from + static_cast<int>(b0 << 4);
+    t.rows = min(static_cast<int>((each + (q < static_cast<int>(more))) << 4), to - t.row0);
+    t.valid = true;
+    t.only = n == 1;
     return t;
   }
 

@@ -10,14 +10,15 @@ torch's allocator with every call, so captured graphs share none.
 """
 from __future__ import annotations
 
-import ctypes
-
 import torch
 
 from . import _lib
 from .layer import _DT
 
-_GATES = ("none", "channel", "token", "full")
+# the raw handle of a device's current stream; torch.cuda.current_stream builds a Stream object around
+# it, which costs a call more than its checks
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _need(ok, msg):
@@ -29,6 +30,9 @@ def _check_all(dev, dtype, named):
     """(name, tensor, shape, dtype or None for the call's): shapes, types, layout, device."""
     grad = torch.is_grad_enabled()
     for name, t, shape, dt in named:
+        if (t.shape == shape and t.dtype is (dt or dtype) and t.device == dev and t.is_contiguous()
+                and not (grad and t.requires_grad)):
+            continue
         if t.shape != shape:
             raise ValueError(f"{name}: shape {tuple(t.shape)} != {tuple(shape)}")
         if t.dtype != (dt or dtype):
@@ -37,25 +41,27 @@ def _check_all(dev, dtype, named):
             raise ValueError(f"{name} must be contiguous")
         if t.device != dev:
             raise ValueError(f"{name} is on {t.device}, expected {dev}")
-        if grad and t.requires_grad:
-            raise ValueError(f"{name} requires a gradient: call under torch.no_grad() and use the *_grad functions")
+        raise ValueError(f"{name} requires a gradient: call under torch.no_grad() and use the *_grad functions")
     if dev.type != "cuda":
         raise ValueError(f"the tensors are on {dev}: a GPU is needed")
 
 
 def _dtype_of(name, t, dims):
-    _need(isinstance(t, torch.Tensor) and t.dim() == dims, f"{name} must be a tensor of {dims} dimensions")
-    _need(t.dtype in _DT, f"{name}: unsupported dtype {t.dtype}")
+    if not isinstance(t, torch.Tensor) or t.dim() != dims:
+        raise ValueError(f"{name} must be a tensor of {dims} dimensions")
+    if t.dtype not in _DT:
+        raise ValueError(f"{name}: unsupported dtype {t.dtype}")
     return t.dtype
 
 
 def _enqueue(dev, fn, *args):
     """fn(*args, stream) on the current stream of dev, with dev current."""
-    if dev.index == torch.cuda.current_device():
-        st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    index = dev.index
+    if index == torch.cuda.current_device():
+        st = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(dev):
-            st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            st = fn(*args, _raw_stream(index))
     if st != _lib.ACE_OK:
         raise _lib.AceError(st, _lib.status_string(st))
 
@@ -128,27 +134,30 @@ def grouped_matmul_grad_w(dy, x, offsets, *, out=None):
                     ((S, M), (S, K)), out)
 
 
-def _norm_call(rows, d, dtype, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, more):
-    """Check a block_norm call's tensors; (desc, inputs)."""
-    named = list(more)
-    for name, t in (("h", h), ("y", y)):
-        if t is not None:
-            named.append((name, t, (rows, d), None))
-    for name, t in (("w_post", w_post), ("w_pre", w_pre)):
-        if t is not None:
-            named.append((name, t, (d,), None))
-    kind = 0
+def _norm_call(lead, dtype, T, d, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, named):
+    """Check a block_norm call's tensors, `named` among them; (desc, inputs)."""
+    rows, vec, kind = (T, d), (d,), 0
+    if y is not None:
+        named.append(("y", y, rows, None))
+    elif w_post is not None or gate is not None or res_scale != 1.0:
+        raise ValueError("w_post, gate and res_scale need y")
+    elif w_pre is None:
+        raise ValueError("y or w_pre is required")
+    if w_post is not None:
+        named.append(("w_post", w_post, vec, None))
+    if w_pre is not None:
+        named.append(("w_pre", w_pre, vec, None))
     if gate is not None:
-        kind = {(d,): 1, (rows, 1): 2, (rows, d): 3}.get(tuple(gate.shape), 0)
-        _need(kind, f"gate: shape {tuple(gate.shape)} is none of [d], [T, 1], [T, d]")
-        named.append(("gate", gate, gate.shape, None))
-    _need(y is not None or (w_post is None and gate is None and res_scale == 1.0),
-          "w_post, gate and res_scale need y")
-    _need(y is not None or w_pre is not None, "y or w_pre is required")
-    _check_all(named[0][1].device, dtype, named)
-    desc = _lib.NormDesc(rows, d, _DT[dtype], kind, res_scale, branch_scale, eps)
-    inp = _lib.NormInputs(*[None if t is None else t.data_ptr() for t in (h, y, w_post, w_pre, gate)])
-    return desc, inp
+        shape = tuple(gate.shape)
+        kind = 1 if shape == vec else 2 if shape == (T, 1) else 3 if shape == rows else 0
+        if kind == 0:
+            raise ValueError(f"gate: shape {shape} is none of [d], [T, 1], [T, d]")
+        named.append(("gate", gate, shape, None))
+    _check_all(lead.device, dtype, named)
+    return (_lib.NormDesc(T, d, _DT[dtype], kind, res_scale, branch_scale, eps),
+            _lib.NormInputs(h if h is None else h.data_ptr(), y if y is None else y.data_ptr(),
+                            w_post if w_post is None else w_post.data_ptr(),
+                            w_pre if w_pre is None else w_pre.data_ptr(), gate if gate is None else gate.data_ptr()))
 
 
 def block_norm(h, y=None, *, w_post=None, w_pre=None, gate=None, res_scale=1.0, branch_scale=1.0, eps=1e-6, out=None):
@@ -166,10 +175,13 @@ def block_norm(h, y=None, *, w_post=None, w_pre=None, gate=None, res_scale=1.0, 
     d is a multiple of 8 (fp32: 4), at most 16384; eps > 0.  Returns dict(h=h'[, n]); without y, h' is h."""
     dtype = _dtype_of("h", h, 2)
     T, d = h.shape
-    out = {} if out is None else dict(out)
-    more = [(f"out['{k}']", out[k], (T, d), None) for k in ("h", "n") if k in out]
-    desc, inp = _norm_call(T, d, dtype, h, y, w_post, w_pre, gate, float(res_scale), float(branch_scale), float(eps),
-                           [("h", h, (T, d), None)] + more)
+    named = [("h", h, h.shape, None)]
+    if out is None:
+        out = {}
+    else:
+        out = dict(out)
+        named += [(f"out['{k}']", out[k], h.shape, None) for k in ("h", "n") if k in out]
+    desc, inp = _norm_call(h, dtype, T, d, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, named)
     if y is None:
         out["h"] = h
     elif "h" not in out:
@@ -198,17 +210,16 @@ def block_norm_grad(dh, dn, h, y=None, *, w_post=None, w_pre=None, gate=None, re
     T, d = lead.shape
     _need((dn is None) == (w_pre is None), "dn and w_pre go together")
     _need(h is not None or w_pre is None, "h is required with w_pre")
-    more = [(n, t, (T, d), None) for n, t in (("dh", dh), ("dn", dn)) if t is not None]
-    desc, inp = _norm_call(T, d, dtype, h, y, w_post, w_pre, gate, float(res_scale), float(branch_scale), float(eps),
-                           more)
+    named = [(n, t, lead.shape, None) for n, t in (("dh", dh), ("dn", dn), ("h", h)) if t is not None]
+    desc, inp = _norm_call(lead, dtype, T, d, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, named)
     dev = lead.device
     out = {"h": torch.empty_like(lead)}
     for name, t in (("y", y), ("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
         if t is not None:
             out[name] = torch.empty_like(t)
-    grads = _lib.NormGrads(*[out[n].data_ptr() if n in out else None for n in ("h", "y", "w_post", "w_pre", "gate")])
+    grads = _lib.NormGrads(**{n: t.data_ptr() for n, t in out.items()})
     lib = _lib.lib()
-    n = lib.ace_block_norm_grad_workspace_size(ctypes.byref(desc))
+    n = lib.ace_block_norm_grad_workspace_size(desc)
     ws = torch.empty(max(n, 256), dtype=torch.uint8, device=dev)
     _enqueue(dev, lib.ace_block_norm_grad, desc, inp, None if dh is None else dh.data_ptr(),
              None if dn is None else dn.data_ptr(), grads, ws.data_ptr(), ws.numel())
