@@ -80,6 +80,37 @@ def test_against_the_definition(case, dtype):
     check(ace.adapter_add(args[0].to(DEV), *d[1:]), args, None, dtype)
 
 
+# tiles of 64 rows: every rank class, tiles of one to four row blocks, several column shares and parts
+LARGE = [
+    ([1500, 700, 33, 0, 2100, 20, 5, 48], [0, 1, 2, 3, -1, 1, 0, 2], 3, 5, 3, 8, 136, 72),
+    ([1500, 700, 33, 0, 2100, 20, 5, 48], [0, 1, 2, 3, -1, 1, 0, 2], 0, 0, 4, 24, 520, 328),
+    ([4100, 1, 1, 40], [1, 0, 1, 0], 0, 17, 2, 40, 264, 600),
+    ([4200], [0], 0, 0, 1, 64, 1032, 264),
+    ([2000, 2300], [1, 0], 0, 0, 2, 88, 136, 136),
+    ([4500], [0], 0, 0, 1, 128, 264, 520),
+    ([i % 9 for i in range(600)], [i % 7 - 1 for i in range(600)], 2, 1, 6, 16, 72, 1000),
+    ([30, 2], [0, 1], 0, 0, 2, 128, 4104, 136),  # few rows, a long inner product: parts of it
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", LARGE, ids=lambda c: f"{len(c[0])}req_{sum(c[0])}r_rank{c[5]}_{c[6]}x{c[7]}")
+def test_many_rows(case, dtype):
+    from paper_2609_05228_amd import _lib
+
+    *args, scale = make(*case, dtype)
+    code = _lib.ACE_BF16 if dtype == "bf16" else _lib.ACE_F32
+    desc = _lib.AdapterDesc(args[0].shape[0], len(case[0]), case[4], case[5], case[6], case[7], code)
+    assert ace.lib().ace_adapter_workspace_size(desc) > 0
+    d = [t.to(DEV) for t in args]
+    got = ace.adapter_add(*d, scale=scale.to(DEV))
+    torch.cuda.synchronize()
+    check(got, args, scale, dtype)
+    assert torch.equal(ace.adapter_add(*d, scale=scale.to(DEV)), got)
+    assert ace.adapter_add(*d, scale=scale.to(DEV), out=d[0]) is d[0]
+    assert torch.equal(d[0], got)
+
+
 def test_no_rows():
     *args, scale = make([], [], 0, 0, 1, 8, 64, 40, "bf16")
     assert ace.adapter_add(*[t.to(DEV) for t in args]).shape == (0, 40)

@@ -11,9 +11,9 @@ pytestmark = pytest.mark.gpu
 
 DEV = "cuda:0"
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
-# fp32 operations on a result's terms: a sum over a row is at most 38 deep (16 elements in a
-# thread, 6 steps in a wave, 16 waves), one over the rows of these cases at most 40, and some 20
-# more form a result from them
+# fp32 operations on a result's terms: a sum over a row is at most 26 deep (16 elements in a
+# thread, 6 steps in a wave, 4 over the waves), one over the rows of these cases at most 50 (2 rows of a
+# thread, 16 of a workgroup, 16 lines of a wave, 16 waves), and some 10 more form a result from them
 TERMS = 64
 
 SIZES = [(1, 8), (1, 2048), (3, 64), (7, 520), (5, 1032), (2, 4096), (3, 4104), (2, 8192), (2, 16384), (515, 264)]
@@ -72,6 +72,22 @@ def test_forms(post, pre, gate, dtype):
     both(t, dh, dn, dtype, eps=1e-5)
     if pre:
         both(t, None, dn, dtype, branch_scale=-2.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", [(4200, 72), (1100, 1032), (530, 4104), (300, 8192)])
+def test_more_rows_than_one_round(T, d, dtype):
+    """Workgroups that take several rows one after the other, the next ones copied ahead."""
+    t, dh, dn = make(T, d, dtype)
+    both(t, dh, dn, dtype, res_scale=1.25, branch_scale=-0.5)
+
+
+@pytest.mark.parametrize("post,pre,gate", list(itertools.product([True, False], [True, False],
+                                                                 ["none", "channel", "token", "full"])))
+def test_forms_of_several_rows(post, pre, gate):
+    """The gradients of each form store differently many results behind the copies they wait for."""
+    t, dh, dn = make(9000, 40, "bf16", gate, post, pre)
+    both(t, dh, dn, "bf16")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

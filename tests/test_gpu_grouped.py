@@ -209,3 +209,99 @@ def test_streams_graphs_and_repeats(fn):
         torch.cuda.synchronize()
         assert torch.equal(got, want)
         assert torch.equal(f(a, b, d[3]), want)
+
+
+def check_all(sizes, tail, M, K, dtype="bf16", seed=0, ways=("fwd", "grad_x", "grad_w")):
+    """The ways against the definition in 64 bits, on the GPU (larger cases)."""
+    x, w, dy, offs = make(sizes, 0, tail, M, K, dtype, seed)
+    d = [t.to(DEV) for t in (x, w, dy, offs)]
+    n = int(offs[-1])
+    gap = rest(offs, x.shape[0])
+    calls = {"fwd": (ace.grouped_matmul, d[0], d[1], K), "grad_x": (ace.grouped_matmul_grad_x, d[2], d[1], M),
+             "grad_w": (ace.grouped_matmul_grad_w, d[2], d[0], max(max(sizes), 1))}
+    for way in ways:
+        fn, a, b, terms = calls[way]
+        got = fn(a, b, d[3])
+        torch.cuda.synchronize()
+        if way == "grad_w":
+            want, mag = ref.grouped_grad_w(dy, x, offs)
+        else:
+            want, mag = ref.grouped(a.cpu(), w if way == "fwd" else w.transpose(1, 2), offs)
+            assert not got[gap].any()
+        ref.close(got, want, mag, DT[dtype], terms, way)
+        assert torch.equal(fn(a, b, d[3]), got)
+    return n
+
+
+def shape_of(sizes, cols):
+    """The tile shape that the large kernel takes, by its documented costs."""
+    def cost(rows, width, stage):
+        items = sum(-(-n // rows) for n in sizes) * -(-cols // width)
+        return -(-items // 256) * stage
+    costs = {"256": cost(256, 256, 42), "320": cost(320, 192, 41), "192": cost(192, 192, 28), "192w": cost(192, 256, 35)}
+    return min(costs, key=costs.get)
+
+
+LARGE = {"192": (64, 185, 1032), "192w": (40, 180, 1288), "256": (64, 250, 776), "320": (40, 250, 2056)}
+
+
+@pytest.mark.parametrize("shape", LARGE)
+def test_large_shapes(shape):
+    """Every tile shape of the large kernel (many rows a group), forward and rows' gradient."""
+    N, r, cols = LARGE[shape]
+    sizes = [r + (i * 7) % 11 - 5 for i in range(N)]
+    assert shape_of(sizes, cols) == shape and sum(sizes) > 80 * N
+    check_all(sizes, 0, cols, 72, ways=("fwd",))
+    check_all(sizes, 0, 72, cols, ways=("grad_x",))
+
+
+def test_large_with_a_skewed_plan():
+    """Groups of none to thousands of rows, rows of no group behind them."""
+    sizes = [3000, 0, 1, 700, 15, 16, 17, 0, 1100, 256, 257, 90] * 2
+    assert sum(sizes) > 80 * len(sizes)
+    check_all(sizes, 130, 1544, 136, ways=("fwd",))
+    check_all(sizes, 130, 136, 1544, ways=("grad_x",))
+
+
+@pytest.mark.parametrize("sizes,M,K", [([20] * 40, 1544, 104), ([50] * 40, 1544, 136), ([9, 0, 40] * 30, 1160, 200)])
+def test_middle_shapes(sizes, M, K):
+    """64 x 128 and 128 x 128 tiles: enough of them, few rows a group."""
+    check_all(sizes, 3, M, K, ways=("fwd",))
+    check_all(sizes, 3, K, M, ways=("grad_x",))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sizes,M,K", [([3, 2], 64, 4168), ([700, 900], 72, 136), ([2000], 8, 8), ([0, 5000, 1], 40, 200)])
+def test_split_reductions(sizes, M, K, dtype):
+    """Few tiles with a long reduction: its parts are joined in order, rows of no group stay zero."""
+    size = ace.lib().ace_grouped_workspace_size
+    from paper_2609_05228_amd import _lib
+    code = _lib.ACE_BF16 if dtype == "bf16" else _lib.ACE_F32
+    desc = _lib.GroupedDesc(sum(sizes) + 4, len(sizes), M, K, code, 0)
+    assert size(desc, 0 if K > 1000 else 2) > 0
+    check_all(sizes, 4, M, K, dtype)
+    check_all(sizes, 4, K, M, dtype)
+
+
+@pytest.mark.parametrize("sizes,M,K", [([65, 0, 3, 130, 1] * 14, 264, 520), ([30] * 16, 520, 520)])
+def test_weight_gradient_shapes(sizes, M, K):
+    """256 x 256 and 128 x 128 tiles of the weights' gradient."""
+    check_all(sizes, 1, M, K, ways=("grad_w",))
+
+
+def test_more_tiles_than_one_list():
+    """Work past 64 tiles a workgroup, done in several lists."""
+    sizes = [(i * 5) % 4 for i in range(4096)]
+    check_all(sizes, 2, 1160, 8, ways=("fwd",))
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    N, S, M, K = 4096, 8192, 264, 520
+    offs = torch.arange(N + 1, device=DEV, dtype=torch.int32) * 2
+    dy = torch.randn((S, M), generator=gen, device=DEV).bfloat16()
+    x = torch.randn((S, K), generator=gen, device=DEV).bfloat16()
+    dw = ace.grouped_matmul_grad_w(dy, x, offs)
+    for i in range(0, N, 512):
+        a, b = dy[2 * i:2 * i + 1024].double().view(512, 2, M, 1), x[2 * i:2 * i + 1024].double().view(512, 2, 1, K)
+        want, mag = (a * b).sum(1), (a * b).abs().sum(1)
+        # two products and a sum, then one rounding
+        tol = ref.HALF[torch.bfloat16] * want.abs() + 1.01 * 3 * 2 * ref.F32 * mag
+        assert bool(((dw[i:i + 512].double() - want).abs() <= tol).all()), i
