@@ -223,11 +223,16 @@ template <class Op, int D, bool IS_A> struct Feed {
   }
 };
 
-// 16 bytes of a result, which nothing here reads again: with the non-temporal hint, so it takes
-// no cache from the operands (the weights' gradient of 128 groups of 768 x 2048 and 128 rows: 136 -> 114 us)
-__device__ __forceinline__ void put16(void *p, uint4 v) {
+// 16 bytes of a result.  Nothing here reads it again, so where rows are whole 128-byte lines it goes with the
+// non-temporal hint and takes no cache from the operands (the weights' gradient of 128 groups of 768 x 2048
+// and 128 rows: 136 -> 114 us).  Where a line is shared by two rows, the caches have to put it together
+// (34 groups of 3712 x 1288 with 58 rows: 190 us with the hint).
+template <bool LINES> __device__ __forceinline__ void put16(void *p, uint4 v) {
   typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
-  __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), reinterpret_cast<u32x4_t *>(p));
+  if constexpr (LINES)
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), reinterpret_cast<u32x4_t *>(p));
+  else
+    *reinterpret_cast<uint4 *>(p) = v;
 }
 
 // lane r of 16 <-> lane r ^ 8
@@ -239,7 +244,7 @@ __device__ __forceinline__ uint32_t swap8(uint32_t v) {
 // lane % 16 of each block.  bf16: 8 consecutive columns from each pair of column blocks, so two pairs are
 // 128 bytes of a row over 4 lanes each; lanes r and r + 8 exchange one of them, and a store writes whole
 // lines of 8 rows in place of half lines of 16.
-template <typename T, int MW, int NW, int WR>
+template <typename T, bool LINES, int MW, int NW, int WR>
 __device__ __forceinline__ void store_rows(const TileRef<T> &t, size_t ldo, const f32x4_t (&acc)[MW][NW], int wr,
                                            int c0, int lane) {
   const int r16 = lane & 15, g = lane >> 4;
@@ -271,12 +276,12 @@ __device__ __forceinline__ void store_rows(const TileRef<T> &t, size_t ldo, cons
             second[d] = lower ? got : p[1][d];
           }
           if (col + 16 * j >= t.cols) continue;
-          if (row < t.rows) put16(o + 16 * j, uint4{first[0], first[1], first[2], first[3]});
-          if (row + 8 < t.rows) put16(o + 16 * j + 8 * ldo, uint4{second[0], second[1], second[2], second[3]});
+          if (row < t.rows) put16<LINES>(o + 16 * j, uint4{first[0], first[1], first[2], first[3]});
+          if (row + 8 < t.rows) put16<LINES>(o + 16 * j + 8 * ldo, uint4{second[0], second[1], second[2], second[3]});
         } else {  // a pair left over: half lines
           const int own = 16 * (wr + WR * i) + r16, at = c0 + 8 * g + 16 * j;
           if (own < t.rows && at < t.cols)
-            put16(t.out + static_cast<size_t>(own) * ldo + at, uint4{p[0][0], p[0][1], p[0][2], p[0][3]});
+            put16<LINES>(t.out + static_cast<size_t>(own) * ldo + at, uint4{p[0][0], p[0][1], p[0][2], p[0][3]});
         }
       }
     }
@@ -289,7 +294,7 @@ __device__ __forceinline__ void store_rows(const TileRef<T> &t, size_t ldo, cons
 #pragma unroll
       for (int j = 0; j < NW; ++j) {
         const int col = c0 + 16 * j + 4 * g;
-        if (col < t.cols) put16(o + col, __builtin_bit_cast(uint4, acc[i][j]));
+        if (col < t.cols) put16<LINES>(o + col, __builtin_bit_cast(uint4, acc[i][j]));
       }
     }
   }
@@ -318,7 +323,7 @@ __device__ __forceinline__ void store_part(const TileRef<T> &t, size_t ldo, cons
 // and DB LDS slots, and across the end of a tile, so the next tile's first stages are under way
 // while a tile ends and stores.  A tile is MB x NB 16-blocks, WR x WC waves.  ref(item) gives a
 // tile's operands; lda, ldb, ldo are common.
-template <typename T, bool ADOWN, bool BDOWN, int MB, int NB, int WR, int WC, int DA, int DB, typename F>
+template <typename T, bool ADOWN, bool BDOWN, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB, typename F>
 __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, int ldb, size_t ldo, uint8_t *smem,
                                               F ref) {
   constexpr int W = WR * WC, MW = MB / WR, NW = NB / WC;
@@ -431,7 +436,7 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
     if (t.part)
       store_part<T, MW, NW, WR>(t, ldo, sum, wr, 16 * wc * NW, lane);
     else
-      store_rows<T, MW, NW, WR>(t, ldo, sum, wr, 16 * wc * NW, lane);
+      store_rows<T, LINES, MW, NW, WR>(t, ldo, sum, wr, 16 * wc * NW, lane);
   }
 }
 
@@ -471,7 +476,7 @@ template <typename T> __device__ __forceinline__ Part part_of(int klen, int s, i
 }
 
 // Tiles of x's or dy's rows by columns, the whole work of a workgroup
-template <typename T, bool GX, int MB, int NB, int WR, int WC, int DA, int DB>
+template <typename T, bool GX, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
 __device__ __forceinline__ void grouped_rows(const GroupedArgs &g, const RaggedTiles &tiles, uint8_t *smem) {
   constexpr int BN = 16 * NB;
   const int cols = GX ? g.K : g.M, klen = GX ? g.M : g.K;
@@ -499,23 +504,23 @@ __device__ __forceinline__ void grouped_rows(const GroupedArgs &g, const RaggedT
     const RaggedTile t = tiles.find(static_cast<int>(i / per));
     const int q = static_cast<int>(i % per);
     __syncthreads();  // every wave is done with the rings
-    grouped_items<T, false, GX, MB, NB, WR, WC, DA, DB>(
+    grouped_items<T, false, GX, LINES, MB, NB, WR, WC, DA, DB>(
         Item{t.group, t.row0, t.rows, q % nN, t.only, q / nN}, n, klen, g.K, cols, smem, ref);
   }
 }
 
 // Forward (GX = false) and rows' gradient (GX = true) in tiles of 16 MB rows of one group x 16 NB columns
-template <typename T, bool GX, int MB, int NB, int WR, int WC, int DA, int DB>
+template <typename T, bool GX, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
 __global__ __launch_bounds__(WR *WC * 64) void grouped_rows_kernel(GroupedArgs g) {
   __shared__ __align__(16) uint8_t smem[(DA * MB + DB * NB) * 2 * kUnitBytes];
   const RaggedTiles tiles(g.offsets, g.N, g.S, 16 * MB, g.fill);
-  grouped_rows<T, GX, MB, NB, WR, WC, DA, DB>(g, tiles, smem);
+  grouped_rows<T, GX, LINES, MB, NB, WR, WC, DA, DB>(g, tiles, smem);
 }
 
 // The same with the tile shape taken here, from the groups' sizes that only the device knows: a
 // group's last row tile costs about a full one, so which height wastes least goes by them.
 // Rounds of a CU times the time of a stage, in units of 50 ns as measured with every CU busy.
-template <bool GX> __global__ __launch_bounds__(512) void grouped_shapes_kernel(GroupedArgs g) {
+template <bool GX, bool LINES> __global__ __launch_bounds__(512) void grouped_shapes_kernel(GroupedArgs g) {
   __shared__ __align__(16) uint8_t smem[160 * 1024];
   const int cols = GX ? g.K : g.M;
   const int heights[3] = {192, 256, 320};
@@ -529,17 +534,17 @@ template <bool GX> __global__ __launch_bounds__(512) void grouped_shapes_kernel(
   const long long c192 = cost(0, 192, 28), c192w = cost(0, 256, 35), c256 = cost(1, 256, 42), c320 = cost(2, 192, 41);
   const long long best = min(min(c192, c192w), min(c256, c320));
   if (best == c256)
-    grouped_rows<bf16_t, GX, 16, 16, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 256, g.fill), smem);
+    grouped_rows<bf16_t, GX, LINES, 16, 16, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 256, g.fill), smem);
   else if (best == c320)
-    grouped_rows<bf16_t, GX, 20, 12, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 320, g.fill), smem);
+    grouped_rows<bf16_t, GX, LINES, 20, 12, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 320, g.fill), smem);
   else if (best == c192)
-    grouped_rows<bf16_t, GX, 12, 12, 4, 2, 3, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 192, g.fill), smem);
+    grouped_rows<bf16_t, GX, LINES, 12, 12, 4, 2, 3, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 192, g.fill), smem);
   else
-    grouped_rows<bf16_t, GX, 12, 16, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 192, g.fill), smem);
+    grouped_rows<bf16_t, GX, LINES, 12, 16, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 192, g.fill), smem);
 }
 
 // Weights' gradient: tile = 16 MB rows x 16 NB columns of one group's dw
-template <typename T, int MB, int NB, int WR, int WC, int DA, int DB>
+template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
 __global__ __launch_bounds__(WR *WC * 64) void grouped_weights_kernel(GroupedArgs g) {
   constexpr int BM = 16 * MB, BN = 16 * NB;
   __shared__ __align__(16) uint8_t smem[(DA * MB + DB * NB) * 2 * kUnitBytes];
@@ -569,7 +574,7 @@ __global__ __launch_bounds__(WR *WC * 64) void grouped_weights_kernel(GroupedArg
     const int e = static_cast<int>(i / per), q = static_cast<int>(i % per);
     const int r0 = min(max(g.offsets[e], 0), g.S), r1 = min(max(g.offsets[e + 1], r0), g.S);
     __syncthreads();  // every wave is done with the rings
-    grouped_items<T, true, true, MB, NB, WR, WC, DA, DB>(Item{e, r0, r1 - r0, q % one, 0, q / one}, n, g.M, g.K, g.K,
+    grouped_items<T, true, true, LINES, MB, NB, WR, WC, DA, DB>(Item{e, r0, r1 - r0, q % one, 0, q / one}, n, g.M, g.K, g.K,
                                                           smem, ref);
   }
 }
@@ -701,16 +706,27 @@ unsigned grouped_grid(long long items, int per_cu) {
   return static_cast<unsigned>(std::min<long long>((items + 7) / 8 * 8, kCUs * per_cu));
 }
 
+// whether every row of the result is whole 128-byte lines (see put16)
+bool whole_lines(const GroupedArgs &g, int cols, int es) {
+  return cols * es % 128 == 0 && reinterpret_cast<uintptr_t>(g.out) % 128 == 0;
+}
+
 template <typename T, bool GX, class Sh> void launch_rows_shape(const GroupedArgs &g, int cols, hipStream_t s) {
   const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(cols, Sh::TN) * g.splits;
-  grouped_rows_kernel<T, GX, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>
-      <<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g);
+  auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g); };
+  if (whole_lines(g, cols, sizeof(T)))
+    launch(grouped_rows_kernel<T, GX, true, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+  else
+    launch(grouped_rows_kernel<T, GX, false, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
 }
 
 template <typename T, class Sh> void launch_weights_shape(const GroupedArgs &g, hipStream_t s) {
   const long long items = g.N * tiles_of(g.M, Sh::TM) * tiles_of(g.K, Sh::TN) * g.splits;
-  grouped_weights_kernel<T, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>
-      <<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g);
+  auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g); };
+  if (whole_lines(g, g.K, sizeof(T)))
+    launch(grouped_weights_kernel<T, true, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+  else
+    launch(grouped_weights_kernel<T, false, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
 }
 
 hipError_t launch_join(const GroupedArgs &g, size_t total, int cols, bool bf16, hipStream_t s) {
@@ -731,7 +747,12 @@ template <bool GX> hipError_t launch_rows(GroupedArgs g, bool bf16, hipStream_t 
     case Kind::k64: launch_rows_shape<bf16_t, GX, Tile64>(g, cols, s); break;
     case Kind::k64x128: launch_rows_shape<bf16_t, GX, Tile64x128>(g, cols, s); break;
     case Kind::k128: launch_rows_shape<bf16_t, GX, Tile128>(g, cols, s); break;
-    case Kind::kLarge: grouped_shapes_kernel<GX><<<kCUs, 512, 0, s>>>(g); break;
+    case Kind::kLarge:
+      if (whole_lines(g, cols, 2))
+        grouped_shapes_kernel<GX, true><<<kCUs, 512, 0, s>>>(g);
+      else
+        grouped_shapes_kernel<GX, false><<<kCUs, 512, 0, s>>>(g);
+      break;
     case Kind::kF32: launch_rows_shape<float, GX, TileF32>(g, cols, s); break;
   }
   const hipError_t e = hipGetLastError();
