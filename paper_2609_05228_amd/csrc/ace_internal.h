@@ -225,7 +225,8 @@ struct GroupedArgs {
   const int32_t *offsets;  // [N + 1]
   int S, N, M, K;
   int fill;
-  int splits;   // parts of the reduction, and their fp32 sums [splits, out's elements]
+  int splits;   // parts of the reduction, and their fp32 sums [splits, out's elements] (a group's, for the weights)
+  int chunk;    // weights' gradient: most rows of a part
   float *part;  // grouped_workspace_bytes
 };
 size_t grouped_workspace_bytes(const GroupedArgs &g, bool weights, bool grad, bool bf16);

@@ -180,7 +180,7 @@ struct Item {
   int row0, rows;  // rows of x / dy: the tile's rows, or (weights' gradient) the group's
   int tile;        // column tile, or (weights' gradient) tile of the group's matrix
   int once;        // no other row tile of the group
-  int split;       // part of the reduction
+  int split;       // part of the reduction (weights' gradient: slot of the partial sums, -1: none)
 };
 constexpr int kFlush = 4;  // stages of an fp32 partial sum
 constexpr int kItems = 64;  // of one list, one in each lane: longer work is done in several
@@ -548,22 +548,20 @@ template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB
 __global__ __launch_bounds__(WR *WC * 64) void grouped_weights_kernel(GroupedArgs g) {
   constexpr int BM = 16 * MB, BN = 16 * NB;
   __shared__ __align__(16) uint8_t smem[(DA * MB + DB * NB) * 2 * kUnitBytes];
-  const int nM = (g.M + BM - 1) / BM, nN = (g.K + BN - 1) / BN, one = nM * nN, per = one * g.splits;
-  const Share share(static_cast<long long>(g.N) * per);
+  const int nM = (g.M + BM - 1) / BM, nN = (g.K + BN - 1) / BN, per = nM * nN;
+  const RaggedTiles tiles(g.offsets, g.N, g.S, g.chunk, false, true);
+  const Share share(static_cast<long long>(tiles.total) * per);
   auto ref = [&](const Item &it) {
     const int m0 = it.tile / nN * BM, c0 = it.tile % nN * BN;
-    const Part k = part_of<T>(it.rows, it.split, g.splits);
-    const size_t row = static_cast<size_t>(it.row0) + k.k0;
+    const size_t at = static_cast<size_t>(m0) * g.K + c0, size = static_cast<size_t>(g.M) * g.K;
     TileRef<T> t;
-    t.a = static_cast<const T *>(g.rows) + row * g.M + m0;
-    t.b = static_cast<const T *>(g.other) + row * g.K + c0;
-    t.out = static_cast<T *>(g.out) + (static_cast<size_t>(it.group) * g.M + m0) * g.K + c0;
-    t.part = g.splits > 1
-                 ? g.part + ((static_cast<size_t>(it.split) * g.N + it.group) * g.M + m0) * g.K + c0
-                 : nullptr;
+    t.a = static_cast<const T *>(g.rows) + static_cast<size_t>(it.row0) * g.M + m0;
+    t.b = static_cast<const T *>(g.other) + static_cast<size_t>(it.row0) * g.K + c0;
+    t.out = static_cast<T *>(g.out) + static_cast<size_t>(it.group) * size + at;
+    t.part = it.split >= 0 ? g.part + static_cast<size_t>(it.split) * size + at : nullptr;
     t.rows = min(BM, g.M - m0);
     t.cols = min(BN, g.K - c0);
-    t.klen = k.len;
+    t.klen = it.rows;
     t.rot = 0;
     t.once = false;
     return t;
@@ -571,24 +569,72 @@ __global__ __launch_bounds__(WR *WC * 64) void grouped_weights_kernel(GroupedArg
   long long done = 0;
   for (int n; (n = share.count(done)) > 0; done += n) {
     const long long i = share.item(done);
-    const int e = static_cast<int>(i / per), q = static_cast<int>(i % per);
-    const int r0 = min(max(g.offsets[e], 0), g.S), r1 = min(max(g.offsets[e + 1], r0), g.S);
+    const RaggedTile t = tiles.find(static_cast<int>(i / per));
+    // offsets that do not ascend can make more parts than there is room for: those go to the last
+    const int slot = t.only ? -1 : min(t.slot, g.splits - 1);
     __syncthreads();  // every wave is done with the rings
-    grouped_items<T, true, true, LINES, MB, NB, WR, WC, DA, DB>(Item{e, r0, r1 - r0, q % one, 0, q / one}, n, g.M, g.K, g.K,
-                                                          smem, ref);
+    grouped_items<T, true, true, LINES, MB, NB, WR, WC, DA, DB>(
+        Item{max(t.group, 0), t.row0, t.rows, static_cast<int>(i % per), 0, slot}, n, g.M, g.K, g.K, smem, ref);
   }
 }
 
-// out = the parts' sum in order, for the elements first .. last of `total` (16 bytes of out a thread);
-// the others get zeros with `fill`, or stay.  Rows (weights' gradient: all): first and last by the offsets.
+// dw of the groups of more than `chunk` rows: their parts' sum in order, 16 bytes of dw a thread.  Workgroups
+// (x, y): the y-th such group, if there is one.
+template <typename T> __global__ __launch_bounds__(256) void grouped_weights_join_kernel(GroupedArgs g) {
+  constexpr int E = kChunkElems<T>;
+  const int lane = threadIdx.x & 63;
+  int nth = static_cast<int>(blockIdx.y), slot = 0, group = -1, parts = 0;
+  for (int e0 = 0; e0 < g.N && group < 0; e0 += 64) {
+    const int e = e0 + lane;
+    int n = 0;
+    if (e < g.N) {
+      const int lo = min(max(g.offsets[e], 0), g.S), hi = min(max(g.offsets[e + 1], 0), g.S);
+      if (hi > lo) n = static_cast<int>((static_cast<uint32_t>(hi - lo) + g.chunk - 1u) / static_cast<uint32_t>(g.chunk));
+    }
+    unsigned long long many = __ballot(n > 1);
+    while (many) {  // wave-uniform
+      const int l = __ffsll(static_cast<long long>(many)) - 1, m = __builtin_amdgcn_readlane(n, l);
+      if (nth-- == 0) {
+        group = e0 + l;
+        parts = m;
+        break;
+      }
+      slot += m;
+      many &= many - 1;
+    }
+  }
+  if (group < 0) return;
+  const size_t size = static_cast<size_t>(g.M) * g.K;
+  for (size_t i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * E; i < size;
+       i += static_cast<size_t>(gridDim.x) * 256 * E) {
+    float v[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[j] = 0.f;
+    for (int s = 0; s < parts; ++s) {
+      const float *p = g.part + min(slot + s, g.splits - 1) * size + i;
+#pragma unroll
+      for (int j = 0; j < E; j += 4) {
+        const f32x4_t u = *reinterpret_cast<const f32x4_t *>(p + j);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[j + k] += u[k];
+      }
+    }
+    T *o = static_cast<T *>(g.out) + static_cast<size_t>(group) * size + i;
+    if constexpr (E == 8)
+      *reinterpret_cast<uint4 *>(o) =
+          uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    else
+      *reinterpret_cast<f32x4_t *>(o) = f32x4_t{v[0], v[1], v[2], v[3]};
+  }
+}
+
+// out = the parts' sum in order, for the rows of the groups (16 bytes of out a thread); the others get zeros
+// with `fill`, or stay
 template <typename T> __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedArgs g, size_t total, int cols) {
   constexpr int E = kChunkElems<T>;
-  size_t first = 0, last = total;
-  if (cols > 0) {
-    const int r0 = min(max(g.offsets[0], 0), g.S);
-    first = static_cast<size_t>(r0) * cols;
-    last = static_cast<size_t>(min(max(g.offsets[g.N], r0), g.S)) * cols;
-  }
+  const int r0 = min(max(g.offsets[0], 0), g.S);
+  const size_t first = static_cast<size_t>(r0) * cols;
+  const size_t last = static_cast<size_t>(min(max(g.offsets[g.N], r0), g.S)) * cols;
   for (size_t i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * E; i < total;
        i += static_cast<size_t>(gridDim.x) * 256 * E) {
     float v[E];
@@ -636,8 +682,9 @@ enum class Kind { k64, k64x128, k128, kLarge, kF32 };
 
 struct Plan {
   Kind kind;
-  int splits;         // parts of the reduction
+  int splits;         // parts of the reduction (weights' gradient: room for so many parts of groups)
   size_t part_elems;  // of one part
+  int chunk;          // weights' gradient: most rows of a part
 };
 
 long long tiles_of(long long n, int t) { return (n + t - 1) / t; }
@@ -689,16 +736,48 @@ Plan plan_rows(const GroupedArgs &g, bool grad, bool bf16) {
 }
 
 // ... and for the weights' gradient.  128 groups of 768 x 2048 and 128 rows: 256 x 256 tiles 114 us, 128 x 128 134.
+// A group of more than p.chunk rows is summed in parts of at most that many, which a second launch adds: a few
+// long groups would otherwise be a few workgroups' work.  Parts are four times the mean group (2048 rows at least),
+// so that their sums take no more room than dw itself (bf16); or fewer rows where all tiles together
+// would leave CUs idle, as far as the time of their stages pays for the launch and the traffic (us; 74 groups of
+// 464 x 256, the largest a quarter of 39997 rows: 122 whole, see DESIGN for the present figure).
 Plan plan_weights(const GroupedArgs &g, bool bf16) {
-  const size_t elems = static_cast<size_t>(g.N) * g.M * g.K;
-  const long long rows = (static_cast<long long>(g.S) + g.N - 1) / g.N;
-  auto items = [&](int t) { return g.N * tiles_of(g.M, t) * tiles_of(g.K, t); };
-  if (!bf16)
-    return {Kind::kF32, pick_splits(items(64), kCUs * TileF32Weights::PER_CU, tiles_of(rows, 32), elems, 0.6), elems};
-  if (items(64) <= kCUs * Tile64::PER_CU)
-    return {Kind::k64, pick_splits(items(64), kCUs * Tile64::PER_CU, tiles_of(rows, 64), elems, 0.45), elems};
-  if (items(256) >= kCUs) return {Kind::kLarge, 1, elems};
-  return {Kind::k128, pick_splits(items(128), kCUs * Tile128::PER_CU, tiles_of(rows, 64), elems, 1.2), elems};
+  const size_t elems = static_cast<size_t>(g.M) * g.K;
+  const long long mean = (static_cast<long long>(g.S) + g.N - 1) / g.N;
+  auto tiles = [&](int t) { return tiles_of(g.M, t) * tiles_of(g.K, t); };
+  Plan p{Kind::kF32, 0, elems};
+  long long one = tiles(64), slots = kCUs * TileF32Weights::PER_CU;
+  double stage = 1.2;  // of 64 rows, us
+  if (bf16) {
+    if (g.N * tiles(64) <= kCUs * Tile64::PER_CU) {
+      p.kind = Kind::k64;
+      slots = kCUs * Tile64::PER_CU;
+      stage = 0.45;
+    } else if (g.N * tiles(256) >= kCUs) {
+      p.kind = Kind::kLarge;
+      one = tiles(256);
+      slots = kCUs;
+      stage = 2.1;
+    } else {
+      p.kind = Kind::k128;
+      one = tiles(128);
+      slots = kCUs * Tile128::PER_CU;
+    }
+  }
+  long long chunk = std::max(4 * mean, 2048ll);
+  if (g.N * one < slots) {
+    double least = static_cast<double>(mean) / 64 * stage;
+    for (long long c = mean / 2; c >= 128 && tiles_of(g.S, static_cast<int>(c)) * one <= slots; c /= 2) {
+      const double t = static_cast<double>(c) / 64 * stage + 4.5 + 2e-6 * (g.S / c) * static_cast<double>(elems);
+      if (t < least) {
+        least = t;
+        chunk = c;
+      }
+    }
+  }
+  p.chunk = static_cast<int>(std::min<long long>((chunk + 63) / 64 * 64, 1 << 30));
+  p.splits = g.S <= p.chunk ? 0 : static_cast<int>(2ll * g.S / p.chunk);
+  return p;
 }
 
 // Workgroups of a launch: whole rounds of the XCDs, per_cu of them on every CU
@@ -721,7 +800,7 @@ template <typename T, bool GX, class Sh> void launch_rows_shape(const GroupedArg
 }
 
 template <typename T, class Sh> void launch_weights_shape(const GroupedArgs &g, hipStream_t s) {
-  const long long items = g.N * tiles_of(g.M, Sh::TM) * tiles_of(g.K, Sh::TN) * g.splits;
+  const long long items = (g.N + g.splits) * tiles_of(g.M, Sh::TM) * tiles_of(g.K, Sh::TN);
   auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g); };
   if (whole_lines(g, g.K, sizeof(T)))
     launch(grouped_weights_kernel<T, true, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
@@ -777,7 +856,7 @@ hipError_t launch_grouped_weights(const GroupedArgs &args, bool bf16, hipStream_
   GroupedArgs g = args;
   const Plan p = plan_weights(g, bf16);
   g.splits = p.splits;
-  g.fill = 1;
+  g.chunk = p.chunk;
   switch (p.kind) {
     case Kind::k64: launch_weights_shape<bf16_t, Tile64>(g, stream); break;
     case Kind::kLarge: launch_weights_shape<bf16_t, Tile256>(g, stream); break;
@@ -785,8 +864,15 @@ hipError_t launch_grouped_weights(const GroupedArgs &args, bool bf16, hipStream_
     default: launch_weights_shape<bf16_t, Tile128>(g, stream); break;
   }
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
-  return launch_join(g, p.part_elems, 0, bf16, stream);
+  if (e != hipSuccess || p.splits == 0) return e;
+  // at most S / chunk groups have more rows than that
+  const size_t blocks = (p.part_elems / (bf16 ? 8 : 4) + 255) / 256;
+  const dim3 grid(static_cast<unsigned>(std::min<size_t>(blocks, 64)), static_cast<unsigned>(std::min(g.N, g.S / g.chunk)));
+  if (bf16)
+    grouped_weights_join_kernel<bf16_t><<<grid, 256, 0, stream>>>(g);
+  else
+    grouped_weights_join_kernel<float><<<grid, 256, 0, stream>>>(g);
+  return hipGetLastError();
 }
 
 }  // namespace ace

@@ -13,6 +13,7 @@ struct RaggedTile {
   int row0, rows;
   bool valid;
   bool only;  // the group's only tile
+  int slot;   // of a tile that is not: its number among those
 };
 
 // Tiles of S rows in N groups and the two gaps around them: a group of r rows has at most
@@ -23,40 +24,49 @@ inline long long ragged_max_tiles(long long S, long long N, int tm) {
 
 // The tiles of all groups in group order, held by one wave (all 64 lanes take part in every
 // call).  The gaps come as groups of their own before the first and behind the last when
-// `gaps` is set.  Offsets are clamped to 0 .. S, so whatever they hold, rows outside the
+// `gaps` is set; with `each`, a group without rows has one tile of none.  Offsets are clamped to 0 .. S, so whatever they hold, rows outside the
 // array are never named.  Lane l counts the tiles of `per` consecutive groups, one wave
 // scan places them: one round of loads and one scan, against a launch of its own for a tile
 // list.
 struct RaggedTiles {
   const int32_t *offsets;
   int N, S, tm, per, cnt, inc, total;
-  bool gaps;
+  int shared, shared_inc;  // tiles of groups of more than one, counted alike
+  bool gaps, each;
 
   // boundary i of the N + 2 groups: 0, offsets[0], .., offsets[N], S
   __device__ __forceinline__ int bound(int i) const {
     return i <= 0 ? 0 : i > N + 1 ? S : min(max(offsets[i - 1], 0), S);
   }
   __device__ __forceinline__ int tiles(int p, int lo, int hi) const {
-    if (p > N + 1 || hi <= lo || ((p == 0 || p == N + 1) && !gaps)) return 0;
+    if (p > N + 1 || ((p == 0 || p == N + 1) && !gaps)) return 0;
+    if (hi <= lo) return each && p > 0 && p <= N;
     return static_cast<int>((static_cast<uint32_t>(hi - lo) + tm - 1u) / static_cast<uint32_t>(tm));
   }
 
-  __device__ __forceinline__ RaggedTiles(const int32_t *offsets_, int N_, int S_, int tm_, bool gaps_)
-      : offsets(offsets_), N(N_), S(S_), tm(tm_), per((N_ + 2 + 63) >> 6), cnt(0), gaps(gaps_) {
+  __device__ __forceinline__ RaggedTiles(const int32_t *offsets_, int N_, int S_, int tm_, bool gaps_,
+                                         bool each_ = false)
+      : offsets(offsets_), N(N_), S(S_), tm(tm_), per((N_ + 2 + 63) >> 6), cnt(0), shared(0), gaps(gaps_), each(each_) {
     const int lane = threadIdx.x & 63;
     const int p0 = lane * per;
     int lo = bound(p0);
 #pragma unroll 4  // the loads of four groups in flight together, here and below
     for (int j = 0; j < per; ++j) {
       const int hi = bound(p0 + j + 1);
-      cnt += tiles(p0 + j, lo, hi);
+      const int n = tiles(p0 + j, lo, hi);
+      cnt += n;
+      shared += n > 1 ? n : 0;
       lo = hi;
     }
     inc = cnt;
+    shared_inc = shared;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(inc, o);
-      if (lane >= o) inc += v;
+      const int v = __shfl_up(inc, o), w = __shfl_up(shared_inc, o);
+      if (lane >= o) {
+        inc += v;
+        shared_inc += w;
+      }
     }
     total = __builtin_amdgcn_readlane(inc, 63);
   }
@@ -84,13 +94,13 @@ struct RaggedTiles {
 
   // tile `tile`, each lane its own
   __device__ __forceinline__ RaggedTile find(int tile) const {
-    RaggedTile t{-1, 0, 0, false, false};
+    RaggedTile t{-1, 0, 0, false, false, 0};
     // the lane that counts the tile: the first whose inclusive sum exceeds it
     int src = 0;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
       if (__shfl(inc, src + o - 1) <= tile) src += o;
-    int q = tile - __shfl(inc - cnt, src);
+    int q = tile - __shfl(inc - cnt, src), slot = __shfl(shared_inc - shared, src);
     if (tile < 0 || tile >= total) return t;
     const int p0 = src * per;
     int lo = bound(p0), from = 0, to = 0, n = 0;
@@ -105,6 +115,7 @@ struct RaggedTiles {
           n = m;
         } else {
           q -= m;
+          slot += m > 1 ? m : 0;
         }
       }
       lo = hi;
@@ -113,12 +124,13 @@ struct RaggedTiles {
     t.group = t.group == 0 || t.group == N + 1 ? -1 : t.group - 1;
     // the group's 16-row blocks spread evenly over its tiles: a short tile would stream the group's
     // operands for a few rows
-    const uint32_t blocks = (static_cast<uint32_t>(to - from) + 15u) >> 4, each = blocks / n, more = blocks % n;
+    const uint32_t blocks = (static_cast<uint32_t>(max(to - from, 0)) + 15u) >> 4, each = blocks / n, more = blocks % n;
     const uint32_t b0 = q * each + min(static_cast<uint32_t>(q), more);
     t.row0 = from + static_cast<int>(b0 << 4);
-    t.rows = min(static_cast<int>((each + (q < static_cast<int>(more))) << 4), to - t.row0);
+    t.rows = min(static_cast<int>((each + (q < static_cast<int>(more))) << 4), max(to - t.row0, 0));
     t.valid = true;
     t.only = n == 1;
+    t.slot = slot + q;
     return t;
   }
 

@@ -47,7 +47,8 @@ def test_grouped_workspace():
         for kw in (dict(ws=0), dict(ws=P[15] + 16), dict(ws_bytes=n - 1)):
             assert _grouped(fn, **few, **kw) == WSP, kw
         many = _lib.GroupedDesc(32768, 128, 768, 2048, _lib.ACE_BF16, 0)
-        assert size(many, way) == 0
+        # the weights' gradient keeps room for the parts of groups of eight times the mean
+        assert size(many, way) == 0 if way < 2 else 0 < size(many, way) <= 2 * 128 * 768 * 2048
         assert size(_lib.GroupedDesc(64, 0, 64, 64, _lib.ACE_BF16, 0), way) == 0
     assert size(many, 3) == 0 and size(many, -1) == 0
 
