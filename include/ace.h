@@ -278,7 +278,7 @@ ace_status ace_tau_map(const float *scores, int64_t n_rows, int32_t k, int32_t m
  *   ace_grouped_matmul_grad_w   dw[e] = sum over the rows r of e: dy[r] x[r]^T  (0 for an empty group)
  * Rows of no group (before offsets[0], from offsets[N] on) keep what y or dx holds, or get
  * zeros with ACE_ZERO_REST, and add nothing to dw.  Empty calls (S = 0) write nothing in the first
- * two.  Limits (else ACE_ERR_UNSUPPORTED): S < 2^31 - 1024, N <= 4096, M and K <= 65536.
+ * two.  Limits (else ACE_ERR_UNSUPPORTED): S < 2^31 - 2^16, N <= 4096, M and K <= 65536.
  *   workspace  DEVICE scratch of ace_grouped_workspace_size(desc, way) bytes, 256-byte aligned (may be NULL
  *              when that is 0): partial sums where few tiles leave a long reduction to split.
  */
@@ -317,7 +317,7 @@ ace_status ace_grouped_matmul_grad_w(const ace_grouped_desc *desc, const void *d
  * dh, dn, h and y itself.  Sums over rows (w_post, w_pre, a gate per channel) are added in a fixed
  * order; T = 0 gives zeros for them.
  *   workspace  DEVICE scratch of ace_block_norm_grad_workspace_size(desc) bytes, 256-byte aligned.
- * eps has to be positive.  Limit (else ACE_ERR_UNSUPPORTED): d <= 16384.
+ * eps has to be positive.  Limits (else ACE_ERR_UNSUPPORTED): T < 2^31 - 2^16, d <= 16384.
  */
 typedef enum {
   ACE_GATE_NONE = 0,
@@ -357,7 +357,7 @@ ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs 
  *   scale [L] fp32 or NULL (ones); offsets [R + 1] and adapter [R] int32 (adapter may be NULL when R = 0).
  *   workspace  DEVICE scratch of ace_adapter_workspace_size(desc) bytes, 256-byte aligned (may be NULL when
  *              that is 0: small batches).
- * An adapter of lower rank is padded with zero rows of a.  Limits (else ACE_ERR_UNSUPPORTED): S < 2^31 - 1024, R <= 4096,
+ * An adapter of lower rank is padded with zero rows of a.  Limits (else ACE_ERR_UNSUPPORTED): S < 2^31 - 2^16, R <= 4096,
  * rank <= 128, d_in and d_out <= 65536.
  */
 typedef struct {

@@ -53,7 +53,7 @@ template <typename T> __device__ __forceinline__ void store_vec(T *p, const floa
 template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_add(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, true));
 }
-// over N = 1, 2, 4, 8 or 16 neighbouring lanes, in each of them
+// over N <= 16 neighbouring lanes rounded up to a power of two, in each of them
 template <int N> __device__ __forceinline__ float lanes_sum(float v) {
   if constexpr (N > 1) v = dpp_add<0xb1, 0xf>(v);   // lanes 1 apart
   if constexpr (N > 2) v = dpp_add<0x4e, 0xf>(v);   // 2 apart
@@ -66,6 +66,13 @@ __device__ __forceinline__ float wave_sum(float v) {
   v = dpp_add<0x142, 0xa>(v);  // rows 1 and 3 add the row before
   v = dpp_add<0x143, 0xc>(v);  // rows 2 and 3 add row 1's: lane 63 holds all
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// of N waves' sums in LDS, in every lane
+template <int N> __device__ __forceinline__ float waves_sum(const float *sums) {
+  constexpr int P = N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : N <= 8 ? 8 : 16;
+  const int l = threadIdx.x % P;
+  return lanes_sum<N>(l < N ? sums[l] : 0.f);
 }
 
 // Sums over the workgroup, the same in every thread, in a fixed order.  Successive calls
@@ -83,7 +90,7 @@ template <int NT, int N> struct BlockSum {
         for (int i = 0; i < N; ++i) red[par][i][wave] = v[i];
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = lanes_sum<NT / 64>(red[par][i][threadIdx.x % (NT / 64)]);
+      for (int i = 0; i < N; ++i) v[i] = waves_sum<NT / 64>(red[par][i]);
       par ^= 1;
     }
   }
@@ -171,7 +178,7 @@ template <int NT, int RG, int N> struct RowSum {
         for (int i = 0; i < N; ++i) red[par][grp][i][wave] = v[i];
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = lanes_sum<NT / 64>(red[par][grp][i][threadIdx.x % (NT / 64)]);
+      for (int i = 0; i < N; ++i) v[i] = waves_sum<NT / 64>(red[par][grp][i]);
       par ^= 1;
     }
   }
@@ -404,30 +411,42 @@ constexpr int kGradBlocks = 256;  // a workgroup a CU
 
 // Threads of a gradient workgroup: 1024, or 512 where those would not fill the CUs once (bf16: 117 rows of 384
 // 10.8 us with 1024 and 8.4 with 512, 1574 rows of 200 11.6 and 9.8; 4096 rows of 2048 29 and 32, 10819 of 1296 63 and 77)
+// They come as whole rows' threads.
+constexpr int grad_small(int nt) { return nt >= 512 ? nt : 512 / nt * nt; }
+constexpr int grad_large(int nt) { return 1024 / nt * nt; }
 int grad_threads(int T, int nt) {
-  const int small = std::max(nt, 512);
-  return static_cast<long long>(T) <= static_cast<long long>(kGradBlocks) * (1024 / nt) ? small : 1024;
+  return static_cast<long long>(T) <= static_cast<long long>(kGradBlocks) * (1024 / nt) ? grad_small(nt) : grad_large(nt);
 }
 
 
-// the smallest workgroup whose threads hold a row of d in one access each, else 1024
-// threads with two or four
+// Threads of a row: the fewest of these that hold it in one access each, else 1024 with two or four.  Between the
+// powers of two as well: 15927 rows of 1088 (bf16) took the gradient 81 us with 256 threads, of which it uses 136.
+constexpr int kRowThreads[] = {64, 128, 192, 256, 320, 512, 640, 1024};
+int row_threads(int d, int vec) {
+  for (int nt : kRowThreads)
+    if (d <= nt * vec) return nt;
+  return 1024;
+}
+
 template <typename T, typename F> void by_width(int d, F f) {
   constexpr int V = kVec<T>;
-  if (d <= 64 * V)
-    f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-  else if (d <= 128 * V)
-    f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
-  else if (d <= 256 * V)
-    f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
-  else if (d <= 512 * V)
-    f(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{});
-  else if (d <= 1024 * V)
-    f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
-  else if (d <= 2048 * V)
-    f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
-  else if constexpr (V == 4)
-    f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
+  using std::integral_constant;
+  const integral_constant<int, 1> one{};
+  if (d > 2048 * V) {
+    if constexpr (V == 4) f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    return;
+  }
+  if (d > 1024 * V) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  switch (row_threads(d, V)) {
+    case 64: return f(integral_constant<int, 64>{}, one);
+    case 128: return f(integral_constant<int, 128>{}, one);
+    case 192: return f(integral_constant<int, 192>{}, one);
+    case 256: return f(integral_constant<int, 256>{}, one);
+    case 320: return f(integral_constant<int, 320>{}, one);
+    case 512: return f(integral_constant<int, 512>{}, one);
+    case 640: return f(integral_constant<int, 640>{}, one);
+    default: return f(integral_constant<int, 1024>{}, one);
+  }
 }
 
 template <typename T> void launch_fwd(const NormArgs &a, hipStream_t s) {
@@ -438,11 +457,11 @@ template <typename T> void launch_fwd(const NormArgs &a, hipStream_t s) {
 
 template <typename T> void launch_grad(const NormArgs &a, hipStream_t s) {
   by_width<T>(a.d, [&](auto nt, auto ch) {
-    constexpr int NT = nt(), SMALL = std::max(NT, 512);
+    constexpr int NT = nt(), SMALL = grad_small(NT), LARGE = grad_large(NT);
     if (grad_threads(a.T, NT) == SMALL)
       block_norm_grad_kernel<T, NT, ch(), SMALL / NT><<<a.blocks, SMALL, 0, s>>>(a);
     else
-      block_norm_grad_kernel<T, NT, ch(), 1024 / NT><<<a.blocks, 1024, 0, s>>>(a);
+      block_norm_grad_kernel<T, NT, ch(), LARGE / NT><<<a.blocks, LARGE, 0, s>>>(a);
   });
   const int n = (a.g_pre != nullptr) + (a.g_post != nullptr) + (a.gate_kind == 1);
   if (n > 0) param_sum_kernel<T><<<dim3((a.d + 63) / 64, n), 1024, 0, s>>>(a);
@@ -451,11 +470,9 @@ template <typename T> void launch_grad(const NormArgs &a, hipStream_t s) {
 }  // namespace
 
 int block_norm_grad_blocks(int T, int d, bool bf16) {
-  const int v = bf16 ? 8 : 4;
-  int nt = 64;
-  while (nt < 1024 && d > nt * v) nt *= 2;
+  const int nt = row_threads(d, bf16 ? 8 : 4);
   const int threads = grad_threads(T, nt), rows = threads / nt;  // of a workgroup at a time
-  return std::min((std::max(T, 1) - 1) / rows + 1, threads < 1024 ? 2 * kGradBlocks : kGradBlocks);
+  return std::min((std::max(T, 1) - 1) / rows + 1, threads <= 512 ? 2 * kGradBlocks : kGradBlocks);
 }
 
 hipError_t launch_block_norm(const NormArgs &a, bool bf16, hipStream_t stream) {

@@ -571,7 +571,7 @@ __global__ __launch_bounds__(WR *WC * 64) void grouped_weights_kernel(GroupedArg
     const long long i = share.item(done);
     const RaggedTile t = tiles.find(static_cast<int>(i / per));
     // offsets that do not ascend can make more parts than there is room for: those go to the last
-    const int slot = t.only ? -1 : min(t.slot, g.splits - 1);
+    const int slot = t.only ? -1 : min(max(t.slot, 0), g.splits - 1);
     __syncthreads();  // every wave is done with the rings
     grouped_items<T, true, true, LINES, MB, NB, WR, WC, DA, DB>(
         Item{max(t.group, 0), t.row0, t.rows, static_cast<int>(i % per), 0, slot}, n, g.M, g.K, g.K, smem, ref);
@@ -611,7 +611,7 @@ template <typename T> __global__ __launch_bounds__(256) void grouped_weights_joi
 #pragma unroll
     for (int j = 0; j < E; ++j) v[j] = 0.f;
     for (int s = 0; s < parts; ++s) {
-      const float *p = g.part + min(slot + s, g.splits - 1) * size + i;
+      const float *p = g.part + static_cast<size_t>(min(max(slot + s, 0), g.splits - 1)) * size + i;
 #pragma unroll
       for (int j = 0; j < E; j += 4) {
         const f32x4_t u = *reinterpret_cast<const f32x4_t *>(p + j);

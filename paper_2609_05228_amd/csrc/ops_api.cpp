@@ -15,7 +15,7 @@ constexpr int32_t kMaxGroups = 4096;  // groups of rows, requests
 constexpr int32_t kMaxWidth = 65536;  // feature sizes
 constexpr int32_t kMaxNormWidth = 16384;
 constexpr int32_t kMaxRank = 128;
-constexpr int32_t kMaxRows = 0x7fffffff - 1024;  // rounding up to a tile or stage stays an int
+constexpr int32_t kMaxRows = 0x7fffffff - 65536;  // rounding up to a tile, a stage or a grid's rows stays an int
 
 bool is_dtype(int32_t t) { return t == ACE_F32 || t == ACE_BF16; }
 size_t elem_bytes(int32_t t) { return t == ACE_BF16 ? 2 : 4; }
@@ -98,7 +98,7 @@ ace_status norm_desc(const ace_norm_desc *d) {
     return ACE_ERR_INVALID_ARG;
   if (!std::isfinite(d->res_scale) || !std::isfinite(d->branch_scale) || !std::isfinite(d->eps) || !(d->eps > 0.f))
     return ACE_ERR_INVALID_ARG;
-  if (d->d > kMaxNormWidth || bad_width(d->d, d->dtype)) return ACE_ERR_UNSUPPORTED;
+  if (d->T > kMaxRows || d->d > kMaxNormWidth || bad_width(d->d, d->dtype)) return ACE_ERR_UNSUPPORTED;
   return ACE_OK;
 }
 

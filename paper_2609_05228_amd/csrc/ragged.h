@@ -68,7 +68,8 @@ struct RaggedTiles {
         shared_inc += w;
       }
     }
-    total = __builtin_amdgcn_readlane(inc, 63);
+    // ascending offsets make no more than this; others could ask for thousands of passes over the array
+    total = min(__builtin_amdgcn_readlane(inc, 63), S / tm + N + 2);
   }
 
   // tiles[i]: how many tiles of heights[i] rows there are, without the list of any
@@ -101,7 +102,7 @@ struct RaggedTiles {
     for (int o = 32; o > 0; o >>= 1)
       if (__shfl(inc, src + o - 1) <= tile) src += o;
     int q = tile - __shfl(inc - cnt, src), slot = __shfl(shared_inc - shared, src);
-    if (tile < 0 || tile >= total) return t;
+    if (tile < 0 || tile >= total || q < 0) return t;
     const int p0 = src * per;
     int lo = bound(p0), from = 0, to = 0, n = 0;
 #pragma unroll 4

@@ -16,7 +16,7 @@ DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 # thread, 16 of a workgroup, 16 lines of a wave, 16 waves), and some 10 more form a result from them
 TERMS = 64
 
-SIZES = [(1, 8), (1, 2048), (3, 64), (7, 520), (5, 1032), (2, 4096), (3, 4104), (2, 8192), (2, 16384), (515, 264)]
+SIZES = [(1, 8), (1, 2048), (3, 64), (7, 520), (5, 1032), (2, 4096), (3, 4104), (2, 8192), (2, 16384), (515, 264), (9, 1288), (70, 2200), (5, 4888), (40, 648)]
 
 
 def make(T, d, dtype, gate="channel", post=True, pre=True, seed=0):
@@ -75,7 +75,7 @@ def test_forms(post, pre, gate, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,d", [(4200, 72), (1100, 1032), (530, 4104), (300, 8192)])
+@pytest.mark.parametrize("T,d", [(4200, 72), (1100, 1032), (530, 4104), (300, 8192), (1500, 1288), (800, 2320), (2700, 648)])
 def test_more_rows_than_one_round(T, d, dtype):
     """Workgroups that take several rows one after the other, the next ones copied ahead."""
     t, dh, dn = make(T, d, dtype)

@@ -128,6 +128,20 @@ def test_bad_offsets_stay_inside(offs):
         assert bool((buf[:pad] == 5).all()) and bool((buf[-pad:] == 5).all())
 
 
+def test_offsets_that_go_back_and_forth():
+    """4096 groups that each claim the whole array or nothing: no more work than the array is worth."""
+    S, N, M, K = 3000, 4096, 24, 16
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn((S, K), generator=gen, device=DEV).bfloat16()
+    w = torch.randn((N, M, K), generator=gen, device=DEV).bfloat16()
+    dy = torch.randn((S, M), generator=gen, device=DEV).bfloat16()
+    o = torch.tensor([0, S] * (N // 2) + [0], dtype=torch.int32, device=DEV)
+    assert ace.grouped_matmul(x, w, o).shape == (S, M)
+    assert ace.grouped_matmul_grad_x(dy, w, o).shape == (S, K)
+    assert ace.grouped_matmul_grad_w(dy, x, o).shape == (N, M, K)
+    torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_past_two_gib(dtype):
     """Rows whose byte offsets pass 2^32 (and element offsets 2^31): the last rows are right."""

@@ -81,7 +81,7 @@ def test_block_norm_refusals():
                dict(ho=P[0] + 16), dict(no=P[1] + 16), dict(ho=P[2]), dict(no=P[3]),
                dict(inp=dict(gate=P[4]), gate_kind=3, ho=P[4])):
         assert _norm(**kw) == BAD, kw
-    for kw in (dict(d=16392), dict(d=60), dict(d=6, dtype=_lib.ACE_F32)):
+    for kw in (dict(T=BIG, inp=dict(y=P[12]), ho=P[13], no=P[14]), dict(d=16392), dict(d=60), dict(d=6, dtype=_lib.ACE_F32)):
         assert _norm(**kw) == UNS, kw
     assert _norm(T=0, inp=dict(h=None, y=None), ho=None, no=None) == _lib.ACE_OK
 
