@@ -110,10 +110,11 @@ template <typename T> struct VFrag {
   }
 };
 
-// Rows of v in LDS, 16-byte quads: odd strides, so that 16 rows' reads go to different banks
-template <typename T, int KB> constexpr int kVStride = KB * kStepK<T> / 4 + 1;
+// Rows of v in LDS, 16-byte quads, zeros behind the rank: odd strides, so that 16 rows' reads go to different banks
+template <typename T, int KB> constexpr int kVQuads = KB * kStepK<T> / 4;
+template <typename T, int KB> constexpr int kVStride = kVQuads<T, KB> + 1;
 template <typename T, int KB>
-__device__ __forceinline__ void read_v(const f32x4_t *vs, int row, int r, VFrag<T> (&vf)[KB]) {
+__device__ __forceinline__ void read_v(const f32x4_t *vs, int row, VFrag<T> (&vf)[KB]) {
   constexpr int E = kChunkElems<T>;
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
@@ -122,7 +123,7 @@ __device__ __forceinline__ void read_v(const f32x4_t *vs, int row, int r, VFrag<
     float f[E];
 #pragma unroll
     for (int j = 0; j < E; j += 4) {
-      const f32x4_t u = k < r ? vs[row * kVStride<T, KB> + k / 4 + j / 4] : f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const f32x4_t u = vs[row * kVStride<T, KB> + k / 4 + j / 4];
 #pragma unroll
       for (int l = 0; l < 4; ++l) f[j + l] = u[l];
     }
@@ -157,7 +158,7 @@ template <typename T, int KB> struct Columns {
   static constexpr int PIECES = 4 / STEP;  // of 16 bytes of a row in a lane
   __device__ __forceinline__ int col(int i) const { return c0 + 16 * STEP * i + E * static_cast<int>((threadIdx.x & 63) >> 4); }
 
-  // base's 16 columns-pieces of a row
+  // a row of base, in pieces of 16 bytes
   __device__ __forceinline__ void base_of(const AdapterArgs &p, size_t row, bool there, uint4 (&v)[PIECES]) const {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i)
@@ -256,13 +257,13 @@ template <typename T, int RB> __global__ __launch_bounds__(256) void adapter_shr
 }
 
 // Tile = 64 rows x one of p.chunks shares of the columns, 64 of them a wave at a time: B_a's fragments
-// are read once for the four row blocks
+// are read once for the four row blocks.  Bound by the chain offsets -> adapter -> B_a -> products -> stores with
+// two waves a SIMD to hide it; so base and v are asked for before the adapter's number, and no load hangs on a
+// condition of its own (4096 rows, rank 64, 2048 columns: 15.6 us with such conditions, 13.8 without).
 template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_kernel(AdapterArgs p) {
   const int b = ragged_block();
   const RaggedTile t = RaggedTiles(p.offsets, p.R, p.S, kTileRows, p.out != p.base).find_uniform(b / p.chunks);
   if (!t.valid) return;
-  const int ad = tile_adapter(p, t);
-  if (ad < 0 && p.out == p.base) return;
   const int r16 = threadIdx.x & 15, wave = threadIdx.x >> 6;
   const Groups cols(p, b % p.chunks);
   using Cols = Columns<T, KB>;
@@ -271,7 +272,22 @@ template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) vo
   const int blocks = (t.rows + 15) >> 4;
   auto row_of = [&](int i) { return static_cast<size_t>(t.row0) + 16 * i + r16; };
   auto there = [&](int i) { return 16 * i + r16 < t.rows; };
+  // base's first rows and the first part of v are under way while the adapter's number is read
+  w.c0 = 64 * (cols.first + wave);
+  w.base_of(p, row_of(0), there(0), bv);
+  constexpr int VQ = kVQuads<T, KB>, VT = kTileRows * VQ / (64 * kExpandWaves);  // quads of a thread
+  static_assert(VT * 64 * kExpandWaves == kTileRows * VQ, "v of a tile in whole rounds");
+  const float *v[VT];
+  f32x4_t vsum[VT];
+#pragma unroll
+  for (int j = 0; j < VT; ++j) {
+    const int i = static_cast<int>(threadIdx.x) + j * 64 * kExpandWaves;
+    v[j] = p.v + (static_cast<size_t>(t.row0) + min(i / VQ, t.rows - 1)) * p.r + min(4 * (i % VQ), p.r - 4);
+    vsum[j] = *reinterpret_cast<const f32x4_t *>(v[j]);
+  }
+  const int ad = tile_adapter(p, t);
   if (ad < 0) {
+    if (p.out == p.base) return;
     for (int q = cols.first + wave; q < cols.last; q += kExpandWaves) {
       w.c0 = 64 * q;
       for (int i = 0; i < blocks; ++i) {
@@ -281,28 +297,17 @@ template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) vo
     }
     return;
   }
+  if (cols.first + wave < cols.last) w.load(p, ad, 64 * (cols.first + wave));
   // v of the tile's rows: the parts added in order, times the scale, once for all waves
   __shared__ f32x4_t vs[kTileRows * kVStride<T, KB>];
   const float sc = p.scale ? p.scale[ad] : 1.f;
-  const int quads = p.r >> 2;
-  for (int i = threadIdx.x; i < t.rows * quads; i += 64 * kExpandWaves) {
-    const int row = i / quads, q = i % quads;
-    const float *v = p.v + static_cast<size_t>(t.row0 + row) * p.r + 4 * q;
-    f32x4_t sum = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < p.splits; s0 += 4) {  // four loads in flight
-      f32x4_t u[4];
+  for (int s = 1; s < p.splits; ++s)
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        u[s] = *reinterpret_cast<const f32x4_t *>(v + static_cast<size_t>(min(s0 + s, p.splits - 1)) * p.S * p.r);
+    for (int j = 0; j < VT; ++j) vsum[j] += *reinterpret_cast<const f32x4_t *>(v[j] + static_cast<size_t>(s) * p.S * p.r);
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        if (s0 + s < p.splits) sum += u[s];
-    }
-    vs[row * kVStride<T, KB> + q] = sum * sc;
-  }
-  if (cols.first + wave < cols.last) {  // under way while the waves meet
-    w.load(p, ad, 64 * (cols.first + wave));
-    w.base_of(p, row_of(0), there(0), bv);
+  for (int j = 0; j < VT; ++j) {
+    const int i = static_cast<int>(threadIdx.x) + j * 64 * kExpandWaves, q = i % VQ;
+    vs[i / VQ * kVStride<T, KB> + q] = 4 * q < p.r ? vsum[j] * sc : f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
   __syncthreads();
   for (int q = cols.first + wave; q < cols.last; q += kExpandWaves) {
@@ -312,7 +317,7 @@ template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) vo
     }
     for (int i = 0; i < blocks; ++i) {
       VFrag<T> vf[KB];
-      read_v<T, KB>(vs, 16 * i + r16, p.r, vf);
+      read_v<T, KB>(vs, 16 * i + r16, vf);
       // the next block's rows of base are under way while this one's are finished
       if (i + 1 < blocks) w.base_of(p, row_of(i + 1), there(i + 1), next);
       w.finish(p, vf, row_of(i), there(i), bv);
@@ -366,11 +371,14 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
     f32x4_t s = red[0][c][lane];
 #pragma unroll
     for (int i = 1; i < kSmallWaves; ++i) s += red[i][c][lane];
-    if (4 * c + g < KB * kStepK<T> / 4) vs[r16 * kVStride<T, KB> + 4 * c + g] = s * sc;
+    const int q = 4 * c + g;
+    vs[r16 * kVStride<T, KB> + q] = 4 * q < p.r ? s * sc : f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
+  for (int i = threadIdx.x; i < kRowBlock * (kVQuads<T, KB> - 4 * RB); i += 64 * kSmallWaves)
+    vs[i % kRowBlock * kVStride<T, KB> + 4 * RB + i / kRowBlock] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   __syncthreads();
   VFrag<T> vf[KB];
-  read_v<T, KB>(vs, r16, p.r, vf);
+  read_v<T, KB>(vs, r16, vf);
   for (int q = g0 + wave; q < g1; q += kSmallWaves) {
     if (q != g0 + wave) {
       w.load(p, ad, 64 * q);
@@ -399,7 +407,7 @@ template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t 
   }
   const long long tiles = ragged_max_tiles(p.S, p.R, kTileRows);
   // column shares: eight workgroups a CU, where there are more tiles fewer, longer ones (1225 rows of 504 requests,
-  // 3280 columns: 57 us with a workgroup for every 256 columns)
+  // 3280 columns: 57 us with a workgroup for every 256 columns, 38 so)
   const long long most = (p.dout + 64 * kExpandWaves - 1) / (64 * kExpandWaves);
   p.chunks = static_cast<int>(std::min(most, (8 * kCUs + tiles - 1) / tiles));
   const long long shrink = tiles * p.splits, expand = tiles * p.chunks;

@@ -713,12 +713,14 @@ int pick_splits(long long items, int slots, long long nk, size_t elems, double s
 
 // Which kernel for the forward and the rows' gradient.  us on 128 groups of 768 x 2048 (forward):
 //   rows a group               2    16    48    96   128   256  1024
-//   64 x 128 (two a CU)       65    70    84   112   134   208   673
 //   128 x 128 (two a CU)      66    68    73    81   119   173   543
 //   large (best of its four)  64    71    74    82    94   140   478
 // and 16 groups of 1024 x 1024 with 1, 16, 128 and 512 rows: 64 x 64 12.8, 14.2, -, -; 128 x 128 15.2, 16.4, 20, 25;
-// large 17, 18, 23, 31.  So: the large shapes past 80 rows a group for work of at least a round of 128 x 128
-// tiles, 64 x 64 tiles while they are at most a round.
+// large 17, 18, 23, 31.  Few rows a group, where its weights' way from memory bounds all of them: 64 x 128 tiles with
+// deeper rings, 128 groups of 2048 x 768 with 2, 16, 32 rows 63, 70, 72.6 against 68, 71, 73.7 with 128 x 128;
+// with 48 rows of the table's 84 against 73.
+// So: 64 x 64 tiles while they are at most a round, 64 x 128 up to 32 rows a group, the large shapes past 80 for work
+// of at least a round of 128 x 128 tiles.
 Plan plan_rows(const GroupedArgs &g, bool grad, bool bf16) {
   const int cols = grad ? g.K : g.M, klen = grad ? g.M : g.K;
   const size_t elems = static_cast<size_t>(g.S) * cols;
@@ -740,7 +742,7 @@ Plan plan_rows(const GroupedArgs &g, bool grad, bool bf16) {
 // long groups would otherwise be a few workgroups' work.  Parts are four times the mean group (2048 rows at least),
 // so that their sums take no more room than dw itself (bf16); or fewer rows where all tiles together
 // would leave CUs idle, as far as the time of their stages pays for the launch and the traffic (us; 74 groups of
-// 464 x 256, the largest a quarter of 39997 rows: 122 whole, see DESIGN for the present figure).
+// 464 x 256, the largest a quarter of 39997 rows: 122 us whole, 54 in parts).
 Plan plan_weights(const GroupedArgs &g, bool bf16) {
   const size_t elems = static_cast<size_t>(g.M) * g.K;
   const long long mean = (static_cast<long long>(g.S) + g.N - 1) / g.N;

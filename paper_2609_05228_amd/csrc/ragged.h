@@ -32,6 +32,7 @@ struct RaggedTiles {
   const int32_t *offsets;
   int N, S, tm, per, cnt, inc, total;
   int shared, shared_inc;  // tiles of groups of more than one, counted alike
+  int first, last;         // boundaries of this lane's groups
   bool gaps, each;
 
   // boundary i of the N + 2 groups: 0, offsets[0], .., offsets[N], S
@@ -58,6 +59,8 @@ struct RaggedTiles {
       shared += n > 1 ? n : 0;
       lo = hi;
     }
+    first = bound(p0);
+    last = lo;
     inc = cnt;
     shared_inc = shared;
 #pragma unroll
@@ -104,9 +107,15 @@ struct RaggedTiles {
     int q = tile - __shfl(inc - cnt, src), slot = __shfl(shared_inc - shared, src);
     if (tile < 0 || tile >= total || q < 0) return t;
     const int p0 = src * per;
-    int lo = bound(p0), from = 0, to = 0, n = 0;
+    int from = __shfl(first, src), to = __shfl(last, src), n = 0;
+    if (per == 1) {  // the lane's only group, without another load
+      n = tiles(p0, from, to);
+      if (q >= n) return t;
+      t.group = p0;
+    }
+    int lo = from;
 #pragma unroll 4
-    for (int j = 0; j < per; ++j) {
+    for (int j = 0; per > 1 && j < per; ++j) {
       const int hi = bound(p0 + j + 1), m = tiles(p0 + j, lo, hi);
       if (n == 0) {  // not found yet
         if (q < m) {
