@@ -90,16 +90,21 @@ __device__ __forceinline__ void shrink(const AdapterArgs &p, const RaggedTile &t
   }
 }
 
-// A lane's E values of v as fragments: bf16 the value rounded and the rest of it, fp32 itself
+// A lane's E values of v as fragments: bf16 the value rounded and the rest of it (nothing where that is no
+// number: an infinite v stays one), fp32 itself
 template <typename T> struct VFrag {
   frag_of<T> hi, lo;
+  static __device__ __forceinline__ float rest(float f, uint32_t rounded) {
+    const float d = f - __uint_as_float(rounded);
+    return __builtin_isfinite(d) ? d : 0.f;
+  }
   __device__ __forceinline__ void set(const float *f) {
     if constexpr (sizeof(T) == 2) {
       uint32_t h[4], l[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         h[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
-        l[i] = pack_bf16x2(f[2 * i] - __uint_as_float(h[i] << 16), f[2 * i + 1] - __uint_as_float(h[i] & 0xffff0000u));
+        l[i] = pack_bf16x2(rest(f[2 * i], h[i] << 16), rest(f[2 * i + 1], h[i] & 0xffff0000u));
       }
       hi = __builtin_bit_cast(frag_of<T>, uint4{h[0], h[1], h[2], h[3]});
       lo = __builtin_bit_cast(frag_of<T>, uint4{l[0], l[1], l[2], l[3]});

@@ -418,7 +418,6 @@ int grad_threads(int T, int nt) {
   return static_cast<long long>(T) <= static_cast<long long>(kGradBlocks) * (1024 / nt) ? grad_small(nt) : grad_large(nt);
 }
 
-
 // Threads of a row: the fewest of these that hold it in one access each, else 1024 with two or four.  Between the
 // powers of two as well: 15927 rows of 1088 (bf16) took the gradient 81 us with 256 threads, of which it uses 136.
 constexpr int kRowThreads[] = {64, 128, 192, 256, 320, 512, 640, 1024};

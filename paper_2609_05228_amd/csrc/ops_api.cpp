@@ -134,6 +134,16 @@ size_t gate_bytes(const ace_norm_desc &d) {
   return es * (d.gate_kind == ACE_GATE_CHANNEL ? w : d.gate_kind == ACE_GATE_TOKEN ? T : d.gate_kind == ACE_GATE_FULL ? T * w : 0);
 }
 
+ace_status adapter_desc(const ace_adapter_desc *d) {
+  if (!d) return ACE_ERR_INVALID_ARG;
+  if (d->S < 0 || d->R < 0 || d->L <= 0 || d->rank <= 0 || d->d_in <= 0 || d->d_out <= 0 || !is_dtype(d->dtype))
+    return ACE_ERR_INVALID_ARG;
+  if (d->S > kMaxRows || d->R > kMaxGroups || d->rank > kMaxRank || d->d_in > kMaxWidth || d->d_out > kMaxWidth ||
+      bad_width(d->rank, d->dtype) || bad_width(d->d_in, d->dtype) || bad_width(d->d_out, d->dtype))
+    return ACE_ERR_UNSUPPORTED;
+  return ACE_OK;
+}
+
 // A result may lie exactly on an input of the same rows (each thread reads its elements of a
 // row before it writes them); any other overlap is refused.
 bool bad_alias(const Span &out, const Span &in, bool may_equal) {
@@ -190,7 +200,7 @@ ace_status ace_block_norm(const ace_norm_desc *desc, const ace_norm_inputs *in, 
 }
 
 size_t ace_block_norm_grad_workspace_size(const ace_norm_desc *desc) {
-  if (!desc || desc->T < 0 || desc->d <= 0) return 0;
+  if (norm_desc(desc) != ACE_OK) return 0;
   return static_cast<size_t>(ace::block_norm_grad_blocks(desc->T, desc->d, desc->dtype == ACE_BF16)) * desc->d * 3 * sizeof(float);
 }
 
@@ -239,7 +249,7 @@ ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs 
 }
 
 size_t ace_adapter_workspace_size(const ace_adapter_desc *desc) {
-  if (!desc || desc->S <= 0 || desc->R < 0 || desc->rank <= 0 || desc->d_in <= 0 || !is_dtype(desc->dtype)) return 0;
+  if (adapter_desc(desc) != ACE_OK || desc->S == 0) return 0;
   return static_cast<size_t>(ace::adapter_splits(desc->S, desc->R, desc->rank, desc->d_in, desc->dtype == ACE_BF16)) * desc->S *
          desc->rank * sizeof(float);
 }
@@ -247,13 +257,9 @@ size_t ace_adapter_workspace_size(const ace_adapter_desc *desc) {
 ace_status ace_adapter_add(const ace_adapter_desc *desc, const void *base, const void *x, const void *a, const void *b,
                            const float *scale, const int32_t *offsets, const int32_t *adapter, void *out,
                            void *workspace, size_t workspace_bytes, void *stream) {
-  if (!desc) return ACE_ERR_INVALID_ARG;
+  const ace_status st = adapter_desc(desc);
+  if (st != ACE_OK) return st;
   const ace_adapter_desc &d = *desc;
-  if (d.S < 0 || d.R < 0 || d.L <= 0 || d.rank <= 0 || d.d_in <= 0 || d.d_out <= 0 || !is_dtype(d.dtype))
-    return ACE_ERR_INVALID_ARG;
-  if (d.S > kMaxRows || d.R > kMaxGroups || d.rank > kMaxRank || d.d_in > kMaxWidth || d.d_out > kMaxWidth || bad_width(d.rank, d.dtype) ||
-      bad_width(d.d_in, d.dtype) || bad_width(d.d_out, d.dtype))
-    return ACE_ERR_UNSUPPORTED;
   if (d.S == 0) return ACE_OK;
   for (const void *p : {base, x, a, b, static_cast<const void *>(out)})
     if (!usable(p, 16)) return ACE_ERR_INVALID_ARG;

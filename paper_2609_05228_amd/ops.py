@@ -54,6 +54,14 @@ def _dtype_of(name, t, dims):
     return t.dtype
 
 
+def _sizes(*n):
+    """The sizes as the library's 32-bit ones; more would be cut off on the way there."""
+    for v in n:
+        if v > 0x7fffffff:
+            raise ValueError(f"a size of {v}: at most 2^31 - 1")
+    return n
+
+
 def _enqueue(dev, fn, *args):
     """fn(*args, stream) on the current stream of dev, with dev current."""
     index = dev.index
@@ -68,6 +76,7 @@ def _enqueue(dev, fn, *args):
 
 def _grouped(way, rows, other, offsets, S, N, M, K, shape, names, shapes, out):
     dtype, dev = rows.dtype, rows.device
+    size = _sizes(S, N, M, K)
     named = [(names[0], rows, shapes[0], None), (names[1], other, shapes[1], None),
              ("offsets", offsets, (N + 1,), torch.int32)]
     flags = 0
@@ -77,7 +86,7 @@ def _grouped(way, rows, other, offsets, S, N, M, K, shape, names, shapes, out):
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=dev)
         flags = _lib.ACE_ZERO_REST
-    desc = _lib.GroupedDesc(S, N, M, K, _DT[dtype], flags)
+    desc = _lib.GroupedDesc(*size, _DT[dtype], flags)
     lib = _lib.lib()
     n = lib.ace_grouped_workspace_size(desc, way)
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
@@ -136,7 +145,7 @@ def grouped_matmul_grad_w(dy, x, offsets, *, out=None):
 
 def _norm_call(lead, dtype, T, d, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, named):
     """Check a block_norm call's tensors, `named` among them; (desc, inputs)."""
-    rows, vec, kind = (T, d), (d,), 0
+    rows, vec, kind, size = (T, d), (d,), 0, _sizes(T, d)
     if y is not None:
         named.append(("y", y, rows, None))
     elif w_post is not None or gate is not None or res_scale != 1.0:
@@ -154,7 +163,7 @@ def _norm_call(lead, dtype, T, d, h, y, w_post, w_pre, gate, res_scale, branch_s
             raise ValueError(f"gate: shape {shape} is none of [d], [T, 1], [T, d]")
         named.append(("gate", gate, shape, None))
     _check_all(lead.device, dtype, named)
-    return (_lib.NormDesc(T, d, _DT[dtype], kind, res_scale, branch_scale, eps),
+    return (_lib.NormDesc(*size, _DT[dtype], kind, res_scale, branch_scale, eps),
             _lib.NormInputs(h if h is None else h.data_ptr(), y if y is None else y.data_ptr(),
                             w_post if w_post is None else w_post.data_ptr(),
                             w_pre if w_pre is None else w_pre.data_ptr(), gate if gate is None else gate.data_ptr()))
@@ -246,7 +255,7 @@ def adapter_add(base, x, a, b, offsets, adapter, *, scale=None, out=None):
     L, rank, _ = a.shape
     d_out = b.shape[1]
     R = (_groups_of(offsets) if isinstance(offsets, torch.Tensor) and offsets.shape != (1,) else 0)
-    dev = x.device
+    dev, size = x.device, _sizes(S, R, L, rank, d_in, d_out)
     named = [("x", x, (S, d_in), None), ("base", base, (S, d_out), None), ("a", a, (L, rank, d_in), None),
              ("b", b, (L, d_out, rank), None), ("offsets", offsets, (R + 1,), torch.int32),
              ("adapter", adapter, (R,), torch.int32)]
@@ -257,7 +266,7 @@ def adapter_add(base, x, a, b, offsets, adapter, *, scale=None, out=None):
     _check_all(dev, dtype, named)
     if out is None:
         out = torch.empty_like(base)
-    desc = _lib.AdapterDesc(S, R, L, rank, d_in, d_out, _DT[dtype])
+    desc = _lib.AdapterDesc(*size, _DT[dtype])
     lib = _lib.lib()
     n = lib.ace_adapter_workspace_size(desc)
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None

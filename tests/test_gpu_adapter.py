@@ -111,6 +111,19 @@ def test_many_rows(case, dtype):
     assert torch.equal(d[0], got)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [5, 4200])
+def test_an_infinite_inner_product_stays_in_its_row(rows, dtype):
+    """x infinite in one place, a and b positive there: that row of the result is infinite, no number is lost."""
+    (base, x, a, b, offs, ids), scale = (lambda m: (m[:-1], m[-1]))(make([rows], [0], 0, 0, 1, 24, 136, 72, dtype))
+    a, b = a.abs() + 0.01, b.abs() + 0.01
+    x[3, 77], x[rows - 1, 5] = float("inf"), -float("inf")
+    got = ace.adapter_add(*[t.to(DEV) for t in (base, x, a, b, offs, ids)], scale=scale.to(DEV)).cpu()
+    assert bool((got[3] == float("inf")).all()) and bool((got[rows - 1] == -float("inf")).all())
+    keep = [r for r in range(rows) if r not in (3, rows - 1)]
+    check(got[keep], (base[keep], x[keep], a, b, torch.tensor([0, rows - 2]), ids), scale, dtype)
+
+
 def test_no_rows():
     *args, scale = make([], [], 0, 0, 1, 8, 64, 40, "bf16")
     assert ace.adapter_add(*[t.to(DEV) for t in args]).shape == (0, 40)

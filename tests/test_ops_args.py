@@ -47,7 +47,7 @@ def test_grouped_workspace():
         for kw in (dict(ws=0), dict(ws=P[15] + 16), dict(ws_bytes=n - 1)):
             assert _grouped(fn, **few, **kw) == WSP, kw
         many = _lib.GroupedDesc(32768, 128, 768, 2048, _lib.ACE_BF16, 0)
-        # the weights' gradient keeps room for the parts of groups of eight times the mean
+        # the weights' gradient keeps room for the parts of groups of more than four times the mean
         assert size(many, way) == 0 if way < 2 else 0 < size(many, way) <= 2 * 128 * 768 * 2048
         assert size(_lib.GroupedDesc(64, 0, 64, 64, _lib.ACE_BF16, 0), way) == 0
     assert size(many, 3) == 0 and size(many, -1) == 0
@@ -175,3 +175,28 @@ def test_wrappers_refuse():
         with pytest.raises(ValueError, match=match):
             print(i, inspect.getsource(call).strip())
             call()
+
+
+def test_sizes_past_32_bits_are_refused():
+    """2^32 + 5 rows or columns are not 5."""
+    n = (1 << 32) + 5
+
+    def m(*shape):
+        return torch.empty(shape, dtype=torch.bfloat16, device="meta")
+
+    o, i = torch.empty(3, dtype=torch.int32, device="meta"), torch.empty(2, dtype=torch.int32, device="meta")
+    for call in (lambda: ace.grouped_matmul(m(n, 16), m(2, 8, 16), o), lambda: ace.grouped_matmul(m(1, n), m(2, 8, n), o),
+                 lambda: ace.grouped_matmul_grad_x(m(n, 8), m(2, 8, 16), o),
+                 lambda: ace.grouped_matmul_grad_w(m(n, 8), m(n, 16), o), lambda: ace.block_norm(m(n, 8), m(n, 8)),
+                 lambda: ace.block_norm_grad(m(n, 8), None, None, m(n, 8)),
+                 lambda: ace.adapter_add(m(n, 8), m(n, 16), m(2, 8, 16), m(2, 8, 8), o, i),
+                 lambda: ace.adapter_add(m(6, 8), m(6, 16), m(n, 8, 16), m(n, 8, 8), o, i)):
+        with pytest.raises(ValueError, match="size of"):
+            call()
+
+
+def test_workspace_sizes_of_refused_calls():
+    assert ace.lib().ace_block_norm_grad_workspace_size(_lib.NormDesc(BIG, 64, _lib.ACE_BF16, 0, 1.0, 1.0, 1e-6)) == 0
+    assert ace.lib().ace_block_norm_grad_workspace_size(_lib.NormDesc(64, 64, 7, 0, 1.0, 1.0, 1e-6)) == 0
+    assert ace.lib().ace_adapter_workspace_size(_lib.AdapterDesc(BIG, 4, 2, 16, 64, 64, _lib.ACE_BF16)) == 0
+    assert ace.lib().ace_adapter_workspace_size(_lib.AdapterDesc(8192, 4, 2, 12, 64, 64, _lib.ACE_BF16)) == 0
