@@ -45,18 +45,21 @@ __device__ __forceinline__ int tile_adapter(const AdapterArgs &p, const RaggedTi
 
 // acc[i][c] += rows 16 i .. of x times rows 16 c .. of A over k = first, first + step, .. (a fragment
 // pair each): lane holds rank 16 c + 4 g + q of row 16 i + lane % 16.  Rows past the tile repeat its last.
+// The whole steps begin at the rot-th, so that tiles side by side are not all at the same 64 bytes of A's rows, which
+// lie in few cache channels (8192 rows, rank 128, 2048 columns: 90 us from the first, 81 so; where a wave has two
+// steps only, 2048 fp32 rows of the same took 55 from the first, 66 so).
 template <typename T, int RT, int RB>
-__device__ __forceinline__ void shrink(const AdapterArgs &p, const RaggedTile &t, int ad, int first, int step,
+__device__ __forceinline__ void shrink(const AdapterArgs &p, const RaggedTile &t, int ad, int first, int step, int rot,
                                        f32x4_t (&acc)[RT][RB]) {
   constexpr int E = kChunkElems<T>;
   const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
-  const T *x[RT], *w[RB];
+  const T *xb = static_cast<const T *>(p.x) + static_cast<size_t>(t.row0) * p.din;
+  const T *wb = static_cast<const T *>(p.a) + static_cast<size_t>(ad) * p.r * p.din;
+  uint32_t x[RT], w[RB];  // this lane's rows from there on: at most 128 of 65536
 #pragma unroll
-  for (int i = 0; i < RT; ++i)
-    x[i] = static_cast<const T *>(p.x) + static_cast<size_t>(t.row0 + min(16 * i + r16, t.rows - 1)) * p.din;
+  for (int i = 0; i < RT; ++i) x[i] = static_cast<uint32_t>(min(16 * i + r16, t.rows - 1) * p.din + E * g);
 #pragma unroll
-  for (int c = 0; c < RB; ++c)
-    w[c] = static_cast<const T *>(p.a) + (static_cast<size_t>(ad) * p.r + min(16 * c + r16, p.r - 1)) * p.din;
+  for (int c = 0; c < RB; ++c) w[c] = static_cast<uint32_t>(min(16 * c + r16, p.r - 1) * p.din + E * g);
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -70,22 +73,25 @@ __device__ __forceinline__ void shrink(const AdapterArgs &p, const RaggedTile &t
 #pragma unroll
         for (int c = 0; c < RB; ++c) acc[i][c] = Frag<T>::mma(wf[c], xf[i], s, acc[i][c]);
   };
-  int k0 = first;
-#pragma unroll(RT == 1 ? 4 : 2)
-  for (; k0 + kStepK<T> <= p.din; k0 += step) {
+  const int whole = max(p.din - first - kStepK<T> + step, 0) / step;  // steps that end within din
+  int at = whole >= 4 ? rot % whole : 0;
+#pragma unroll 2
+  for (int s = 0; s < whole; ++s) {
+    const int k0 = first + at * step;
+    at = at + 1 == whole ? 0 : at + 1;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) xf[i] = *reinterpret_cast<const frag_of<T> *>(x[i] + k0 + E * g);
+    for (int i = 0; i < RT; ++i) xf[i] = *reinterpret_cast<const frag_of<T> *>(xb + k0 + x[i]);
 #pragma unroll
-    for (int c = 0; c < RB; ++c) wf[c] = *reinterpret_cast<const frag_of<T> *>(w[c] + k0 + E * g);
+    for (int c = 0; c < RB; ++c) wf[c] = *reinterpret_cast<const frag_of<T> *>(wb + k0 + w[c]);
     multiply();
   }
+  const int k0 = first + whole * step;
   if (k0 < p.din) {  // din ends inside the step: zeros behind the end, in both operands
-    const int k = k0 + E * g;
-    const bool in = k < p.din;
+    const bool in = k0 + E * g < p.din;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) xf[i] = in ? *reinterpret_cast<const frag_of<T> *>(x[i] + k) : zero_frag<T>();
+    for (int i = 0; i < RT; ++i) xf[i] = in ? *reinterpret_cast<const frag_of<T> *>(xb + k0 + x[i]) : zero_frag<T>();
 #pragma unroll
-    for (int c = 0; c < RB; ++c) wf[c] = in ? *reinterpret_cast<const frag_of<T> *>(w[c] + k) : zero_frag<T>();
+    for (int c = 0; c < RB; ++c) wf[c] = in ? *reinterpret_cast<const frag_of<T> *>(wb + k0 + w[c]) : zero_frag<T>();
     multiply();
   }
 }
@@ -234,7 +240,7 @@ template <typename T, int RB> __global__ __launch_bounds__(256) void adapter_shr
   // with as many row blocks as the tile has (1, 2 or all)
   auto run = [&](auto rt) {
     f32x4_t acc[rt()][RB];
-    shrink<T, rt(), RB>(p, t, ad, (split * 4 + wave) * kStepK<T>, 4 * p.splits * kStepK<T>, acc);
+    shrink<T, rt(), RB>(p, t, ad, (split * 4 + wave) * kStepK<T>, 4 * p.splits * kStepK<T>, t.row0 / kTileRows, acc);
     // the waves' sums: row block i's are added by wave i in wave order
 #pragma unroll
     for (int i = 0; i < rt(); ++i) {
@@ -367,7 +373,7 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
   __shared__ f32x4_t red[kSmallWaves][RB][64];
   __shared__ f32x4_t vs[kRowBlock * kVStride<T, KB>];
   f32x4_t acc[1][RB];
-  shrink<T, 1, RB>(p, t, ad, wave * kStepK<T>, kSmallWaves * kStepK<T>, acc);
+  shrink<T, 1, RB>(p, t, ad, wave * kStepK<T>, kSmallWaves * kStepK<T>, t.row0 / kRowBlock, acc);
 #pragma unroll
   for (int c = 0; c < RB; ++c) red[wave][c][lane] = acc[0][c];
   __syncthreads();
@@ -393,20 +399,24 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
   }
 }
 
-// One launch for up to kSmallTiles 16-row tiles, their columns in shares that fill the CUs, unless computing v
-// in each share takes longer than another launch: past 512 KB of A_a in bf16, 256 KB in fp32,
-// whose products take 16 times as long.
+// One launch for up to kSmallTiles 16-row tiles, their columns in as many shares as give every CU a workgroup (1024
+// rows of 7 requests, rank 64, 2048 columns: 18.7 us, with twice as many shares 28.7, in two launches 20.6), unless
+// computing v in each share takes longer than another launch: past 512 KB of A_a in bf16, 256 KB in fp32,
+// whose products take 16 times as long.  Requests of few rows, which would leave most of a 64-row tile empty: up to
+// twice the tiles, with half of that A_a (1000 rows of 300 requests, 2048 columns, rank 16: 16.5 us, in two launches 27;
+// rank 64 37.6 and 44; 768 columns, rank 64 in fp32 99 and 87).
 constexpr int kSmallTiles = 256;
 bool is_small(int S, int R, int r, int din, bool bf16) {
-  const long long bytes = static_cast<long long>((r + 15) / 16 * 16) * din * (bf16 ? 2 : 4);
-  return ragged_max_tiles(S, R, kRowBlock) <= kSmallTiles && bytes <= (bf16 ? 512 : 256) << 10;
+  const long long tiles = ragged_max_tiles(S, R, kRowBlock);
+  const long long bytes = static_cast<long long>((r + 15) / 16 * 16) * din * (bf16 ? 2 : 4), most = (bf16 ? 512 : 256) << 10;
+  return (tiles <= kSmallTiles && bytes <= most) || (S <= 16ll * R && tiles <= 2 * kSmallTiles && bytes <= most / 2);
 }
 
 template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t s) {
   if (is_small(p.S, p.R, p.r, p.din, sizeof(T) == 2)) {
     const long long tiles = ragged_max_tiles(p.S, p.R, kRowBlock);
     const long long groups = (p.dout + 63) / 64, most = (groups + kSmallWaves - 1) / kSmallWaves;
-    p.chunks = static_cast<int>(std::max(1ll, std::min(most, 2 * kCUs / tiles)));
+    p.chunks = static_cast<int>(std::max(1ll, std::min(most, kCUs / tiles)));
     adapter_small_kernel<T, RB><<<ragged_grid(tiles * p.chunks), 64 * kSmallWaves, 0, s>>>(p);
     return hipGetLastError();
   }
