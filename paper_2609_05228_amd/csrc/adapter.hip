@@ -402,14 +402,14 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
 // One launch for up to kSmallTiles 16-row tiles, their columns in as many shares as give every CU a workgroup (1024
 // rows of 7 requests, rank 64, 2048 columns: 18.7 us, with twice as many shares 28.7, in two launches 20.6), unless
 // computing v in each share takes longer than another launch: past 512 KB of A_a in bf16, 256 KB in fp32,
-// whose products take 16 times as long.  Requests of few rows, which would leave most of a 64-row tile empty: up to
-// twice the tiles, with half of that A_a (1000 rows of 300 requests, 2048 columns, rank 16: 16.5 us, in two launches 27;
-// rank 64 37.6 and 44; 768 columns, rank 64 in fp32 99 and 87).
+// whose products take 16 times as long.  Requests of few rows would leave most of a 64-row tile empty: one launch
+// for any number of them, with half of that A_a (2048 columns, rank 16: 1000 rows of 300 requests 16.5 us, in two
+// launches 27, 8000 rows of 700 48 and 67; rank 64 37.6 and 44, 84 and 99; fp32 rank 64 with 768 columns 99 and 87).
 constexpr int kSmallTiles = 256;
 bool is_small(int S, int R, int r, int din, bool bf16) {
   const long long tiles = ragged_max_tiles(S, R, kRowBlock);
   const long long bytes = static_cast<long long>((r + 15) / 16 * 16) * din * (bf16 ? 2 : 4), most = (bf16 ? 512 : 256) << 10;
-  return (tiles <= kSmallTiles && bytes <= most) || (S <= 16ll * R && tiles <= 2 * kSmallTiles && bytes <= most / 2);
+  return (tiles <= kSmallTiles && bytes <= most) || (S <= 16ll * R && bytes <= most / 2);
 }
 
 template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t s) {
@@ -421,8 +421,8 @@ template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t 
     return hipGetLastError();
   }
   const long long tiles = ragged_max_tiles(p.S, p.R, kTileRows);
-  // column shares: eight workgroups a CU, where there are more tiles fewer, longer ones (1225 rows of 504 requests,
-  // 3280 columns: 57 us with a workgroup for every 256 columns, 38 so)
+  // column shares: eight workgroups a CU, where there are more tiles fewer, longer ones (582 tiles, 3280 columns: 57 us
+  // with a workgroup for every 256 columns, 38 so)
   const long long most = (p.dout + 64 * kExpandWaves - 1) / (64 * kExpandWaves);
   p.chunks = static_cast<int>(std::min(most, (8 * kCUs + tiles - 1) / tiles));
   const long long shrink = tiles * p.splits, expand = tiles * p.chunks;

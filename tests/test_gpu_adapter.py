@@ -89,6 +89,7 @@ LARGE = [
     ([2000, 2300], [1, 0], 0, 0, 2, 88, 136, 136),
     ([4500], [0], 0, 0, 1, 128, 264, 520),
     ([i % 9 for i in range(600)], [i % 7 - 1 for i in range(600)], 2, 1, 6, 16, 72, 1000),
+    ([3, 0, 7] * 60, [i % 5 - 1 for i in range(180)], 0, 2, 4, 128, 2056, 72),  # few rows of many requests, a wide a
     ([30, 2], [0, 1], 0, 0, 2, 128, 4104, 136),  # few rows, a long inner product: parts of it
 ]
 
@@ -101,7 +102,8 @@ def test_many_rows(case, dtype):
     *args, scale = make(*case, dtype)
     code = _lib.ACE_BF16 if dtype == "bf16" else _lib.ACE_F32
     desc = _lib.AdapterDesc(args[0].shape[0], len(case[0]), case[4], case[5], case[6], case[7], code)
-    assert ace.lib().ace_adapter_workspace_size(desc) > 0
+    if len(case[0]) != 600:  # those are one launch again: many requests of few rows
+        assert ace.lib().ace_adapter_workspace_size(desc) > 0
     d = [t.to(DEV) for t in args]
     got = ace.adapter_add(*d, scale=scale.to(DEV))
     torch.cuda.synchronize()
