@@ -261,7 +261,7 @@ struct AdapterArgs {
   int chunks;                    // shares of the columns (small batches)
 };
 // parts of the inner product's partial sums; 0: none are kept
-int adapter_splits(int S, int R, int r, int din, bool bf16);
+int adapter_splits(int S, int R, int r, int din, int dout, bool bf16);
 // hipErrorInvalidValue, with nothing enqueued, for grids past 2^31 workgroups
 hipError_t launch_adapter(const AdapterArgs &a, bool bf16, hipStream_t stream);
 

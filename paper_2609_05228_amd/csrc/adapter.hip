@@ -399,24 +399,31 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
   }
 }
 
-// One launch for up to kSmallTiles 16-row tiles, their columns in as many shares as give every CU a workgroup (1024
-// rows of 7 requests, rank 64, 2048 columns: 18.7 us, with twice as many shares 28.7, in two launches 20.6), unless
-// computing v in each share takes longer than another launch: past 512 KB of A_a in bf16, 256 KB in fp32,
-// whose products take 16 times as long.  Requests of few rows would leave most of a 64-row tile empty: one launch
+// Column shares of one launch: as many as give every CU a workgroup, a 64-column group a wave at least (1024 rows of 7
+// requests, rank 64, 2048 columns: 18.7 us, with twice as many shares 28.7, in two launches 20.6).
+constexpr int kSmallTiles = 256;
+int small_shares(long long tiles, int dout) {
+  const int groups = (dout + 63) / 64, most = (groups + kSmallWaves - 1) / kSmallWaves;
+  return static_cast<int>(std::max(1ll, std::min<long long>(most, kCUs / tiles)));
+}
+
+// One launch for up to kSmallTiles 16-row tiles, unless computing v in each share takes longer than another launch: past
+// 512 KB of A_a in bf16, 256 KB in fp32, whose products take 16 times as long; or a share's part of B_a does: past
+// 512 KB (2048 rows of 7 requests, 768 x 4096: rank 128 46 us and in two launches 40, rank 64 29 and 27, 3000 rows 30 and
+// 33).  Requests of few rows would leave most of a 64-row tile empty: one launch
 // for any number of them, with half of that A_a (2048 columns, rank 16: 1000 rows of 300 requests 16.5 us, in two
 // launches 27, 8000 rows of 700 48 and 67; rank 64 37.6 and 44, 84 and 99; fp32 rank 64 with 768 columns 99 and 87).
-constexpr int kSmallTiles = 256;
-bool is_small(int S, int R, int r, int din, bool bf16) {
-  const long long tiles = ragged_max_tiles(S, R, kRowBlock);
-  const long long bytes = static_cast<long long>((r + 15) / 16 * 16) * din * (bf16 ? 2 : 4), most = (bf16 ? 512 : 256) << 10;
-  return (tiles <= kSmallTiles && bytes <= most) || (S <= 16ll * R && bytes <= most / 2);
+bool is_small(int S, int R, int r, int din, int dout, bool bf16) {
+  const long long tiles = ragged_max_tiles(S, R, kRowBlock), row = (r + 15) / 16 * 16 * (bf16 ? 2 : 4);
+  const long long most = (bf16 ? 512 : 256) << 10;
+  if (row * dout / small_shares(tiles, dout) > 512 << 10) return false;
+  return (tiles <= kSmallTiles && row * din <= most) || (S <= 16ll * R && row * din <= most / 2);
 }
 
 template <typename T, int RB> hipError_t launch_rank(AdapterArgs p, hipStream_t s) {
-  if (is_small(p.S, p.R, p.r, p.din, sizeof(T) == 2)) {
+  if (is_small(p.S, p.R, p.r, p.din, p.dout, sizeof(T) == 2)) {
     const long long tiles = ragged_max_tiles(p.S, p.R, kRowBlock);
-    const long long groups = (p.dout + 63) / 64, most = (groups + kSmallWaves - 1) / kSmallWaves;
-    p.chunks = static_cast<int>(std::max(1ll, std::min(most, kCUs / tiles)));
+    p.chunks = small_shares(tiles, p.dout);
     adapter_small_kernel<T, RB><<<ragged_grid(tiles * p.chunks), 64 * kSmallWaves, 0, s>>>(p);
     return hipGetLastError();
   }
@@ -445,8 +452,8 @@ template <typename T> hipError_t launch_t(const AdapterArgs &p, hipStream_t s) {
 
 }  // namespace
 
-int adapter_splits(int S, int R, int r, int din, bool bf16) {
-  if (is_small(S, R, r, din, bf16)) return 0;
+int adapter_splits(int S, int R, int r, int din, int dout, bool bf16) {
+  if (is_small(S, R, r, din, dout, bf16)) return 0;
   const long long tiles = ragged_max_tiles(S, R, kTileRows);
   const int step = bf16 ? kStepK<bf16_t> : kStepK<float>;
   int n = 1;

@@ -250,7 +250,7 @@ ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs 
 
 size_t ace_adapter_workspace_size(const ace_adapter_desc *desc) {
   if (adapter_desc(desc) != ACE_OK || desc->S == 0) return 0;
-  return static_cast<size_t>(ace::adapter_splits(desc->S, desc->R, desc->rank, desc->d_in, desc->dtype == ACE_BF16)) * desc->S *
+  return static_cast<size_t>(ace::adapter_splits(desc->S, desc->R, desc->rank, desc->d_in, desc->d_out, desc->dtype == ACE_BF16)) * desc->S *
          desc->rank * sizeof(float);
 }
 
@@ -289,7 +289,7 @@ ace_status ace_adapter_add(const ace_adapter_desc *desc, const void *base, const
   p.r = d.rank;
   p.din = d.d_in;
   p.dout = d.d_out;
-  p.splits = ace::adapter_splits(d.S, d.R, d.rank, d.d_in, d.dtype == ACE_BF16);
+  p.splits = ace::adapter_splits(d.S, d.R, d.rank, d.d_in, d.d_out, d.dtype == ACE_BF16);
   return status_of(ace::launch_adapter(p, d.dtype == ACE_BF16, static_cast<hipStream_t>(stream)));
 }
 
