@@ -10,7 +10,7 @@
 // for itself and multiplies it by its share of B_a's rows.
 // Operands go from memory straight into the matrix cores' registers: a wave reads each fragment
 // of A_a and B_a once and uses it for every row of its tile, so staging them would save nothing.
-// v stays exact to 16 bits in bf16 calls: it is multiplied as the sum of two bf16 numbers (a
+// v stays exact to 2^-16 in bf16 calls: it is multiplied as the sum of two bf16 numbers (a
 // single rounding of v to 8 bits would cost as much as that of the output).
 #include <algorithm>
 #include <type_traits>
@@ -96,21 +96,18 @@ __device__ __forceinline__ void shrink(const AdapterArgs &p, const RaggedTile &t
   }
 }
 
-// A lane's E values of v as fragments: bf16 the value rounded and the rest of it (nothing where that is no
-// number: an infinite v stays one), fp32 itself
+// A lane's E values of v as fragments: bf16 the value cut off and the rest of it (of the same sign, so the two
+// parts' products never cancel; a value between bf16's largest and fp32's stays finite), fp32 itself
 template <typename T> struct VFrag {
   frag_of<T> hi, lo;
-  static __device__ __forceinline__ float rest(float f, uint32_t rounded) {
-    const float d = f - __uint_as_float(rounded);
-    return __builtin_isfinite(d) ? d : 0.f;
-  }
   __device__ __forceinline__ void set(const float *f) {
     if constexpr (sizeof(T) == 2) {
       uint32_t h[4], l[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        h[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
-        l[i] = pack_bf16x2(rest(f[2 * i], h[i] << 16), rest(f[2 * i + 1], h[i] & 0xffff0000u));
+        const uint32_t a = __float_as_uint(f[2 * i]) & 0xffff0000u, b = __float_as_uint(f[2 * i + 1]) & 0xffff0000u;
+        h[i] = a >> 16 | b;
+        l[i] = pack_bf16x2(f[2 * i] - __uint_as_float(a), f[2 * i + 1] - __uint_as_float(b));
       }
       hi = __builtin_bit_cast(frag_of<T>, uint4{h[0], h[1], h[2], h[3]});
       lo = __builtin_bit_cast(frag_of<T>, uint4{l[0], l[1], l[2], l[3]});
@@ -180,18 +177,35 @@ template <typename T, int KB> struct Columns {
   __device__ __forceinline__ void finish(const AdapterArgs &p, const VFrag<T> (&v)[KB], size_t row, bool there,
                                          uint4 (&bv)[PIECES]) const {
     f32x4_t acc[4];
+    auto multiply = [&](f32x4_t (&d)[4], bool rest) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < 4; ++c) d[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int s = 0; s < Frag<T>::steps; ++s) {
+        for (int s = 0; s < Frag<T>::steps; ++s) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) acc[c] = Frag<T>::mma(w[kb][c], v[kb].hi, s, acc[c]);
-        if constexpr (PAIR)
+          for (int c = 0; c < 4; ++c) d[c] = Frag<T>::mma(w[kb][c], v[kb].hi, s, d[c]);
+          if constexpr (PAIR)
+            if (rest)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) acc[c] = Frag<T>::mma(w[kb][c], v[kb].lo, s, acc[c]);
+              for (int c = 0; c < 4; ++c) d[c] = Frag<T>::mma(w[kb][c], v[kb].lo, s, d[c]);
+        }
+    };
+    multiply(acc, true);
+    if constexpr (PAIR) {
+      // An infinite b or v makes no number of its product with v's rest (infinity times zero).  Where a sum is not
+      // finite, the products of v's first part alone say what it is.
+      const f32x4_t t = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+      if (__any(!__builtin_isfinite((t[0] + t[1]) + (t[2] + t[3])))) {
+        f32x4_t first[4];
+        multiply(first, false);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[c][j] = __builtin_isfinite(first[c][j]) ? acc[c][j] : first[c][j];
       }
+    }
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       if constexpr (PAIR) {
