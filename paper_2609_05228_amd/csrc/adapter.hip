@@ -173,8 +173,9 @@ template <typename T, int KB> struct Columns {
       v[i] = there && col(i) < p.dout ? *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.base) + row * p.dout + col(i))
                                       : uint4{0, 0, 0, 0};
   }
-  // out = base + B v for the row of this lane
-  __device__ __forceinline__ void finish(const AdapterArgs &p, const VFrag<T> (&v)[KB], size_t row, bool there,
+  // out = base + scale B v for the row of this lane.  The scale comes last, as the definition has it: on v, an infinite
+  // one would make no number of the zeros that pad an adapter of lower rank.
+  __device__ __forceinline__ void finish(const AdapterArgs &p, const VFrag<T> (&v)[KB], float scale, size_t row, bool there,
                                          uint4 (&bv)[PIECES]) const {
     f32x4_t acc[4];
     auto multiply = [&](f32x4_t (&d)[4], bool rest) {
@@ -213,12 +214,12 @@ template <typename T, int KB> struct Columns {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const f32x4_t &d = acc[2 * i + (j >> 1)];
-          b[j] = pack_bf16x2(__uint_as_float(b[j] << 16) + d[2 * (j & 1)],
-                             __uint_as_float(b[j] & 0xffff0000u) + d[2 * (j & 1) + 1]);
+          b[j] = pack_bf16x2(__uint_as_float(b[j] << 16) + scale * d[2 * (j & 1)],
+                             __uint_as_float(b[j] & 0xffff0000u) + scale * d[2 * (j & 1) + 1]);
         }
         bv[i] = uint4{b[0], b[1], b[2], b[3]};
       } else {
-        bv[i] = __builtin_bit_cast(uint4, __builtin_bit_cast(f32x4_t, bv[i]) + acc[i]);
+        bv[i] = __builtin_bit_cast(uint4, __builtin_bit_cast(f32x4_t, bv[i]) + scale * acc[i]);
       }
     }
     put(p, row, there, bv);
@@ -323,7 +324,7 @@ template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) vo
     return;
   }
   if (cols.first + wave < cols.last) w.load(p, ad, 64 * (cols.first + wave));
-  // v of the tile's rows: the parts added in order, times the scale, once for all waves
+  // v of the tile's rows: the parts added in order, once for all waves
   __shared__ f32x4_t vs[kTileRows * kVStride<T, KB>];
   const float sc = p.scale ? p.scale[ad] : 1.f;
   for (int s = 1; s < p.splits; ++s)
@@ -332,7 +333,7 @@ template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) vo
 #pragma unroll
   for (int j = 0; j < VT; ++j) {
     const int i = static_cast<int>(threadIdx.x) + j * 64 * kExpandWaves, q = i % VQ;
-    vs[i / VQ * kVStride<T, KB> + q] = 4 * q < p.r ? vsum[j] * sc : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    vs[i / VQ * kVStride<T, KB> + q] = 4 * q < p.r ? vsum[j] : f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
   __syncthreads();
   for (int q = cols.first + wave; q < cols.last; q += kExpandWaves) {
@@ -345,7 +346,7 @@ template <typename T, int KB> __global__ __launch_bounds__(64 * kExpandWaves) vo
       read_v<T, KB>(vs, 16 * i + r16, vf);
       // the next block's rows of base are under way while this one's are finished
       if (i + 1 < blocks) w.base_of(p, row_of(i + 1), there(i + 1), next);
-      w.finish(p, vf, row_of(i), there(i), bv);
+      w.finish(p, vf, sc, row_of(i), there(i), bv);
 #pragma unroll
       for (int j = 0; j < Cols::PIECES; ++j) bv[j] = next[j];
     }
@@ -397,7 +398,7 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
 #pragma unroll
     for (int i = 1; i < kSmallWaves; ++i) s += red[i][c][lane];
     const int q = 4 * c + g;
-    vs[r16 * kVStride<T, KB> + q] = 4 * q < p.r ? s * sc : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    vs[r16 * kVStride<T, KB> + q] = 4 * q < p.r ? s : f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
   for (int i = threadIdx.x; i < kRowBlock * (kVQuads<T, KB> - 4 * RB); i += 64 * kSmallWaves)
     vs[i % kRowBlock * kVStride<T, KB> + 4 * RB + i / kRowBlock] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -409,7 +410,7 @@ template <typename T, int RB> __global__ __launch_bounds__(64 * kSmallWaves) voi
       w.load(p, ad, 64 * q);
       w.base_of(p, row, there, bv);
     }
-    w.finish(p, vf, row, there, bv);
+    w.finish(p, vf, sc, row, there, bv);
   }
 }
 

@@ -66,3 +66,30 @@ def test_a_product_past_fp32_is_infinite(rows, dtype):
     b[0, 8] = -b[0, 7]
     got = run(args, None).cpu()
     assert got[1, 7] == INF and got[1, 8] == -INF and got[3, 7] == -INF and got[3, 8] == INF
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [5, 4200])
+def test_an_infinite_scale_and_an_adapter_of_lower_rank(rows, dtype):
+    """Ranks past the adapter's own have zeros in a, anything in b: infinity times the product is infinite."""
+    *args, scale = make([rows], [0], 0, 0, 1, 16, 136, 72, dtype)
+    base, x, a, b, offs, ids = args
+    for t in (x, a, b):
+        t.copy_(t.abs() + 0.01)
+    a[0, 8:] = 0
+    b[0, :, 11] *= -1
+    for sign in (INF, -INF):
+        scale[0] = sign
+        assert bool((run(args, scale).cpu() == sign).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [5, 4200])
+def test_a_large_scale_of_a_small_product(rows, dtype):
+    """The inner product, some 2^50, times the scale alone would pass fp32; with b it does not."""
+    *args, scale = make([rows], [0], 0, 0, 1, 8, 136, 72, dtype)
+    args[1].mul_(2.0 ** 25)
+    args[2].mul_(2.0 ** 25)
+    args[3].mul_(2.0 ** -100)
+    scale[0] = 2.0 ** 80
+    check(run(args, scale), args, scale, dtype)
