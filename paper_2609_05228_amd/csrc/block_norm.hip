@@ -296,10 +296,12 @@ __global__ __launch_bounds__(NT *RG) void block_norm_grad_kernel(NormArgs a) {
     const float gt = there ? a.branch_scale * gate_of_row<T>(a, row) : 0.f;
     float q[CH][V];
     float s2[2] = {0.f, 0.f};  // sum q y, sum t u
+    // a row that is not there adds nothing to the parameters' sums: its zeros times an infinite parameter would
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
+      if (!there) break;
       const int col = (c * NT + tid) * V;
-      const bool in = there && col < a.d;
+      const bool in = col < a.d;
       float h[V], p[V], y[V], t[V], w[V], o[V];
       unpack<T>(cur[0][c], h);
       unpack<T>(cur[1][c], p);
