@@ -341,15 +341,17 @@ __global__ __launch_bounds__(NT *RG) void block_norm_grad_kernel(NormArgs a) {
     if (a.w_post || a.gate_kind == 2) sum2(s2);
     if (a.gate_kind == 2 && tid == 0 && there)
       static_cast<T *>(a.g_gate)[row] = Elem<T>::from_f32(a.branch_scale * s2[1]);
-    const float k = a.w_post ? s2[0] * inv_d * s * s * s : 0.f;
+    const float k = s2[0] * inv_d * s * s * s;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int col = (c * NT + tid) * V;
-      float y[V], o[V];
-      unpack<T>(cur[2][c], y);
+      if (a.w_post) {  // else dy is q, whatever y is
+        float y[V];
+        unpack<T>(cur[2][c], y);
 #pragma unroll
-      for (int i = 0; i < V; ++i) o[i] = s * q[c][i] - y[i] * k;
-      if (there && col < a.d) store_vec(static_cast<T *>(a.g_y) + ro + col, o);
+        for (int i = 0; i < V; ++i) q[c][i] = s * q[c][i] - y[i] * k;
+      }
+      if (there && col < a.d) store_vec(static_cast<T *>(a.g_y) + ro + col, q[c]);
     }
   }
   float *part = a.part;

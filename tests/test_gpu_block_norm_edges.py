@@ -41,3 +41,19 @@ def test_an_infinite_parameter_and_rows_that_are_not_there(where, d, T, dtype):
     assert want[other][3] == INF and bool(want[where].isfinite().all())
     for k in ("h", "gate", "w_post"):
         same(got[k], want[k], mag[k], dtype, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gate", ["channel", "token", "full"])
+@pytest.mark.parametrize("d", [40, 8200])
+def test_y_does_not_reach_its_own_gradient_without_a_norm(d, gate, dtype):
+    """u = gate y: the gradient of y is the gate's times dh', whatever y holds."""
+    t, dh, _ = make(5, d, dtype, gate, False, False)
+    t["y"][1, 7], t["y"][2, 30], t["y"][4, 0] = INF, NAN, -INF
+    got = ace.block_norm_grad(dh.to(DEV), None, **dev(t))
+    torch.cuda.synchronize()
+    want, mag = ref.block_norm_grad(dh, None, **t)
+    assert bool(want["y"].isfinite().all()) and not bool(want["gate"].isfinite().all())
+    for k in ("h", "y"):
+        ref.close(got[k], want[k], mag[k], DT[dtype], TERMS, k)
+    same(got["gate"], want["gate"], mag["gate"], dtype, "gate")
