@@ -180,7 +180,7 @@ def block_norm(h, y=None, *, w_post=None, w_pre=None, gate=None, res_scale=1.0, 
     y        [T, d]: the block's output (`moe_forward`'s y); None for the norm before the first block
     w_post, w_pre  [d] or None
     gate     [d], [T, 1] or [T, d], or None
-    out      dict that may hold "h" and "n" [T, d] (h or y themselves are fine)
+    out      dict that may hold "h" and "n" [T, d] (h or y themselves are fine; "h" only with y)
     d is a multiple of 8 (fp32: 4), at most 16384; eps > 0.  Returns dict(h=h'[, n]); without y, h' is h."""
     dtype = _dtype_of("h", h, 2)
     T, d = h.shape
@@ -189,6 +189,8 @@ def block_norm(h, y=None, *, w_post=None, w_pre=None, gate=None, res_scale=1.0, 
         out = {}
     else:
         out = dict(out)
+        if y is None and out.get("h", h) is not h:
+            raise ValueError("out['h'] needs y: without it h' is h itself")
         named += [(f"out['{k}']", out[k], h.shape, None) for k in ("h", "n") if k in out]
     desc, inp = _norm_call(h, dtype, T, d, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, named)
     if y is None:
