@@ -5,12 +5,14 @@ scale, and low-rank adapters of many requests at once.
 Like `moe_forward` they marshal device tensors into the C ABI of libace.so and enqueue on the
 current HIP stream of the tensors' device.  They record no autograd graph: the gradients are
 entry points of their own (`grouped_matmul_grad_x`, `grouped_matmul_grad_w`, `block_norm_grad`),
-and inputs that require a gradient are refused while autograd is on.  Workspaces come from
-torch's allocator with every call, so captured graphs share none.
+and inputs that require a gradient are refused while autograd is on, inputs with a forward-mode
+tangent always.  Workspaces come from torch's allocator with every call, so captured graphs share
+none.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
 from .layer import _DT
@@ -29,6 +31,11 @@ def _need(ok, msg):
 def _check_all(dev, dtype, named):
     """(name, tensor, shape, dtype or None for the call's): shapes, types, layout, device."""
     grad = torch.is_grad_enabled()
+    # asked for each tensor inside a forward-mode level only: that takes as long as the other checks
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        for name, t, _, _ in named:
+            if forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError(f"{name} has a forward-mode tangent, which the call would lose")
     for name, t, shape, dt in named:
         if (t.shape == shape and t.dtype is (dt or dtype) and t.device == dev and t.is_contiguous()
                 and not (grad and t.requires_grad)):
