@@ -57,3 +57,50 @@ def test_y_does_not_reach_its_own_gradient_without_a_norm(d, gate, dtype):
     for k in ("h", "y"):
         ref.close(got[k], want[k], mag[k], DT[dtype], TERMS, k)
     same(got["gate"], want["gate"], mag["gate"], dtype, "gate")
+
+
+PLACES = ("dh", "dn", "h", "y")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,gate", [(9001, 264, "channel"), (9001, 264, "token"), (9001, 264, "full"), (600, 8200, "channel"),
+                                      (5, 40, "token")])
+def test_gradients_on_their_inputs(T, d, gate, dtype):
+    """The C entry allows the gradients of h and of y each on one of dh, dn, h and y: the same bits as apart from
+    them, also where a workgroup copies its next rows before it writes the present ones' results."""
+    from paper_2609_05228_amd import _lib
+
+    t, dh, dn = make(T, d, dtype, gate)
+    src = dict(dev(t), dh=dh.to(DEV), dn=dn.to(DEV))
+    code = _lib.ACE_BF16 if dtype == "bf16" else _lib.ACE_F32
+    desc = _lib.NormDesc(T, d, code, {"channel": 1, "token": 2, "full": 3}[gate], 0.75, 0.3, 1e-6)
+    lib = ace.lib()
+    ws = torch.empty(lib.ace_block_norm_grad_workspace_size(desc), dtype=torch.uint8, device=DEV)
+
+    def run(on_h, on_y):
+        g = {k: v.clone() for k, v in src.items()}
+        out = {k: torch.full_like(g[k], 3) for k in ("w_post", "w_pre", "gate")}
+        out["h"] = g[on_h] if on_h else torch.full_like(g["h"], 3)
+        out["y"] = g[on_y] if on_y else torch.full_like(g["y"], 3)
+        inp = _lib.NormInputs(*[g[k].data_ptr() for k in ("h", "y", "w_post", "w_pre", "gate")])
+        grads = _lib.NormGrads(*[out[k].data_ptr() for k in ("h", "y", "w_post", "w_pre", "gate")])
+        st = lib.ace_block_norm_grad(desc, inp, g["dh"].data_ptr(), g["dn"].data_ptr(), grads, ws.data_ptr(), ws.numel(),
+                                     torch.cuda.current_stream().cuda_stream)
+        assert st == _lib.ACE_OK, (on_h, on_y)
+        torch.cuda.synchronize()
+        for k in PLACES:  # what no result lies on stays
+            assert k in (on_h, on_y) or torch.equal(g[k], src[k]), (on_h, on_y, k)
+        return out
+
+    want = run(None, None)
+    w = ace.block_norm_grad(src["dh"], src["dn"], src["h"], src["y"], w_post=src["w_post"], w_pre=src["w_pre"],
+                            gate=src["gate"], res_scale=0.75, branch_scale=0.3)
+    for k in want:
+        assert torch.equal(want[k], w[k]), k
+    for on_h in (None, *PLACES):
+        for on_y in (None, *PLACES):
+            if on_h == on_y:
+                continue
+            got = run(on_h, on_y)
+            for k in want:
+                assert torch.equal(got[k], want[k]), (on_h, on_y, k)
