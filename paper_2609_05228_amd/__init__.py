@@ -13,8 +13,8 @@ ratios (App. C.1); and `build_tables` computes the offline GSP / RCR tables
 Around the layer, for the decoder that contains it and for fine-tuning it:
 `grouped_matmul` (matrix products grouped by expert with ragged sizes) with its
 gradients, `block_norm` (the norms before and after a block with its gate and
-residual scale) with its gradient, and `adapter_add` (low-rank adapters of many
-requests beside a shared projection).
+residual scale) with its gradient, and, for serving only, `adapter_add` (low-rank
+adapters of many requests beside a shared projection).
 """
 from ._lib import (  # noqa: F401
     ACE_BF16, ACE_ERR_HIP, ACE_ERR_INVALID_ARG, ACE_ERR_UNSUPPORTED, ACE_ERR_WORKSPACE, ACE_F32,

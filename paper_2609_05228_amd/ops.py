@@ -48,7 +48,8 @@ def _check_all(dev, dtype, named):
             raise ValueError(f"{name} must be contiguous")
         if t.device != dev:
             raise ValueError(f"{name} is on {t.device}, expected {dev}")
-        raise ValueError(f"{name} requires a gradient: call under torch.no_grad() and use the *_grad functions")
+        raise ValueError(f"{name} requires a gradient, and no graph is recorded: call under torch.no_grad() (gradients of "
+                         "grouped_matmul and block_norm: the *_grad functions; adapter_add has none)")
     if dev.type != "cuda":
         raise ValueError(f"the tensors are on {dev}: a GPU is needed")
 
@@ -256,7 +257,7 @@ def adapter_add(base, x, a, b, offsets, adapter, *, scale=None, out=None):
     scale    [L] fp32 or None
     out      [S, d_out] or None; `base` itself adds in place
     Rows without an adapter, and rows of no request, are base's.  d_in, d_out and the rank (at most 128) are
-    multiples of 8 (fp32: 4).  Returns out."""
+    multiples of 8 (fp32: 4).  For serving: it has no gradient.  Returns out."""
     dtype = _dtype_of("x", x, 2)
     _dtype_of("a", a, 3)
     _dtype_of("b", b, 3)

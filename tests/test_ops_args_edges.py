@@ -18,6 +18,13 @@ def test_a_buffer_for_h_without_y_is_refused():
         ace.block_norm(h, w_pre=w, out={"h": h, "n": _z(6, 16)})
 
 
+def test_a_refused_gradient_names_no_function_that_is_not_there():
+    x, dy = _z(6, 16), _z(6, 8)
+    with pytest.raises(ValueError, match="no_grad.*adapter_add has none"):
+        ace.adapter_add(dy, x.requires_grad_(), _z(2, 8, 16), _z(2, 8, 8), torch.tensor([0, 2, 6], dtype=torch.int32),
+                        torch.tensor([0, -1], dtype=torch.int32))
+
+
 @pytest.mark.parametrize("which", range(4))
 def test_forward_mode_tangents_are_refused(which):
     """A dual tensor's tangent would be lost without a word; the same call outside needs only a GPU."""
