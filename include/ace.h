@@ -357,6 +357,7 @@ ace_status ace_block_norm_grad(const ace_norm_desc *desc, const ace_norm_inputs 
  *   scale [L] fp32 or NULL (ones); offsets [R + 1] and adapter [R] int32 (adapter may be NULL when R = 0).
  *   workspace  DEVICE scratch of ace_adapter_workspace_size(desc) bytes, 256-byte aligned (may be NULL when
  *              that is 0: small batches).
+ * The scale multiplies the finished product.  There is no gradient entry.
  * An adapter of lower rank is padded with zero rows of a.  Limits (else ACE_ERR_UNSUPPORTED): S < 2^31 - 2^16, R <= 4096,
  * rank <= 128, d_in and d_out <= 65536.
  */

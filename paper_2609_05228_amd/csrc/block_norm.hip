@@ -9,7 +9,7 @@
 //   q   = du w_post, dy = (q - y (sum q y) / (d rms^2)) / rms               (rms of y)
 //   dw_pre = sum over rows of dn h' / rms,  dw_post = sum over rows of du y / rms
 // A row belongs to one workgroup whose threads keep its elements in registers between the
-// sums, so every operand is read once and every result written once: HBM-bound.  All
+// sums, so every operand is read once and every result written once: the forward is HBM-bound.  All
 // arithmetic and every sum is fp32, each result rounded once.
 #include <algorithm>
 #include <type_traits>
@@ -186,14 +186,18 @@ template <int NT, int RG, int N> struct RowSum {
 
 // A workgroup takes RG rows at a time (NT threads each).  While it works on them, held in registers as
 // stored and widened where used, the next ones are copied into LDS (each thread its own 16 bytes of
-// each operand, so a wave waits for its own copies only); weights and a gate per channel lie in LDS too, so
-// that no other load has to be waited for.
+// each operand, so no barrier is needed for them); weights and a gate per channel lie in LDS too.  As compiled, a
+// round's first reads of LDS wait for all of the wave's memory operations, the last row's stores among them
+// (the choice between an operand and zeros is made between addresses, so they are flat loads), and a gate per
+// token or element, loaded behind the next rows' copies, waits for those.
 // The parameter gradients are sums over rows: a thread keeps its columns' sums of its rows in registers,
 // the RG rows' are added through LDS at the end, and each workgroup writes one line of part
 // [w_pre, w_post, gate [d]][gridDim.x][d], which param_sum_kernel adds in a fixed order (no atomics:
 // equal calls give equal bits).  RG rows at a time keep these lines few.
-// Bound by HBM and the fp32 pipes alike: some 30 operations an element, 12 of the 19 us that the memory
-// takes for 4096 rows of 2048 (bf16).
+// Not at the memory's rate: 4096 rows of 2048 (bf16) take 28.6 us with a gate per channel, 27.7 per token, 29.9 per
+// element, where the memory takes 19.4, 19.4 and 25.8; 4 of them are param_sum_kernel's.  Some 30 fp32 operations
+// an element and the waits above stand beside it.  Two or four accesses a thread spill registers (72 of bf16,
+// 83 of fp32): 2048 rows of 16384 (bf16) take 231 us, the memory 78.
 template <typename T, int NT, int CH, int RG>
 __global__ __launch_bounds__(NT *RG) void block_norm_grad_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
@@ -245,7 +249,7 @@ __global__ __launch_bounds__(NT *RG) void block_norm_grad_kernel(NormArgs a) {
     __syncthreads();
   }
   // stores of a wave after the copies that it waits for: at least these (a wave's memory operations finish
-  // in order)
+  // in order; see above for what is waited for behind it)
   const int behind = 1 + (a.y != nullptr) + (a.gate_kind == 3);
   bool first = true;
   for (int row0 = blockIdx.x * RG; row0 < a.T; row0 += step) {
@@ -414,7 +418,8 @@ constexpr int kNormBlocks = 2048;
 constexpr int kGradBlocks = 256;  // a workgroup a CU
 
 // Threads of a gradient workgroup: 1024, or 512 where those would not fill the CUs once (bf16: 117 rows of 384
-// 10.8 us with 1024 and 8.4 with 512, 1574 rows of 200 11.6 and 9.8; 4096 rows of 2048 29 and 32, 10819 of 1296 63 and 77)
+// 10.8 us with 1024 and 8.4 with 512, 1574 rows of 200 11.6 and 9.8; 4096 rows of 2048 29 and 32, 10819 of 1296 63 and 77;
+// of the bf16 kernel's 131 to 135 registers only one such workgroup fits a CU, of the fp32 kernel's 86 to 94 two).
 // They come as whole rows' threads.
 constexpr int grad_small(int nt) { return nt >= 512 ? nt : 512 / nt * nt; }
 constexpr int grad_large(int nt) { return 1024 / nt * nt; }

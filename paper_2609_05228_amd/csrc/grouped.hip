@@ -321,7 +321,8 @@ __device__ __forceinline__ void store_part(const TileRef<T> &t, size_t ldo, cons
 // The tiles of a workgroup's list (item j in lane j of every wave, n of them) as one pipeline:
 // stages of a tile's operands are copied DA - 1 and DB - 1 ahead of their use through rings of DA
 // and DB LDS slots, and across the end of a tile, so the next tile's first stages are under way
-// while a tile ends and stores.  A tile is MB x NB 16-blocks, WR x WC waves.  ref(item) gives a
+// while a tile ends and stores.  Where PENDING is 0 (both rings two deep: the weights' gradient in 256 x 256 tiles) the
+// next tile's first products wait for those stores.  A tile is MB x NB 16-blocks, WR x WC waves.  ref(item) gives a
 // tile's operands; lda, ldb, ldo are common.
 template <typename T, bool ADOWN, bool BDOWN, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB, typename F>
 __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, int ldb, size_t ldo, uint8_t *smem,
@@ -519,7 +520,8 @@ __global__ __launch_bounds__(WR *WC * 64) void grouped_rows_kernel(GroupedArgs g
 
 // The same with the tile shape taken here, from the groups' sizes that only the device knows: a
 // group's last row tile costs about a full one, so which height wastes least goes by them.
-// Rounds of a CU times the time of a stage, in units of 50 ns as measured with every CU busy.
+// Rounds of a CU times the time of a stage, in units of 50 ns as measured with every CU busy.  Four tile bodies
+// in one kernel spill 49 vector registers in the rows' gradient and 6 in the forward.
 template <bool GX, bool LINES> __global__ __launch_bounds__(512) void grouped_shapes_kernel(GroupedArgs g) {
   __shared__ __align__(16) uint8_t smem[160 * 1024];
   const int cols = GX ? g.K : g.M;
@@ -737,7 +739,8 @@ Plan plan_rows(const GroupedArgs &g, bool grad, bool bf16) {
   return {large ? Kind::kLarge : Kind::k128, 1, elems};
 }
 
-// ... and for the weights' gradient.  128 groups of 768 x 2048 and 128 rows: 256 x 256 tiles 114 us, 128 x 128 134.
+// ... and for the weights' gradient.  128 groups of 768 x 2048 and 128 rows: 256 x 256 tiles 114 us, 128 x 128 134
+// (the former spill 27 registers and wait for each tile's stores).
 // A group of more than p.chunk rows is summed in parts of at most that many, which a second launch adds: a few
 // long groups would otherwise be a few workgroups' work.  Parts are four times the mean group (2048 rows at least),
 // so that their sums take no more room than dw itself (bf16); or fewer rows where all tiles together

@@ -26,8 +26,9 @@ inline long long ragged_max_tiles(long long S, long long N, int tm) {
 // call).  The gaps come as groups of their own before the first and behind the last when
 // `gaps` is set; with `each`, a group without rows has one tile of none.  Offsets are clamped to 0 .. S, so whatever they hold, rows outside the
 // array are never named.  Lane l counts the tiles of `per` consecutive groups, one wave
-// scan places them: one round of loads and one scan, against a launch of its own for a tile
-// list.
+// scan places them: `per` + 2 loads and one scan, against a launch of its own for a tile
+// list.  Each load stands behind a condition of its own, so they come one after the other: three trips to the
+// cache up to 62 groups, some 70 for 4096, and `per` more to find a tile where it is over 1.
 struct RaggedTiles {
   const int32_t *offsets;
   int N, S, tm, per, cnt, inc, total;
@@ -51,7 +52,7 @@ struct RaggedTiles {
     const int lane = threadIdx.x & 63;
     const int p0 = lane * per;
     int lo = bound(p0);
-#pragma unroll 4  // the loads of four groups in flight together, here and below
+#pragma unroll 4
     for (int j = 0; j < per; ++j) {
       const int hi = bound(p0 + j + 1);
       const int n = tiles(p0 + j, lo, hi);
