@@ -197,7 +197,7 @@ def block_norm(h, y=None, *, w_post=None, w_pre=None, gate=None, res_scale=1.0, 
         out = {}
     else:
         out = dict(out)
-        if y is None and out.get("h", h) is not h:
+        if y is None and out.get("h", h).data_ptr() != h.data_ptr():
             raise ValueError("out['h'] needs y: without it h' is h itself")
         named += [(f"out['{k}']", out[k], h.shape, None) for k in ("h", "n") if k in out]
     desc, inp = _norm_call(h, dtype, T, d, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, named)

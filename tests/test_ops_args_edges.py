@@ -16,6 +16,8 @@ def test_a_buffer_for_h_without_y_is_refused():
         ace.block_norm(h, w_pre=w, out={"h": _z(6, 16)})
     with pytest.raises(ValueError, match="GPU"):  # h itself holds it
         ace.block_norm(h, w_pre=w, out={"h": h, "n": _z(6, 16)})
+    with pytest.raises(ValueError, match="GPU"):  # and so does another view of it
+        ace.block_norm(h, w_pre=w, out={"h": h.view(6, 16)})
 
 
 def test_a_refused_gradient_names_no_function_that_is_not_there():
