@@ -196,8 +196,8 @@ template <int NT, int RG, int N> struct RowSum {
 // equal calls give equal bits).  RG rows at a time keep these lines few.
 // Not at the memory's rate: 4096 rows of 2048 (bf16) take 28.6 us with a gate per channel, 27.7 per token, 29.9 per
 // element, where the memory takes 19.4, 19.4 and 25.8; 4 of them are param_sum_kernel's.  Some 30 fp32 operations
-// an element and the waits above stand beside it.  Two or four accesses a thread spill registers (72 of bf16,
-// 83 of fp32): 2048 rows of 16384 (bf16) take 231 us, the memory 78.
+// an element and the waits above stand beside it.  Rows past 8192 elements spill registers (72 in bf16, 83 in
+// fp32; from 5128 on 11 in bf16): 2048 rows of 16384 (bf16) take 231 us, the memory 78.
 template <typename T, int NT, int CH, int RG>
 __global__ __launch_bounds__(NT *RG) void block_norm_grad_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
