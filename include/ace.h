@@ -32,7 +32,7 @@
 extern "C" {
 #endif
 
-#define ACE_ABI_VERSION 6
+#define ACE_ABI_VERSION 7
 
 typedef enum {
   ACE_OK = 0,
@@ -300,6 +300,40 @@ ace_status ace_grouped_matmul_grad_x(const ace_grouped_desc *desc, const void *d
 ace_status ace_grouped_matmul_grad_w(const ace_grouped_desc *desc, const void *dy, const void *x,
                                      const int32_t *offsets, void *dw, void *workspace, size_t workspace_bytes,
                                      void *stream);
+
+/*
+ * The gated feed-forward block of the experts, grouped as above, over w_gate and w_up [N, M, K] and x [S, K]:
+ *   g[r] = w_gate[e] x[r],  u[r] = w_up[e] x[r],  a[r] = act(g[r]) * u[r]   for every row r of group e
+ * act is SiLU, g / (1 + exp(-g)), or GELU, g Phi(g) with the normal distribution's Phi (not its tanh approximation).
+ * g and u [S, M] are kept where both are given (NULL, NULL: not); a comes from their sums before that rounding.
+ * ace_grouped_gated_grad takes da [S, M] and writes
+ *   dg = da u act'(g),  du = da act(g)                    (rounded to dtype, in the workspace)
+ *   dx[r] = w_gate[e]^T dg[r] + w_up[e]^T du[r]
+ *   dw_gate[e] = sum over the rows r of e: dg[r] x[r]^T,  dw_up[e] alike with du   (0 for an empty group)
+ * from the kept g and u, or (NULL, NULL) from both projections computed again.  dw_gate and dw_up may both be NULL:
+ * not asked for (x is then read only without g and u).  Rows of no group: as for the products above, in a, g, u and dx.
+ * Empty calls (S = 0) write the zeros of dw_gate and dw_up.  Limits as for the products.
+ *   workspace  DEVICE scratch of ace_grouped_gated_workspace_size(desc) or ace_grouped_gated_grad_workspace_size(desc,
+ *              kept, weights) bytes (kept: g and u are given, weights: dw_gate and dw_up are), 256-byte aligned (may
+ *              be NULL when that is 0).
+ */
+typedef enum { ACE_ACT_SILU = 0, ACE_ACT_GELU = 1 } ace_activation;
+typedef struct {
+  int32_t S;          /* rows (0 is allowed) */
+  int32_t N;          /* groups */
+  int32_t M, K;       /* features of g, u and a; of x */
+  int32_t dtype;      /* ace_dtype of every array */
+  int32_t activation; /* ace_activation */
+  uint32_t flags;     /* 0 or ACE_ZERO_REST */
+} ace_gated_desc;
+size_t ace_grouped_gated_workspace_size(const ace_gated_desc *desc);
+ace_status ace_grouped_gated(const ace_gated_desc *desc, const void *x, const void *w_gate, const void *w_up,
+                             const int32_t *offsets, void *a, void *g, void *u, void *workspace,
+                             size_t workspace_bytes, void *stream);
+size_t ace_grouped_gated_grad_workspace_size(const ace_gated_desc *desc, int kept, int weights);
+ace_status ace_grouped_gated_grad(const ace_gated_desc *desc, const void *da, const void *x, const void *w_gate,
+                                  const void *w_up, const int32_t *offsets, const void *g, const void *u, void *dx,
+                                  void *dw_gate, void *dw_up, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * The RMSNorms after a block and before the next one, fused with the block's gate and the

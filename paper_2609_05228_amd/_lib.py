@@ -27,6 +27,7 @@ ACE_WRITE_SCORES = 1 << 1
 ACE_FUSION_SHIFT = 2
 ACE_ZERO_REST = 1 << 0
 GROUPED_FORWARD, GROUPED_GRAD_X, GROUPED_GRAD_W = 0, 1, 2  # ace_grouped_way
+ACTIVATIONS = {"silu": 0, "gelu": 1}  # ace_activation
 # contribution rules (ace_fusion): ACE's max rule and the ablation variants
 FUSIONS = {"max": 0, "min": 1, "mean": 2, "gsp": 3, "rcr": 4, "score": 5}
 
@@ -52,6 +53,10 @@ class Outputs(ctypes.Structure):
 
 class GroupedDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("S", "N", "M", "K", "dtype")] + [("flags", ctypes.c_uint32)]
+
+
+class GatedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("S", "N", "M", "K", "dtype", "activation")] + [("flags", ctypes.c_uint32)]
 
 
 class NormDesc(ctypes.Structure):
@@ -130,6 +135,14 @@ def lib() -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         L.ace_grouped_workspace_size.argtypes = [ctypes.POINTER(GroupedDesc), ctypes.c_int]
         L.ace_grouped_workspace_size.restype = ctypes.c_size_t
+        L.ace_grouped_gated_workspace_size.argtypes = [ctypes.POINTER(GatedDesc)]
+        L.ace_grouped_gated_workspace_size.restype = ctypes.c_size_t
+        L.ace_grouped_gated.argtypes = [ctypes.POINTER(GatedDesc)] + [vp] * 8 + [ctypes.c_size_t, vp]
+        L.ace_grouped_gated.restype = ctypes.c_int
+        L.ace_grouped_gated_grad_workspace_size.argtypes = [ctypes.POINTER(GatedDesc), ctypes.c_int, ctypes.c_int]
+        L.ace_grouped_gated_grad_workspace_size.restype = ctypes.c_size_t
+        L.ace_grouped_gated_grad.argtypes = [ctypes.POINTER(GatedDesc)] + [vp] * 11 + [ctypes.c_size_t, vp]
+        L.ace_grouped_gated_grad.restype = ctypes.c_int
         L.ace_block_norm.argtypes = [ctypes.POINTER(NormDesc), ctypes.POINTER(NormInputs), vp, vp, vp]
         L.ace_block_norm.restype = ctypes.c_int
         L.ace_block_norm_grad_workspace_size.argtypes = [ctypes.POINTER(NormDesc)]

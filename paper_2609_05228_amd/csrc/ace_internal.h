@@ -228,10 +228,35 @@ struct GroupedArgs {
   int splits;   // parts of the reduction, and their fp32 sums [splits, out's elements] (a group's, for the weights)
   int chunk;    // weights' gradient: most rows of a part
   float *part;  // grouped_workspace_bytes
+  const void *rows2;  // weights' gradient of a gated block: the second matrix's dy,
+  void *out2;         // and its dw; null: there is no second one
 };
 size_t grouped_workspace_bytes(const GroupedArgs &g, bool weights, bool grad, bool bf16);
 hipError_t launch_grouped_rows(const GroupedArgs &g, bool grad, bool bf16, hipStream_t stream);
 hipError_t launch_grouped_weights(const GroupedArgs &g, bool bf16, hipStream_t stream);
+// adds up the parts of a result [S, cols]
+hipError_t launch_grouped_join(const GroupedArgs &g, int cols, bool bf16, hipStream_t stream);
+
+// The gated feed-forward block (gated.hip); null pointers: not asked for
+constexpr int kActSilu = 0, kActGelu = 1;
+struct GatedArgs {
+  const void *x, *w_gate, *w_up;  // [S, K], [N, M, K]
+  const int32_t *offsets;         // [N + 1]
+  int S, N, M, K;
+  int act, fill;
+  void *a, *g, *u;       // [S, M]: forward's results (g and u: kept); the gradient of kept ones reads g and u
+  const void *da;        // [S, M]: gradient
+  void *dg, *du;         // [S, M]: between its launches
+  void *dx;              // [S, K]
+  int splits;            // parts of the reduction, and their fp32 sums: of g and u [splits, 2, S, M], of dx [splits, S, K]
+  float *part;
+};
+size_t gated_part_bytes(const GatedArgs &g, bool bf16);
+size_t gated_grad_x_part_bytes(const GatedArgs &g, bool bf16);
+// both projections, and what the epilogue makes of them: a (and g, u), or with da, dg and du
+hipError_t launch_gated(GatedArgs g, bool bf16, hipStream_t stream);
+hipError_t launch_gated_slopes(GatedArgs g, bool bf16, hipStream_t stream);  // dg, du from kept g, u
+hipError_t launch_gated_grad_x(GatedArgs g, bool bf16, hipStream_t stream);
 
 // The norms before and after a block (block_norm.hip); null pointers: absent
 struct NormArgs {

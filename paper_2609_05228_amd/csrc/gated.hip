@@ -1,0 +1,424 @@
+// The gated feed-forward block of the experts, grouped by expert with ragged sizes, and its gradient:
+//   g[r] = w_gate[e] x[r],  u[r] = w_up[e] x[r],  a[r] = act(g[r]) * u[r]      for the rows r of group e
+//   dg = da * u * act'(g),  du = da * act(g)
+//   dx[r] = w_gate[e]^T dg[r] + w_up[e]^T du[r]
+//   dw_gate[e] = sum over the rows r of e: dg[r] x[r]^T, dw_up alike with du
+// act is SiLU, g / (1 + e^-g), or GELU, g Phi(g) with the normal distribution's Phi.
+//
+// Both projections are one tile (grouped_tile.h): its 16-column blocks alternate between
+// the two matrices, so a lane's accumulators hold g and u of the same four features and the
+// activation and the product happen in registers: x is read once, and g and u never leave the
+// chip unless they are kept.  The gradient takes dg and du either from the kept g and u, or in the
+// epilogue of the same product computed again; both are rounded to the tensors' type there,
+// since the two products behind them run on matrix cores of that type.  dx is one
+// product with a reduction of two segments (dg with w_gate, then du with w_up), summed in the same
+// accumulators and rounded once; both gradients of the weights are one launch, where the tiles of a group
+// share its rows of x in an XCD's L2.
+#include "grouped_tile.h"
+
+namespace ace {
+
+namespace {
+
+// exp(-z^2 / 2) for 0 <= z <= 20 to about 2^-23: the hardware base-2 exponential, with what z^2 and its
+// product with log2(e) / 2 lose to rounding put back to first order
+__device__ __forceinline__ float half_square_exp(float z) {
+  constexpr float c = 0.72134752f, c_rest = 8.3e-9f;  // log2(e) / 2 = c + c_rest
+  const float h = z * z, l = fmaf(z, z, -h), e = -c * h;
+  const float rest = -fmaf(c, h, e) - c * l - c_rest * h;
+  return __builtin_amdgcn_exp2f(e) * fmaf(rest, 0.69314718f, 1.f);
+}
+
+// Phi(-z) e^(z^2 / 2) for z >= 0, which falls smoothly from 1/2 as 1 / (sqrt(2 pi) z): t P(t) with t = 1 / (1 + 0.32 z)
+// and P a polynomial fitted to the least relative error (3.3e-8 over all z >= 0; 3e-7 with fp32 arithmetic)
+__device__ __forceinline__ float normal_tail(float z) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.32f, z, 1.f));
+  float p = -0.0210784f;
+  p = fmaf(p, t, 0.095408306f);
+  p = fmaf(p, t, -0.14670941f);
+  p = fmaf(p, t, 0.06532997f);
+  p = fmaf(p, t, -0.009378675f);
+  p = fmaf(p, t, 0.058654312f);
+  p = fmaf(p, t, 0.087829046f);
+  p = fmaf(p, t, 0.11462236f);
+  p = fmaf(p, t, 0.12766095f);
+  p = fmaf(p, t, 0.12766153f);
+  return p * t;
+}
+
+// act(g), and with SLOPE act'(g).  SiLU of bf16 results: hardware exponential and reciprocal (see silu_for_bf16).
+template <typename T, int ACT> struct Activation {
+  static __device__ __forceinline__ float value(float g) {
+    float s;
+    return both<false>(g, s);
+  }
+  template <bool SLOPE> static __device__ __forceinline__ float both(float g, float &slope) {
+    if constexpr (ACT == kActSilu) {
+      const float s = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f))
+                                     : 1.f / (1.f + expf(-g));
+      if (SLOPE) slope = s * fmaf(g, 1.f - s, 1.f);
+      return g * s;
+    } else {
+      const float z = fminf(fabsf(g), 20.f);  // Phi(-20) is 0 in fp32
+      const float e = half_square_exp(z), tail = e * normal_tail(z), phi = g < 0.f ? tail : 1.f - tail;
+      if (SLOPE) slope = fmaf(g * 0.39894228f, e, phi);
+      return g * phi;
+    }
+  }
+};
+
+// 4 consecutive elements of a row
+__device__ __forceinline__ void load4(const float *p, f32x4_t &v) { v = *reinterpret_cast<const f32x4_t *>(p); }
+__device__ __forceinline__ void load4(const bf16_t *p, f32x4_t &v) {
+  const uint2 b = *reinterpret_cast<const uint2 *>(p);
+  v = f32x4_t{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16),
+              __uint_as_float(b.y & 0xffff0000u)};
+}
+__device__ __forceinline__ void store4(float *p, f32x4_t v) { *reinterpret_cast<f32x4_t *>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t *p, f32x4_t v) {
+  *reinterpret_cast<uint2 *>(p) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+
+// a tile of both projections
+template <class S> struct GatedRef : S::Ref {
+  size_t at;  // its first element in g, u, a, da, dg and du
+};
+
+// A wave's share of g and u: what is asked of them, a 16-row block at a time (the whole share at once would hold
+// a second copy of the accumulators)
+template <typename T, bool LINES, class S> struct GatedStore {
+  const GatedArgs &g;
+  static constexpr int NH = S::NW / 2;
+  typedef f32x4_t Block[1][NH];
+
+  __device__ __forceinline__ void put(const GatedRef<S> &t, void *out, const Block &v, int blk, int c0, int lane) const {
+    store_rows<T, LINES, 1, NH, 1>(static_cast<T *>(out) + t.at, t.rows, t.cols, g.M, v, blk, c0, lane);
+  }
+  // dg into the place of g, du into that of u
+  template <int ACT>
+  __device__ __forceinline__ void slopes(const GatedRef<S> &t, Block &vg, Block &vu, int blk, int c0, int lane) const {
+    const int row = 16 * blk + (lane & 15), l4 = lane >> 4;
+    const T *p = static_cast<const T *>(g.da) + t.at + static_cast<size_t>(row) * g.M;
+    f32x4_t da[NH];
+#pragma unroll
+    for (int j = 0; j < NH; ++j) {
+      const int col = c0 + (sizeof(T) == 2 ? 16 * (j & ~1) + 8 * l4 + 4 * (j & 1) : 16 * j + 4 * l4);
+      da[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (row < t.rows && col < t.cols) load4(p + col, da[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NH; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float slope;
+        const float f = Activation<T, ACT>::template both<true>(vg[0][j][q], slope);
+        vg[0][j][q] = da[j][q] * vu[0][j][q] * slope;
+        vu[0][j][q] = da[j][q] * f;
+      }
+  }
+  template <int ACT> __device__ __forceinline__ void values(Block &vg, const Block &vu) const {
+#pragma unroll
+    for (int j = 0; j < NH; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) vg[0][j][q] = Activation<T, ACT>::value(vg[0][j][q]) * vu[0][j][q];
+  }
+
+  __device__ __forceinline__ void operator()(const GatedRef<S> &t, const f32x4_t (&sum)[S::MW][S::NW], int wr, int wc,
+                                             int lane) const {
+    const int c0 = 8 * wc * S::NW;
+#pragma unroll
+    for (int i = 0; i < S::MW; ++i) {
+      const int blk = wr + S::WR * i;
+      if (16 * blk >= t.rows) break;  // wave-uniform
+      Block vg, vu;
+#pragma unroll
+      for (int j = 0; j < NH; ++j) {
+        vg[0][j] = sum[i][2 * j];
+        vu[0][j] = sum[i][2 * j + 1];
+      }
+      if (t.part) {
+        store_part<T, 1, NH, 1>(t.part, t.rows, t.cols, g.M, vg, blk, c0, lane);
+        store_part<T, 1, NH, 1>(t.part + static_cast<size_t>(g.S) * g.M, t.rows, t.cols, g.M, vu, blk, c0, lane);
+      } else if (g.da) {
+        if (g.act == kActSilu)
+          slopes<kActSilu>(t, vg, vu, blk, c0, lane);
+        else
+          slopes<kActGelu>(t, vg, vu, blk, c0, lane);
+        put(t, g.dg, vg, blk, c0, lane);
+        put(t, g.du, vu, blk, c0, lane);
+      } else {
+        if (g.g) {
+          put(t, g.g, vg, blk, c0, lane);
+          put(t, g.u, vu, blk, c0, lane);
+        }
+        if (g.act == kActSilu)
+          values<kActSilu>(vg, vu);
+        else
+          values<kActGelu>(vg, vu);
+        put(t, g.a, vg, blk, c0, lane);
+      }
+    }
+  }
+};
+
+// Both projections in tiles of 16 MB rows of one group x 8 NB features: the whole work of a workgroup
+template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
+__device__ __forceinline__ void gated_rows(const GatedArgs &g, const RaggedTiles &tiles, uint8_t *smem) {
+  using S = DenseTile<T, false, false, MB, NB, WR, WC, DA, DB, 2>;
+  static_assert(sizeof(T) == 4 || S::NW % 4 == 0, "a wave holds whole pairs of feature blocks");
+  constexpr int BF = 8 * NB;
+  const int nN = (g.M + BF - 1) / BF, per = nN * g.splits;
+  const Share share(static_cast<long long>(tiles.total) * per);
+  auto ref = [&](const Item &it, int) {
+    const int f0 = it.tile * BF;
+    const Part k = part_of<T>(it.group < 0 ? 0 : g.K, it.split, g.splits);
+    const size_t w = (static_cast<size_t>(max(it.group, 0)) * g.M + f0) * g.K + k.k0;
+    GatedRef<S> t;
+    t.a.p[0] = static_cast<const T *>(g.x) + static_cast<size_t>(it.row0) * g.K + k.k0;
+    t.b.p[0] = static_cast<const T *>(g.w_gate) + w;
+    t.b.p[1] = static_cast<const T *>(g.w_up) + w;
+    t.at = static_cast<size_t>(it.row0) * g.M + f0;
+    t.out = nullptr;
+    t.part = g.splits > 1 ? g.part + 2 * static_cast<size_t>(it.split) * g.S * g.M + t.at : nullptr;
+    t.rows = it.rows;
+    t.cols = min(BF, g.M - f0);
+    t.klen = k.len;
+    t.rot = max(it.group, 0);
+    t.once = it.once;
+    return t;
+  };
+  long long done = 0;
+  for (int n; (n = share.count(done)) > 0; done += n) {
+    const long long i = share.item(done);
+    const RaggedTile t = tiles.find(static_cast<int>(i / per));
+    const int q = static_cast<int>(i % per);
+    __syncthreads();  // every wave is done with the rings
+    grouped_items<S>(Item{t.group, t.row0, t.rows, q % nN, t.only, q / nN}, n, g.K, g.K, smem, ref,
+                     GatedStore<T, LINES, S>{g});
+  }
+}
+
+template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
+__global__ __launch_bounds__(WR *WC * 64) void gated_rows_kernel(GatedArgs g) {
+  __shared__ __align__(16) uint8_t smem[(DA * MB + DB * NB) * 2 * kUnitBytes];
+  gated_rows<T, LINES, MB, NB, WR, WC, DA, DB>(g, RaggedTiles(g.offsets, g.N, g.S, 16 * MB, g.fill), smem);
+}
+
+// What the epilogue does, from the fp32 parts of g and u (summed in order) or the kept g and u: 4 features a thread.
+// Rows of no group: zeros into a, g and u with `fill`, else they stay (dg and du of them are never read).
+template <typename T, int ACT> __global__ __launch_bounds__(256) void gated_join_kernel(GatedArgs g) {
+  const size_t total = static_cast<size_t>(g.S) * g.M;
+  const int r0 = min(max(g.offsets[0], 0), g.S);
+  const size_t first = static_cast<size_t>(r0) * g.M, last = static_cast<size_t>(min(max(g.offsets[g.N], r0), g.S)) * g.M;
+  for (size_t i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * 4; i < total;
+       i += static_cast<size_t>(gridDim.x) * 256 * 4) {
+    f32x4_t vg{0.f, 0.f, 0.f, 0.f}, vu = vg;
+    if (i >= first && i < last) {
+      if (g.splits > 1) {
+        for (int s = 0; s < g.splits; ++s) {
+          const float *p = g.part + 2 * s * total + i;
+          const f32x4_t a = *reinterpret_cast<const f32x4_t *>(p), b = *reinterpret_cast<const f32x4_t *>(p + total);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            vg[q] += a[q];
+            vu[q] += b[q];
+          }
+        }
+      } else {
+        load4(static_cast<const T *>(g.g) + i, vg);
+        load4(static_cast<const T *>(g.u) + i, vu);
+      }
+    } else if (!g.fill) {
+      continue;
+    }
+    f32x4_t f, slope;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float d;
+      f[q] = Activation<T, ACT>::template both<true>(vg[q], d);
+      slope[q] = d;
+    }
+    if (g.da) {
+      f32x4_t da, dg, du;
+      load4(static_cast<const T *>(g.da) + i, da);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        dg[q] = da[q] * vu[q] * slope[q];
+        du[q] = da[q] * f[q];
+      }
+      store4(static_cast<T *>(g.dg) + i, dg);
+      store4(static_cast<T *>(g.du) + i, du);
+      continue;
+    }
+    if (g.g) {
+      store4(static_cast<T *>(g.g) + i, vg);
+      store4(static_cast<T *>(g.u) + i, vu);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f[q] *= vu[q];
+    store4(static_cast<T *>(g.a) + i, f);
+  }
+}
+
+// dx: tiles of 16 MB rows x 16 NB columns, reduced over the features of the gate, then of the up projection
+template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
+__global__ __launch_bounds__(WR *WC * 64) void gated_grad_x_kernel(GatedArgs g) {
+  using S = DenseTile<T, false, true, MB, NB, WR, WC, DA, DB, 1, 2>;
+  constexpr int BN = 16 * NB;
+  __shared__ __align__(16) uint8_t smem[(DA * MB + DB * NB) * 2 * kUnitBytes];
+  const RaggedTiles tiles(g.offsets, g.N, g.S, 16 * MB, g.fill);
+  const int nN = (g.K + BN - 1) / BN, per = nN * g.splits;
+  const Share share(static_cast<long long>(tiles.total) * per);
+  auto ref = [&](const Item &it, int seg) {
+    const int c0 = it.tile * BN;
+    const Part k = part_of<T>(it.group < 0 ? 0 : g.M, it.split, g.splits);
+    typename S::Ref t;
+    t.a.p[0] = static_cast<const T *>(seg ? g.du : g.dg) + static_cast<size_t>(it.row0) * g.M + k.k0;
+    t.b.p[0] = static_cast<const T *>(seg ? g.w_up : g.w_gate) +
+               (static_cast<size_t>(max(it.group, 0)) * g.M + k.k0) * g.K + c0;
+    t.out = static_cast<T *>(g.dx) + static_cast<size_t>(it.row0) * g.K + c0;
+    t.part = g.splits > 1 ? g.part + (static_cast<size_t>(it.split) * g.S + it.row0) * g.K + c0 : nullptr;
+    t.rows = it.rows;
+    t.cols = min(BN, g.K - c0);
+    t.klen = k.len;
+    t.rot = max(it.group, 0);
+    t.once = it.once;
+    return t;
+  };
+  long long done = 0;
+  for (int n; (n = share.count(done)) > 0; done += n) {
+    const long long i = share.item(done);
+    const RaggedTile t = tiles.find(static_cast<int>(i / per));
+    const int q = static_cast<int>(i % per);
+    __syncthreads();  // every wave is done with the rings
+    grouped_items<S>(Item{t.group, t.row0, t.rows, q % nN, t.only, q / nN}, n, g.M, g.K, smem, ref,
+                     StoreTile<T, LINES, S>{static_cast<size_t>(g.K)});
+  }
+}
+
+using Gated64 = TileShape<4, 4, 4, 1, 4, 4>;     // bf16: few tiles, deep rings
+using GradX64 = TileShape<4, 4, 2, 2, 4, 4>;
+using Gated64x128 = TileShape<4, 8, 2, 2, 3, 3>;  // bf16: a few rows a group
+using Gated128 = TileShape<8, 8, 2, 2, 2, 3>;     // bf16
+using Gated256 = TileShape<16, 16, 4, 2, 2, 3>;   // bf16
+using GatedF32 = TileShape<2, 4, 2, 2, 3, 3>;     // fp32
+
+enum class Kind { k64, k64x128, k128, k256, kF32 };
+struct Plan {
+  Kind kind;
+  int splits;
+};
+
+// Kernel and parts of the reduction for S rows in N groups by `cols` columns (both projections' features, or dx's), over
+// klen, with `elems` sums in a part
+Plan plan_rows(long long S, long long N, int cols, long long klen, size_t elems, bool bf16) {
+  if (!bf16) {
+    const long long items = about_tiles(S, N, GatedF32::TM) * tiles_of(cols, GatedF32::TN);
+    return {Kind::kF32, pick_splits(items, kCUs * GatedF32::PER_CU, tiles_of(klen, 32), elems, 0.6)};
+  }
+  const long long small = about_tiles(S, N, Gated64::TM) * tiles_of(cols, Gated64::TN);
+  if (small <= kCUs * Gated64::PER_CU)
+    return {Kind::k64, pick_splits(small, kCUs * Gated64::PER_CU, tiles_of(klen, 64), elems, 0.45)};
+  if (S <= 32 * N) return {Kind::k64x128, 1};
+  const long long items = about_tiles(S, N, Gated128::TM) * tiles_of(cols, Gated128::TN);
+  const bool large = S > 80 * N && items >= kCUs * Gated128::PER_CU;
+  return {large ? Kind::k256 : Kind::k128, 1};
+}
+Plan plan_gated(const GatedArgs &g, bool bf16) {
+  return plan_rows(g.S, g.N, 2 * g.M, g.K, 2 * static_cast<size_t>(g.S) * g.M, bf16);
+}
+Plan plan_grad_x(const GatedArgs &g, bool bf16) {
+  return plan_rows(g.S, g.N, g.K, 2ll * g.M, static_cast<size_t>(g.S) * g.K, bf16);
+}
+
+bool lines(const void *p) { return reinterpret_cast<uintptr_t>(p) % 128 == 0; }
+
+template <typename T, class Sh> void launch_gated_shape(const GatedArgs &g, hipStream_t s) {
+  const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(g.M, Sh::TN / 2) * g.splits;
+  auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g); };
+  const bool whole = g.M * sizeof(T) % 128 == 0 && lines(g.a) && lines(g.g) && lines(g.u) && lines(g.dg) && lines(g.du);
+  if (whole)
+    launch(gated_rows_kernel<T, true, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+  else
+    launch(gated_rows_kernel<T, false, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+}
+
+template <typename T, class Sh> void launch_grad_x_shape(const GatedArgs &g, hipStream_t s) {
+  const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(g.K, Sh::TN) * g.splits;
+  auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g); };
+  if (g.K * sizeof(T) % 128 == 0 && lines(g.dx))
+    launch(gated_grad_x_kernel<T, true, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+  else
+    launch(gated_grad_x_kernel<T, false, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+}
+
+hipError_t launch_gated_join(const GatedArgs &g, bool bf16, hipStream_t s) {
+  const size_t blocks = (static_cast<size_t>(g.S) * g.M / 4 + 255) / 256;
+  const unsigned grid = static_cast<unsigned>(std::min<size_t>(std::max<size_t>(blocks, 1), 8 * kCUs));
+  auto launch = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(g); };
+  if (bf16)
+    g.act == kActSilu ? launch(gated_join_kernel<bf16_t, kActSilu>) : launch(gated_join_kernel<bf16_t, kActGelu>);
+  else
+    g.act == kActSilu ? launch(gated_join_kernel<float, kActSilu>) : launch(gated_join_kernel<float, kActGelu>);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t gated_part_bytes(const GatedArgs &g, bool bf16) {
+  const int n = g.S > 0 ? plan_gated(g, bf16).splits : 1;
+  return n > 1 ? 2 * n * static_cast<size_t>(g.S) * g.M * sizeof(float) : 0;
+}
+
+size_t gated_grad_x_part_bytes(const GatedArgs &g, bool bf16) {
+  const int n = g.S > 0 ? plan_grad_x(g, bf16).splits : 1;
+  return n > 1 ? n * static_cast<size_t>(g.S) * g.K * sizeof(float) : 0;
+}
+
+hipError_t launch_gated(GatedArgs g, bool bf16, hipStream_t s) {
+  if (g.S <= 0) return hipSuccess;
+  const Plan p = plan_gated(g, bf16);
+  g.splits = p.splits;
+  switch (p.kind) {
+    case Kind::k64: launch_gated_shape<bf16_t, Gated64>(g, s); break;
+    case Kind::k64x128: launch_gated_shape<bf16_t, Gated64x128>(g, s); break;
+    case Kind::k128: launch_gated_shape<bf16_t, Gated128>(g, s); break;
+    case Kind::k256: launch_gated_shape<bf16_t, Gated256>(g, s); break;
+    case Kind::kF32: launch_gated_shape<float, GatedF32>(g, s); break;
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  return launch_gated_join(g, bf16, s);
+}
+
+hipError_t launch_gated_slopes(GatedArgs g, bool bf16, hipStream_t s) {
+  if (g.S <= 0) return hipSuccess;
+  g.splits = 1;
+  return launch_gated_join(g, bf16, s);
+}
+
+hipError_t launch_gated_grad_x(GatedArgs g, bool bf16, hipStream_t s) {
+  if (g.S <= 0) return hipSuccess;
+  const Plan p = plan_grad_x(g, bf16);
+  g.splits = p.splits;
+  switch (p.kind) {
+    case Kind::k64: launch_grad_x_shape<bf16_t, GradX64>(g, s); break;
+    case Kind::k64x128: launch_grad_x_shape<bf16_t, Gated64x128>(g, s); break;
+    case Kind::k128: launch_grad_x_shape<bf16_t, Gated128>(g, s); break;
+    case Kind::k256: launch_grad_x_shape<bf16_t, Gated256>(g, s); break;
+    case Kind::kF32: launch_grad_x_shape<float, GatedF32>(g, s); break;
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  GroupedArgs j{};
+  j.out = g.dx;
+  j.offsets = g.offsets;
+  j.S = g.S;
+  j.N = g.N;
+  j.fill = g.fill;
+  j.splits = p.splits;
+  j.part = g.part;
+  return launch_grouped_join(j, g.K, bf16, s);
+}
+
+}  // namespace ace

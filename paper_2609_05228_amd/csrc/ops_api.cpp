@@ -1,8 +1,9 @@
-// C ABI of the operators around the layer (grouped matrix products, the norms before and
-// after a block, low-rank adapters): host-side validation, then the launches.  Nothing is
+// C ABI of the operators around the layer (grouped matrix products, the gated feed-forward block, the norms
+// before and after a block, low-rank adapters): host-side validation, then the launches.  Nothing is
 // allocated and no call keeps state.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -92,6 +93,58 @@ ace_status grouped(const ace_grouped_desc *d, Way way, const void *rows, const v
                       : ace::launch_grouped_rows(g, way == Way::kGradX, bf16, s));
 }
 
+ace_status gated_desc(const ace_gated_desc *d) {
+  if (!d || (d->activation != ACE_ACT_SILU && d->activation != ACE_ACT_GELU)) return ACE_ERR_INVALID_ARG;
+  const ace_grouped_desc g{d->S, d->N, d->M, d->K, d->dtype, d->flags};
+  return grouped_desc(&g);
+}
+
+ace::GatedArgs gated_args(const ace_gated_desc &d) {
+  ace::GatedArgs g{};
+  g.S = d.S;
+  g.N = d.N;
+  g.M = d.M;
+  g.K = d.K;
+  g.act = d.activation == ACE_ACT_SILU ? ace::kActSilu : ace::kActGelu;
+  g.fill = (d.flags & ACE_ZERO_REST) ? 1 : 0;
+  return g;
+}
+
+// the weights' gradients as the grouped products have them
+ace::GroupedArgs gated_weights_args(const ace_gated_desc &d, const void *dg, const void *du, const void *x,
+                                    const int32_t *offsets, void *dw_gate, void *dw_up, float *part) {
+  ace::GroupedArgs g{};
+  g.rows = dg;
+  g.rows2 = du;
+  g.other = x;
+  g.out = dw_gate;
+  g.out2 = dw_up;
+  g.offsets = offsets;
+  g.S = d.S;
+  g.N = d.N;
+  g.M = d.M;
+  g.K = d.K;
+  g.part = part;
+  return g;
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// dg and du, then the largest of the launches' partial sums
+size_t gated_slope_bytes(const ace_gated_desc &d) { return up256(elem_bytes(d.dtype) * d.S * d.M); }
+size_t gated_grad_bytes(const ace_gated_desc &d, bool kept, bool weights) {
+  const bool bf16 = d.dtype == ACE_BF16;
+  const ace::GatedArgs g = gated_args(d);
+  size_t part = ace::gated_grad_x_part_bytes(g, bf16);
+  if (!kept) part = std::max(part, ace::gated_part_bytes(g, bf16));
+  if (weights) {
+    char ws[1];  // any place: it says that there are two matrices
+    const ace::GroupedArgs w = gated_weights_args(d, nullptr, nullptr, nullptr, nullptr, ws, ws, nullptr);
+    part = std::max(part, ace::grouped_workspace_bytes(w, true, false, bf16));
+  }
+  return 2 * gated_slope_bytes(d) + part;
+}
+
 ace_status norm_desc(const ace_norm_desc *d) {
   if (!d) return ACE_ERR_INVALID_ARG;
   if (d->T < 0 || d->d <= 0 || !is_dtype(d->dtype) || d->gate_kind < ACE_GATE_NONE || d->gate_kind > ACE_GATE_FULL)
@@ -150,6 +203,17 @@ bool bad_alias(const Span &out, const Span &in, bool may_equal) {
   return overlap(out, in) && !(may_equal && out.p == in.p && out.bytes == in.bytes);
 }
 
+// a result on an input, or on another result
+bool any_overlap(const Span *outs, int n_out, const Span *ins, int n_in) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j)
+      if (overlap(outs[i], ins[j])) return true;
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], outs[j])) return true;
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -174,6 +238,98 @@ ace_status ace_grouped_matmul_grad_w(const ace_grouped_desc *desc, const void *d
                                      const int32_t *offsets, void *dw, void *workspace, size_t workspace_bytes,
                                      void *stream) {
   return grouped(desc, Way::kGradW, dy, x, offsets, dw, workspace, workspace_bytes, stream);
+}
+
+size_t ace_grouped_gated_workspace_size(const ace_gated_desc *desc) {
+  if (gated_desc(desc) != ACE_OK) return 0;
+  return ace::gated_part_bytes(gated_args(*desc), desc->dtype == ACE_BF16);
+}
+
+ace_status ace_grouped_gated(const ace_gated_desc *desc, const void *x, const void *w_gate, const void *w_up,
+                             const int32_t *offsets, void *a, void *g, void *u, void *workspace,
+                             size_t workspace_bytes, void *stream) {
+  const ace_status st = gated_desc(desc);
+  if (st != ACE_OK) return st;
+  const ace_gated_desc &d = *desc;
+  if (d.S == 0) return ACE_OK;
+  for (const void *p : {x, w_gate, w_up, static_cast<const void *>(a)})
+    if (!usable(p, 16)) return ACE_ERR_INVALID_ARG;
+  if (!usable(offsets, 4) || (g != nullptr) != (u != nullptr) || (g && (!usable(g, 16) || !usable(u, 16))))
+    return ACE_ERR_INVALID_ARG;
+  const size_t es = elem_bytes(d.dtype), S = d.S, M = d.M, K = d.K, w = es * d.N * M * K, f = es * S * M;
+  const Span outs[] = {{a, f}, {g, f}, {u, f}};
+  const Span ins[] = {{x, es * S * K}, {w_gate, w}, {w_up, w}, {offsets, (d.N + 1u) * size_t{4}}};
+  if (any_overlap(outs, 3, ins, 4)) return ACE_ERR_INVALID_ARG;
+  const size_t need = ace_grouped_gated_workspace_size(desc);
+  if (need > 0 && (!usable(workspace, 256) || workspace_bytes < need)) return ACE_ERR_WORKSPACE;
+  ace::GatedArgs p = gated_args(d);
+  p.x = x;
+  p.w_gate = w_gate;
+  p.w_up = w_up;
+  p.offsets = offsets;
+  p.a = a;
+  p.g = g;
+  p.u = u;
+  p.part = static_cast<float *>(workspace);
+  return status_of(ace::launch_gated(p, d.dtype == ACE_BF16, static_cast<hipStream_t>(stream)));
+}
+
+size_t ace_grouped_gated_grad_workspace_size(const ace_gated_desc *desc, int kept, int weights) {
+  if (gated_desc(desc) != ACE_OK) return 0;
+  return gated_grad_bytes(*desc, kept != 0, weights != 0);
+}
+
+ace_status ace_grouped_gated_grad(const ace_gated_desc *desc, const void *da, const void *x, const void *w_gate,
+                                  const void *w_up, const int32_t *offsets, const void *g, const void *u, void *dx,
+                                  void *dw_gate, void *dw_up, void *workspace, size_t workspace_bytes, void *stream) {
+  const ace_status st = gated_desc(desc);
+  if (st != ACE_OK) return st;
+  const ace_gated_desc &d = *desc;
+  const bool kept = g != nullptr, weights = dw_gate != nullptr, bf16 = d.dtype == ACE_BF16;
+  if (kept != (u != nullptr) || weights != (dw_up != nullptr)) return ACE_ERR_INVALID_ARG;
+  if (d.S == 0 && !weights) return ACE_OK;
+  if (!usable(offsets, 4) || (weights && (!usable(dw_gate, 16) || !usable(dw_up, 16)))) return ACE_ERR_INVALID_ARG;
+  if (d.S > 0) {
+    for (const void *p : {da, w_gate, w_up, static_cast<const void *>(dx)})
+      if (!usable(p, 16)) return ACE_ERR_INVALID_ARG;
+    if ((weights || !kept) && !x) return ACE_ERR_INVALID_ARG;
+    for (const void *p : {x, g, u})
+      if (p && !usable(p, 16)) return ACE_ERR_INVALID_ARG;
+  }
+  const size_t es = elem_bytes(d.dtype), S = d.S, M = d.M, K = d.K, w = es * d.N * M * K, f = es * S * M;
+  const Span outs[] = {{dx, es * S * K}, {dw_gate, w}, {dw_up, w}};
+  const Span ins[] = {{da, f}, {x, es * S * K}, {w_gate, w}, {w_up, w}, {g, f}, {u, f}, {offsets, (d.N + 1u) * size_t{4}}};
+  if (any_overlap(outs, 3, ins, 7)) return ACE_ERR_INVALID_ARG;
+  const size_t need = gated_grad_bytes(d, kept, weights);
+  if (need > 0 && (!usable(workspace, 256) || workspace_bytes < need)) return ACE_ERR_WORKSPACE;
+  const size_t slopes = gated_slope_bytes(d);
+  char *ws = static_cast<char *>(workspace);
+  ace::GatedArgs p = gated_args(d);
+  p.x = x;
+  p.w_gate = w_gate;
+  p.w_up = w_up;
+  p.offsets = offsets;
+  p.da = da;
+  p.dg = ws;
+  p.du = ws + slopes;
+  p.dx = dx;
+  p.part = reinterpret_cast<float *>(ws + 2 * slopes);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int fill = p.fill;
+  p.fill = 0;  // dg and du of rows of no group are never read
+  hipError_t e;
+  if (kept) {
+    p.g = const_cast<void *>(g);
+    p.u = const_cast<void *>(u);
+    e = ace::launch_gated_slopes(p, bf16, s);
+  } else {
+    e = ace::launch_gated(p, bf16, s);
+  }
+  if (e != hipSuccess) return status_of(e);
+  p.fill = fill;
+  e = ace::launch_gated_grad_x(p, bf16, s);
+  if (e != hipSuccess || !weights) return status_of(e);
+  return status_of(ace::launch_grouped_weights(gated_weights_args(d, p.dg, p.du, x, offsets, dw_gate, dw_up, p.part), bf16, s));
 }
 
 ace_status ace_block_norm(const ace_norm_desc *desc, const ace_norm_inputs *in, void *h_out, void *n_out,

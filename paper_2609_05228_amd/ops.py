@@ -151,6 +151,97 @@ def grouped_matmul_grad_w(dy, x, offsets, *, out=None):
                     ((S, M), (S, K)), out)
 
 
+def _activation(name):
+    if name not in _lib.ACTIVATIONS:
+        raise ValueError(f"activation {name!r} is none of {', '.join(_lib.ACTIVATIONS)}")
+    return _lib.ACTIVATIONS[name]
+
+
+def _scratch(n, dev):
+    return torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def grouped_gated(x, w_gate, w_up, offsets, *, activation="silu", keep=False, out=None):
+    """The gated feed-forward block of the experts in one kernel: a[r] = act(g[r]) * u[r] with
+    g[r] = w_gate[e] x[r] and u[r] = w_up[e] x[r] for the rows r of group e.
+
+    x        [S, K] bf16 or fp32 device tensor, rows in group order
+    w_gate, w_up  [N, M, K] weights of the groups (nn.Linear layout)
+    offsets  [N + 1] int32: group e owns rows offsets[e] .. offsets[e + 1] - 1, ascending
+             (the `offsets` of `moe_forward`'s plan; [0, S] for one block that takes every row)
+    activation  "silu", or "gelu" with the normal distribution's integral (not its tanh approximation)
+    keep     also return g and u, for `grouped_gated_grad`
+    out      None, or tensors in the shape of the result.  Rows of no group stay as they are in them; a fresh
+             result holds zeros there.
+    K and M are multiples of 8 (fp32: 4).  Returns a [S, M], with keep (a, (g, u))."""
+    dtype = _dtype_of("x", x, 2)
+    _dtype_of("w_gate", w_gate, 3)
+    act = _activation(activation)
+    N, M, K = w_gate.shape
+    S = x.shape[0]
+    dev, size = x.device, _sizes(S, N, M, K)
+    named = [("x", x, (S, K), None), ("w_gate", w_gate, (N, M, K), None), ("w_up", w_up, (N, M, K), None),
+             ("offsets", offsets, (N + 1,), torch.int32)]
+    flags = 0
+    if out is not None:
+        a, (g, u) = out if keep else (out, (None, None))
+        named += [(n, t, (S, M), None) for n, t in (("out", a), ("out's g", g), ("out's u", u)) if t is not None]
+    _check_all(dev, dtype, named)
+    if out is None:
+        a, g, u = (torch.empty((S, M), dtype=dtype, device=dev) if i == 0 or keep else None for i in range(3))
+        flags = _lib.ACE_ZERO_REST
+    desc = _lib.GatedDesc(*size, _DT[dtype], act, flags)
+    lib = _lib.lib()
+    n = lib.ace_grouped_gated_workspace_size(desc)
+    ws = _scratch(n, dev)
+    _enqueue(dev, lib.ace_grouped_gated, desc, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), offsets.data_ptr(),
+             a.data_ptr(), _ptr(g), _ptr(u), _ptr(ws), n)
+    return (a, (g, u)) if keep else a
+
+
+def grouped_gated_grad(da, x, w_gate, w_up, offsets, *, kept=None, activation="silu", weights=True):
+    """Gradients of `grouped_gated`.
+
+    da       [S, M]: gradient of the result a
+    x, w_gate, w_up, offsets, activation  as in the forward
+    kept     the forward's (g, u), or None: both projections are computed again, which takes as long as the
+             forward and no memory between the passes
+    weights  False: the weights are frozen, only x's gradient is computed (x may be None with kept)
+    Returns a dict of the gradients of x [S, K] (zeros in rows of no group) and, with weights, of w_gate and w_up
+    [N, M, K] (zeros for an empty group).  The gradients of g and u are rounded to the tensors' type between the
+    products; sums are fp32 in a fixed order."""
+    dtype = _dtype_of("da", da, 2)
+    _dtype_of("w_gate", w_gate, 3)
+    act = _activation(activation)
+    N, M, K = w_gate.shape
+    S = da.shape[0]
+    dev, size = da.device, _sizes(S, N, M, K)
+    g, u = (None, None) if kept is None else kept
+    _need(x is not None or (g is not None and not weights), "x is required with weights or without kept")
+    named = [("da", da, (S, M), None), ("w_gate", w_gate, (N, M, K), None), ("w_up", w_up, (N, M, K), None),
+             ("offsets", offsets, (N + 1,), torch.int32)]
+    if x is not None:
+        named.append(("x", x, (S, K), None))
+    if kept is not None:
+        named += [("kept's g", g, (S, M), None), ("kept's u", u, (S, M), None)]
+    _check_all(dev, dtype, named)
+    out = {"x": torch.empty((S, K), dtype=dtype, device=dev)}
+    if weights:
+        out["w_gate"], out["w_up"] = torch.empty_like(w_gate), torch.empty_like(w_up)
+    desc = _lib.GatedDesc(*size, _DT[dtype], act, _lib.ACE_ZERO_REST)
+    lib = _lib.lib()
+    n = lib.ace_grouped_gated_grad_workspace_size(desc, kept is not None, weights)
+    ws = _scratch(n, dev)
+    _enqueue(dev, lib.ace_grouped_gated_grad, desc, da.data_ptr(), _ptr(x), w_gate.data_ptr(), w_up.data_ptr(),
+             offsets.data_ptr(), _ptr(g), _ptr(u), out["x"].data_ptr(), _ptr(out.get("w_gate")), _ptr(out.get("w_up")),
+             _ptr(ws), n)
+    return out
+
+
 def _norm_call(lead, dtype, T, d, h, y, w_post, w_pre, gate, res_scale, branch_scale, eps, named):
     """Check a block_norm call's tensors, `named` among them; (desc, inputs)."""
     rows, vec, kind, size = (T, d), (d,), 0, _sizes(T, d)
