@@ -336,6 +336,55 @@ ace_status ace_grouped_gated_grad(const ace_gated_desc *desc, const void *da, co
                                   void *dw_gate, void *dw_up, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Microscaled 4-bit floating point: blocks of 32 consecutive numbers of a row, each a sign, two bits of exponent and
+ * one of mantissa (0, 0.5, 1, 1.5, 2, 3, 4, 6; codes 0 .. 7, 8 more with the sign), times one power of two per block.
+ *   codes  [rows, K / 2] bytes: number 2 i of a row in the low half of byte i, number 2 i + 1 in its high half;
+ *          16-byte aligned
+ *   scales [rows, 4 * ceil(K / 128)] bytes, 4-byte aligned: byte j is the scale 2^(byte - 127) of block j, 255: the
+ *          block stands for NaN; bytes from K / 32 on (rows are padded to four) mean nothing
+ * K is a multiple of 32, at most 65536.
+ *
+ * ace_mx4_quantize: the scale's exponent is floor(log2 of the block's largest magnitude) - 2, at least -127; each
+ * number over the scale goes to the nearest of the eight magnitudes (ties to the even code, above 6 to 6), zeros keep
+ * their sign.  A block that holds a NaN or an infinity gets scale 255 and codes 0.  Bytes of scales past K / 32 get 0.
+ * ace_mx4_dequantize: the numbers that codes and scales stand for, exactly in bf16 and fp32 (NaN where the scale is
+ * 255; beyond either type's largest, which scales from 253 on reach, infinity).
+ *   x [rows, K] dtype (ACE_F32 or ACE_BF16).  rows * ceil(K / 128) < 2^31, else ACE_ERR_UNSUPPORTED.
+ */
+ace_status ace_mx4_quantize(int64_t rows, int32_t K, int32_t dtype, const void *x, uint8_t *codes, uint8_t *scales,
+                            void *stream);
+ace_status ace_mx4_dequantize(int64_t rows, int32_t K, int32_t dtype, const uint8_t *codes, const uint8_t *scales,
+                              void *x, void *stream);
+
+/*
+ * The products grouped by expert and the gated block (forward) with weights in 4 bits:
+ *   ace_grouped_matmul_mx4  y[r] = w[e] x[r]
+ *   ace_grouped_gated_mx4   a[r] = act(w_gate[e] x[r]) * (w_up[e] x[r])
+ * w, w_gate, w_up: [N, M, K] numbers, i.e. N * M rows of the format.  x [S, K]: bf16 (x_scales NULL), multiplied with
+ * the weights' exact values, or 4-bit codes with x_scales.  y and a are bf16.  Sums are fp32.
+ * Rows of no group, limits and S = 0 as for ace_grouped_matmul; M is a multiple of 8, K of 32.
+ *   workspace  DEVICE scratch of ace_grouped_mx4_workspace_size(desc, gated) bytes, 256-byte aligned (may be NULL when
+ *              that is 0).
+ */
+typedef struct {
+  const uint8_t *codes, *scales; /* DEVICE */
+} ace_mx4;
+typedef struct {
+  int32_t S;          /* rows (0 is allowed) */
+  int32_t N;          /* groups */
+  int32_t M, K;       /* output and input features */
+  int32_t activation; /* ace_activation (of the gated block) */
+  uint32_t flags;     /* 0 or ACE_ZERO_REST */
+} ace_mx4_desc;
+size_t ace_grouped_mx4_workspace_size(const ace_mx4_desc *desc, int gated);
+ace_status ace_grouped_matmul_mx4(const ace_mx4_desc *desc, const void *x, const uint8_t *x_scales, const ace_mx4 *w,
+                                  const int32_t *offsets, void *y, void *workspace, size_t workspace_bytes,
+                                  void *stream);
+ace_status ace_grouped_gated_mx4(const ace_mx4_desc *desc, const void *x, const uint8_t *x_scales,
+                                 const ace_mx4 *w_gate, const ace_mx4 *w_up, const int32_t *offsets, void *a,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * The RMSNorms after a block and before the next one, fused with the block's gate and the
  * residual scale.  With rms(v) = sqrt(mean(v^2) + eps):
  *   u = y / rms(y) * w_post          (u = y without w_post)

@@ -26,6 +26,6 @@ from .layer import (  # noqa: F401
     PreparedForward, build_tables, make_desc, moe_forward, prepare_forward, tau_map, workspace,
 )
 from .ops import (  # noqa: F401
-    adapter_add, block_norm, block_norm_grad, grouped_gated, grouped_gated_grad, grouped_matmul, grouped_matmul_grad_w,
-    grouped_matmul_grad_x,
+    Mx4, adapter_add, block_norm, block_norm_grad, grouped_gated, grouped_gated_grad, grouped_matmul,
+    grouped_matmul_grad_w, grouped_matmul_grad_x, mx4_dequantize, mx4_quantize,
 )

@@ -59,6 +59,14 @@ class GatedDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("S", "N", "M", "K", "dtype", "activation")] + [("flags", ctypes.c_uint32)]
 
 
+class Mx4Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("S", "N", "M", "K", "activation")] + [("flags", ctypes.c_uint32)]
+
+
+class Mx4Ptr(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("codes", "scales")]
+
+
 class NormDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "dtype", "gate_kind")] + [
         (n, ctypes.c_float) for n in ("res_scale", "branch_scale", "eps")]
@@ -143,6 +151,17 @@ def lib() -> ctypes.CDLL:
         L.ace_grouped_gated_grad_workspace_size.restype = ctypes.c_size_t
         L.ace_grouped_gated_grad.argtypes = [ctypes.POINTER(GatedDesc)] + [vp] * 11 + [ctypes.c_size_t, vp]
         L.ace_grouped_gated_grad.restype = ctypes.c_int
+        for name in ("ace_mx4_quantize", "ace_mx4_dequantize"):
+            fn = getattr(L, name)
+            fn.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, vp, vp, vp, vp]
+            fn.restype = ctypes.c_int
+        L.ace_grouped_mx4_workspace_size.argtypes = [ctypes.POINTER(Mx4Desc), ctypes.c_int]
+        L.ace_grouped_mx4_workspace_size.restype = ctypes.c_size_t
+        mx4 = ctypes.POINTER(Mx4Ptr)
+        L.ace_grouped_matmul_mx4.argtypes = [ctypes.POINTER(Mx4Desc), vp, vp, mx4, vp, vp, vp, ctypes.c_size_t, vp]
+        L.ace_grouped_matmul_mx4.restype = ctypes.c_int
+        L.ace_grouped_gated_mx4.argtypes = [ctypes.POINTER(Mx4Desc), vp, vp, mx4, mx4, vp, vp, vp, ctypes.c_size_t, vp]
+        L.ace_grouped_gated_mx4.restype = ctypes.c_int
         L.ace_block_norm.argtypes = [ctypes.POINTER(NormDesc), ctypes.POINTER(NormInputs), vp, vp, vp]
         L.ace_block_norm.restype = ctypes.c_int
         L.ace_block_norm_grad_workspace_size.argtypes = [ctypes.POINTER(NormDesc)]

@@ -257,6 +257,26 @@ size_t gated_grad_x_part_bytes(const GatedArgs &g, bool bf16);
 hipError_t launch_gated(GatedArgs g, bool bf16, hipStream_t stream);
 hipError_t launch_gated_slopes(GatedArgs g, bool bf16, hipStream_t stream);  // dg, du from kept g, u
 hipError_t launch_gated_grad_x(GatedArgs g, bool bf16, hipStream_t stream);
+// the epilogue on parts of g and u (splits > 1), or on kept ones
+hipError_t launch_gated_join(const GatedArgs &g, bool bf16, hipStream_t stream);
+
+// Microscaled 4-bit floating point (mx4.hip).  Products: g.x [S, K] bf16, or codes with x_scales; g.w_gate and g.w_up
+// codes; plain products (not gated) are those of the gate alone, into g.a
+struct Mx4Args {
+  GatedArgs g;
+  bool gated;
+  const uint8_t *x_scales, *gate_scales, *up_scales;
+};
+size_t mx4_part_bytes(const Mx4Args &m);
+hipError_t launch_mx4(Mx4Args m, hipStream_t stream);
+struct Mx4Convert {
+  const void *x;  // [rows, K]; back from 4 bits: the result
+  uint8_t *codes, *scales;
+  int K;
+  uint32_t parts, total;  // of 128 numbers, in a row and in all
+};
+hipError_t launch_mx4_quantize(const Mx4Convert &a, bool bf16, hipStream_t stream);
+hipError_t launch_mx4_dequantize(const Mx4Convert &a, bool bf16, hipStream_t stream);
 
 // The norms before and after a block (block_norm.hip); null pointers: absent
 struct NormArgs {

@@ -14,152 +14,11 @@
 // product with a reduction of two segments (dg with w_gate, then du with w_up), summed in the same
 // accumulators and rounded once; both gradients of the weights are one launch, where the tiles of a group
 // share its rows of x in an XCD's L2.
-#include "grouped_tile.h"
+#include "gated_tile.h"
 
 namespace ace {
 
 namespace {
-
-// exp(-z^2 / 2) for 0 <= z <= 20 to about 2^-23: the hardware base-2 exponential, with what z^2 and its
-// product with log2(e) / 2 lose to rounding put back to first order
-__device__ __forceinline__ float half_square_exp(float z) {
-  constexpr float c = 0.72134752f, c_rest = 8.3e-9f;  // log2(e) / 2 = c + c_rest
-  const float h = z * z, l = fmaf(z, z, -h), e = -c * h;
-  const float rest = -fmaf(c, h, e) - c * l - c_rest * h;
-  return __builtin_amdgcn_exp2f(e) * fmaf(rest, 0.69314718f, 1.f);
-}
-
-// Phi(-z) e^(z^2 / 2) for z >= 0, which falls smoothly from 1/2 as 1 / (sqrt(2 pi) z): t P(t) with t = 1 / (1 + 0.32 z)
-// and P a polynomial fitted to the least relative error (3.3e-8 over all z >= 0; 3e-7 with fp32 arithmetic)
-__device__ __forceinline__ float normal_tail(float z) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.32f, z, 1.f));
-  float p = -0.0210784f;
-  p = fmaf(p, t, 0.095408306f);
-  p = fmaf(p, t, -0.14670941f);
-  p = fmaf(p, t, 0.06532997f);
-  p = fmaf(p, t, -0.009378675f);
-  p = fmaf(p, t, 0.058654312f);
-  p = fmaf(p, t, 0.087829046f);
-  p = fmaf(p, t, 0.11462236f);
-  p = fmaf(p, t, 0.12766095f);
-  p = fmaf(p, t, 0.12766153f);
-  return p * t;
-}
-
-// act(g), and with SLOPE act'(g).  SiLU of bf16 results: hardware exponential and reciprocal (see silu_for_bf16).
-template <typename T, int ACT> struct Activation {
-  static __device__ __forceinline__ float value(float g) {
-    float s;
-    return both<false>(g, s);
-  }
-  template <bool SLOPE> static __device__ __forceinline__ float both(float g, float &slope) {
-    if constexpr (ACT == kActSilu) {
-      const float s = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f))
-                                     : 1.f / (1.f + expf(-g));
-      if (SLOPE) slope = s * fmaf(g, 1.f - s, 1.f);
-      return g * s;
-    } else {
-      const float z = fminf(fabsf(g), 20.f);  // Phi(-20) is 0 in fp32
-      const float e = half_square_exp(z), tail = e * normal_tail(z), phi = g < 0.f ? tail : 1.f - tail;
-      if (SLOPE) slope = fmaf(g * 0.39894228f, e, phi);
-      return g * phi;
-    }
-  }
-};
-
-// 4 consecutive elements of a row
-__device__ __forceinline__ void load4(const float *p, f32x4_t &v) { v = *reinterpret_cast<const f32x4_t *>(p); }
-__device__ __forceinline__ void load4(const bf16_t *p, f32x4_t &v) {
-  const uint2 b = *reinterpret_cast<const uint2 *>(p);
-  v = f32x4_t{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16),
-              __uint_as_float(b.y & 0xffff0000u)};
-}
-__device__ __forceinline__ void store4(float *p, f32x4_t v) { *reinterpret_cast<f32x4_t *>(p) = v; }
-__device__ __forceinline__ void store4(bf16_t *p, f32x4_t v) {
-  *reinterpret_cast<uint2 *>(p) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-}
-
-// a tile of both projections
-template <class S> struct GatedRef : S::Ref {
-  size_t at;  // its first element in g, u, a, da, dg and du
-};
-
-// A wave's share of g and u: what is asked of them, a 16-row block at a time (the whole share at once would hold
-// a second copy of the accumulators)
-template <typename T, bool LINES, class S> struct GatedStore {
-  const GatedArgs &g;
-  static constexpr int NH = S::NW / 2;
-  typedef f32x4_t Block[1][NH];
-
-  __device__ __forceinline__ void put(const GatedRef<S> &t, void *out, const Block &v, int blk, int c0, int lane) const {
-    store_rows<T, LINES, 1, NH, 1>(static_cast<T *>(out) + t.at, t.rows, t.cols, g.M, v, blk, c0, lane);
-  }
-  // dg into the place of g, du into that of u
-  template <int ACT>
-  __device__ __forceinline__ void slopes(const GatedRef<S> &t, Block &vg, Block &vu, int blk, int c0, int lane) const {
-    const int row = 16 * blk + (lane & 15), l4 = lane >> 4;
-    const T *p = static_cast<const T *>(g.da) + t.at + static_cast<size_t>(row) * g.M;
-    f32x4_t da[NH];
-#pragma unroll
-    for (int j = 0; j < NH; ++j) {
-      const int col = c0 + (sizeof(T) == 2 ? 16 * (j & ~1) + 8 * l4 + 4 * (j & 1) : 16 * j + 4 * l4);
-      da[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      if (row < t.rows && col < t.cols) load4(p + col, da[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < NH; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float slope;
-        const float f = Activation<T, ACT>::template both<true>(vg[0][j][q], slope);
-        vg[0][j][q] = da[j][q] * vu[0][j][q] * slope;
-        vu[0][j][q] = da[j][q] * f;
-      }
-  }
-  template <int ACT> __device__ __forceinline__ void values(Block &vg, const Block &vu) const {
-#pragma unroll
-    for (int j = 0; j < NH; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) vg[0][j][q] = Activation<T, ACT>::value(vg[0][j][q]) * vu[0][j][q];
-  }
-
-  __device__ __forceinline__ void operator()(const GatedRef<S> &t, const f32x4_t (&sum)[S::MW][S::NW], int wr, int wc,
-                                             int lane) const {
-    const int c0 = 8 * wc * S::NW;
-#pragma unroll
-    for (int i = 0; i < S::MW; ++i) {
-      const int blk = wr + S::WR * i;
-      if (16 * blk >= t.rows) break;  // wave-uniform
-      Block vg, vu;
-#pragma unroll
-      for (int j = 0; j < NH; ++j) {
-        vg[0][j] = sum[i][2 * j];
-        vu[0][j] = sum[i][2 * j + 1];
-      }
-      if (t.part) {
-        store_part<T, 1, NH, 1>(t.part, t.rows, t.cols, g.M, vg, blk, c0, lane);
-        store_part<T, 1, NH, 1>(t.part + static_cast<size_t>(g.S) * g.M, t.rows, t.cols, g.M, vu, blk, c0, lane);
-      } else if (g.da) {
-        if (g.act == kActSilu)
-          slopes<kActSilu>(t, vg, vu, blk, c0, lane);
-        else
-          slopes<kActGelu>(t, vg, vu, blk, c0, lane);
-        put(t, g.dg, vg, blk, c0, lane);
-        put(t, g.du, vu, blk, c0, lane);
-      } else {
-        if (g.g) {
-          put(t, g.g, vg, blk, c0, lane);
-          put(t, g.u, vu, blk, c0, lane);
-        }
-        if (g.act == kActSilu)
-          values<kActSilu>(vg, vu);
-        else
-          values<kActGelu>(vg, vu);
-        put(t, g.a, vg, blk, c0, lane);
-      }
-    }
-  }
-};
 
 // Both projections in tiles of 16 MB rows of one group x 8 NB features: the whole work of a workgroup
 template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
@@ -171,7 +30,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &g, const RaggedTiles
   const Share share(static_cast<long long>(tiles.total) * per);
   auto ref = [&](const Item &it, int) {
     const int f0 = it.tile * BF;
-    const Part k = part_of<T>(it.group < 0 ? 0 : g.K, it.split, g.splits);
+    const Part k = part_of<S::A::BK>(it.group < 0 ? 0 : g.K, it.split, g.splits);
     const size_t w = (static_cast<size_t>(max(it.group, 0)) * g.M + f0) * g.K + k.k0;
     GatedRef<S> t;
     t.a.p[0] = static_cast<const T *>(g.x) + static_cast<size_t>(it.row0) * g.K + k.k0;
@@ -271,7 +130,7 @@ __global__ __launch_bounds__(WR *WC * 64) void gated_grad_x_kernel(GatedArgs g) 
   const Share share(static_cast<long long>(tiles.total) * per);
   auto ref = [&](const Item &it, int seg) {
     const int c0 = it.tile * BN;
-    const Part k = part_of<T>(it.group < 0 ? 0 : g.M, it.split, g.splits);
+    const Part k = part_of<S::A::BK>(it.group < 0 ? 0 : g.M, it.split, g.splits);
     typename S::Ref t;
     t.a.p[0] = static_cast<const T *>(seg ? g.du : g.dg) + static_cast<size_t>(it.row0) * g.M + k.k0;
     t.b.p[0] = static_cast<const T *>(seg ? g.w_up : g.w_gate) +
@@ -352,6 +211,8 @@ template <typename T, class Sh> void launch_grad_x_shape(const GatedArgs &g, hip
     launch(gated_grad_x_kernel<T, false, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
 }
 
+}  // namespace
+
 hipError_t launch_gated_join(const GatedArgs &g, bool bf16, hipStream_t s) {
   const size_t blocks = (static_cast<size_t>(g.S) * g.M / 4 + 255) / 256;
   const unsigned grid = static_cast<unsigned>(std::min<size_t>(std::max<size_t>(blocks, 1), 8 * kCUs));
@@ -362,8 +223,6 @@ hipError_t launch_gated_join(const GatedArgs &g, bool bf16, hipStream_t s) {
     g.act == kActSilu ? launch(gated_join_kernel<float, kActSilu>) : launch(gated_join_kernel<float, kActGelu>);
   return hipGetLastError();
 }
-
-}  // namespace
 
 size_t gated_part_bytes(const GatedArgs &g, bool bf16) {
   const int n = g.S > 0 ? plan_gated(g, bf16).splits : 1;

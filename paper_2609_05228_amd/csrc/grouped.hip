@@ -22,7 +22,7 @@ __device__ __forceinline__ void grouped_rows(const GroupedArgs &g, const RaggedT
   using S = DenseTile<T, false, GX, MB, NB, WR, WC, DA, DB>;
   auto ref = [&](const Item &it, int) {
     const int c0 = it.tile * BN;
-    const Part k = part_of<T>(it.group < 0 ? 0 : klen, it.split, g.splits);
+    const Part k = part_of<S::A::BK>(it.group < 0 ? 0 : klen, it.split, g.splits);
     typename S::Ref t;
     t.a.p[0] = static_cast<const T *>(g.rows) + static_cast<size_t>(it.row0) * klen + k.k0;
     const T *w = static_cast<const T *>(g.other) + static_cast<size_t>(max(it.group, 0)) * g.M * g.K;

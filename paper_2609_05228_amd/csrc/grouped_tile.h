@@ -518,9 +518,8 @@ struct Share {
 struct Part {
   int k0, len;
 };
-template <typename T> __device__ __forceinline__ Part part_of(int klen, int s, int splits) {
+template <int BK> __device__ __forceinline__ Part part_of(int klen, int s, int splits) {
   if (splits == 1) return {0, klen};
-  constexpr int BK = kStageElems<T>;
   const int nk = (klen + BK - 1) / BK, each = nk / splits, more = nk % splits;
   const int b = s * each + min(s, more), n = each + (s < more);
   return {b * BK, max(min(n * BK, klen - b * BK), 0)};

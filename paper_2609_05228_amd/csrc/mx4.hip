@@ -1,0 +1,244 @@
+// Microscaled 4-bit floating point (the format: mx4_tile.h): numbers into it and back, and products grouped by
+// expert with weights in it.
+//   quantise: e = floor(log2 of the block's largest) - 2, at least -127; numbers / 2^e go to the nearest of 0, .5, 1, 1.5,
+//             2, 3, 4, 6 with their sign (ties to the even code, beyond 6 to 6); a block that holds a NaN or an
+//             infinity stands for NaN
+//   y[r] = w[e] x[r], and a[r] = act(w_gate[e] x[r]) * (w_up[e] x[r]), for the rows r of group e, x in bf16 or in 4 bits
+#include "gated_tile.h"
+#include "mx4_tile.h"
+
+namespace ace {
+
+namespace {
+
+// largest absolute bits over the 4 lanes of a block
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0xB1, 0xf, 0xf, true)));  // lanes 1, 0, 3, 2
+  return max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x4E, 0xf, 0xf, true)));  // 2, 3, 0, 1
+}
+
+// 8 numbers of a lane
+__device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
+  const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = a[i];
+    v[4 + i] = b[i];
+  }
+}
+__device__ __forceinline__ void load8(const bf16_t *p, float (&v)[8]) {
+  const uint4 b = *reinterpret_cast<const uint4 *>(p);
+  const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+// 16 lanes take 128 numbers of a row, 8 each: 4 lanes a block, their four scales one dword.  Bound by memory.
+// `parts` of 128 numbers (the last one may be short) in a row.
+template <typename T> __global__ __launch_bounds__(256) void mx4_quantize_kernel(Mx4Convert a) {
+  const uint32_t l16 = threadIdx.x & 15, step = gridDim.x * 16;
+  for (uint32_t i = blockIdx.x * 16 + (threadIdx.x >> 4); i < a.total; i += step) {
+    const uint32_t row = i / a.parts, k = (i - row * a.parts) * 128 + 8 * l16;
+    const bool in = k < static_cast<uint32_t>(a.K);
+    float v[8] = {};
+    if (in) load8(static_cast<const T *>(a.x) + static_cast<size_t>(row) * a.K + k, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+    const uint32_t e = quad_max(top) >> 23;
+    const uint32_t s = e == 255 ? 255 : e < 2 ? 0 : e - 2;
+    const float scale = __uint_as_float(s << 23);  // its exponent is all that the conversion takes
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+    if (s == 255) c = 0;
+    if (in) *reinterpret_cast<uint32_t *>(a.codes + static_cast<size_t>(row) * (a.K / 2) + k / 2) = c;
+    // lanes 0, 4, 8, 12 of the 16 hold the blocks' scales
+    uint32_t four = in ? s << (8 * (l16 >> 2)) : 0;
+    four |= static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(four), 0x124, 0xf, 0xf, true));  // row_ror:4
+    four |= static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(four), 0x128, 0xf, 0xf, true));  // row_ror:8
+    if (l16 == 0) reinterpret_cast<uint32_t *>(a.scales)[i] = four;
+  }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void mx4_dequantize_kernel(Mx4Convert a) {
+  const uint32_t l16 = threadIdx.x & 15, step = gridDim.x * 16;
+  for (uint32_t i = blockIdx.x * 16 + (threadIdx.x >> 4); i < a.total; i += step) {
+    const uint32_t row = i / a.parts, k = (i - row * a.parts) * 128 + 8 * l16;
+    if (k >= static_cast<uint32_t>(a.K)) continue;
+    const uint32_t c = *reinterpret_cast<const uint32_t *>(a.codes + static_cast<size_t>(row) * (a.K / 2) + k / 2);
+    const float scale = __uint_as_float(static_cast<uint32_t>(a.scales[static_cast<size_t>(i) * 4 + (l16 >> 2)]) << 23);
+    T *o = static_cast<T *>(const_cast<void *>(a.x)) + static_cast<size_t>(row) * a.K + k;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<bf16x8_t *>(o) = mx4_to_bf16(c, scale);
+    } else {
+      typedef float f32x2_v __attribute__((ext_vector_type(2)));
+      const f32x2_v p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
+      const f32x2_v r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
+      reinterpret_cast<f32x4_t *>(o)[0] = f32x4_t{p[0], p[1], q[0], q[1]};
+      reinterpret_cast<f32x4_t *>(o)[1] = f32x4_t{r[0], r[1], t[0], t[1]};
+    }
+  }
+}
+
+// Tiles of 16 MB rows of one group x 16 NB columns (gated, MATS = 2: 8 NB features of both projections)
+template <bool ROWS4, bool LINES, int MATS, int MB, int NB, int WR, int WC, int DA, int DB>
+__global__ __launch_bounds__(WR *WC * 64) void mx4_rows_kernel(Mx4Args m) {
+  using S = Mx4Tile<ROWS4, MB, NB, WR, WC, DA, DB, MATS>;
+  static_assert(MATS == 1 || S::NW % 4 == 0, "gated: a wave holds whole pairs of feature blocks");
+  constexpr int BF = 16 * NB / MATS;
+  __shared__ __align__(16) uint8_t smem[S::LDS];
+  const GatedArgs &g = m.g;
+  const RaggedTiles tiles(g.offsets, g.N, g.S, 16 * MB, g.fill);
+  const int nN = (g.M + BF - 1) / BF, per = nN * g.splits;
+  const Share share(static_cast<long long>(tiles.total) * per);
+  const uint32_t code_row = static_cast<uint32_t>(g.K) / 2, scale_row = mx4_scale_row(g.K);
+  auto ref = [&](const Item &it, int) {
+    const int f0 = it.tile * BF;
+    const Part k = part_of<kMx4Stage>(it.group < 0 ? 0 : g.K, it.split, g.splits);
+    GatedRef<S> t;
+    if constexpr (ROWS4) {
+      t.a.codes[0] = static_cast<const uint8_t *>(g.x) + static_cast<size_t>(it.row0) * code_row + k.k0 / 2;
+      t.a.scales[0] = m.x_scales + static_cast<size_t>(it.row0) * scale_row + k.k0 / kMx4Block;
+    } else {
+      t.a.p[0] = static_cast<const bf16_t *>(g.x) + static_cast<size_t>(it.row0) * g.K + k.k0;
+    }
+    const size_t row = static_cast<size_t>(max(it.group, 0)) * g.M + f0;
+    t.b.codes[0] = static_cast<const uint8_t *>(g.w_gate) + row * code_row + k.k0 / 2;
+    t.b.scales[0] = m.gate_scales + row * scale_row + k.k0 / kMx4Block;
+    if constexpr (MATS == 2) {
+      t.b.codes[1] = static_cast<const uint8_t *>(g.w_up) + row * code_row + k.k0 / 2;
+      t.b.scales[1] = m.up_scales + row * scale_row + k.k0 / kMx4Block;
+    }
+    t.at = static_cast<size_t>(it.row0) * g.M + f0;
+    t.out = static_cast<bf16_t *>(g.a) + t.at;
+    t.part = g.splits > 1 ? g.part + MATS * static_cast<size_t>(it.split) * g.S * g.M + t.at : nullptr;
+    t.rows = it.rows;
+    t.cols = min(BF, g.M - f0);
+    t.klen = k.len;
+    t.rot = max(it.group, 0);
+    t.once = it.once;
+    return t;
+  };
+  long long done = 0;
+  for (int n; (n = share.count(done)) > 0; done += n) {
+    const long long i = share.item(done);
+    const RaggedTile t = tiles.find(static_cast<int>(i / per));
+    const int q = static_cast<int>(i % per);
+    const Item item{t.group, t.row0, t.rows, q % nN, t.only, q / nN};
+    __syncthreads();  // every wave is done with the rings
+    if constexpr (MATS == 2)
+      grouped_items<S>(item, n, g.K, g.K, smem, ref, GatedStore<bf16_t, LINES, S>{g});
+    else
+      grouped_items<S>(item, n, g.K, g.K, smem, ref, StoreTile<bf16_t, LINES, S>{static_cast<size_t>(g.M)});
+  }
+}
+
+template <bool ROWS4_, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_> struct Mx4Shape {
+  static constexpr bool ROWS4 = ROWS4_;
+  static constexpr int MB = MB_, NB = NB_, WR = WR_, WC = WC_, DA = DA_, DB = DB_;
+  static constexpr int TM = 16 * MB, TN = 16 * NB, THREADS = WR * WC * 64;
+  // the larger of the plain and the gated tile, which differ in the scales' place only
+  static constexpr int LDS1 = Mx4Tile<ROWS4, MB, NB, WR, WC, DA, DB, 1>::LDS, LDS2 = Mx4Tile<ROWS4, MB, NB, WR, WC, DA, DB, 2>::LDS;
+  static constexpr int PER_CU = 160 * 1024 / (LDS1 > LDS2 ? LDS1 : LDS2);
+  static_assert(PER_CU >= 1, "fits a CU");
+};
+// bf16 rows
+using Wide16 = Mx4Shape<false, 1, 16, 1, 4, 3, 3>;
+using Wide64 = Mx4Shape<false, 4, 8, 2, 2, 3, 3>;
+using Wide192 = Mx4Shape<false, 12, 16, 2, 4, 2, 2>;
+// rows in 4 bits
+using Four16 = Mx4Shape<true, 1, 16, 1, 4, 4, 4>;
+using Four64 = Mx4Shape<true, 4, 8, 2, 2, 4, 4>;
+using Four256 = Mx4Shape<true, 16, 16, 2, 4, 4, 4>;
+
+enum class Kind { k16, k64, kLarge };
+struct Plan {
+  Kind kind;
+  int splits;
+};
+
+Plan plan_mx4(const Mx4Args &m) {
+  const GatedArgs &g = m.g;
+  const int mats = m.gated ? 2 : 1, cols = mats * g.M;
+  if (g.S <= 16ll * g.N || g.S <= 16) {
+    const long long items = about_tiles(g.S, g.N, 16) * tiles_of(cols, Wide16::TN);
+    return {Kind::k16, pick_splits(items, kCUs * Wide16::PER_CU, tiles_of(g.K, 128), static_cast<size_t>(g.S) * cols, 0.6)};
+  }
+  const long long items = about_tiles(g.S, g.N, 64) * tiles_of(cols, Wide64::TN);
+  if (items <= 2 * kCUs)
+    return {Kind::k64, pick_splits(items, kCUs * Wide64::PER_CU, tiles_of(g.K, 128), static_cast<size_t>(g.S) * cols, 0.8)};
+  return {g.S <= 96ll * g.N ? Kind::k64 : Kind::kLarge, 1};
+}
+
+template <class Sh, int MATS> void launch_shape(const Mx4Args &m, hipStream_t s) {
+  const GatedArgs &g = m.g;
+  const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(g.M, Sh::TN / MATS) * g.splits;
+  auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(m); };
+  if (g.M % 64 == 0 && reinterpret_cast<uintptr_t>(g.a) % 128 == 0)
+    launch(mx4_rows_kernel<Sh::ROWS4, true, MATS, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+  else
+    launch(mx4_rows_kernel<Sh::ROWS4, false, MATS, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+}
+template <class Sh> void launch_kind(const Mx4Args &m, hipStream_t s) {
+  m.gated ? launch_shape<Sh, 2>(m, s) : launch_shape<Sh, 1>(m, s);
+}
+
+unsigned convert_grid(uint32_t total) { return std::min<uint32_t>((total + 15) / 16, 16 * kCUs); }
+
+}  // namespace
+
+size_t mx4_part_bytes(const Mx4Args &m) {
+  const int n = m.g.S > 0 ? plan_mx4(m).splits : 1;
+  return n > 1 ? (m.gated ? 2 : 1) * n * static_cast<size_t>(m.g.S) * m.g.M * sizeof(float) : 0;
+}
+
+hipError_t launch_mx4(Mx4Args m, hipStream_t s) {
+  GatedArgs &g = m.g;
+  if (g.S <= 0) return hipSuccess;
+  const Plan p = plan_mx4(m);
+  g.splits = p.splits;
+  const bool four = m.x_scales != nullptr;
+  switch (p.kind) {
+    case Kind::k16: four ? launch_kind<Four16>(m, s) : launch_kind<Wide16>(m, s); break;
+    case Kind::k64: four ? launch_kind<Four64>(m, s) : launch_kind<Wide64>(m, s); break;
+    case Kind::kLarge: four ? launch_kind<Four256>(m, s) : launch_kind<Wide192>(m, s); break;
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  if (m.gated) return launch_gated_join(g, true, s);
+  GroupedArgs j{};
+  j.out = g.a;
+  j.offsets = g.offsets;
+  j.S = g.S;
+  j.N = g.N;
+  j.fill = g.fill;
+  j.splits = p.splits;
+  j.part = g.part;
+  return launch_grouped_join(j, g.M, true, s);
+}
+
+hipError_t launch_mx4_quantize(const Mx4Convert &a, bool bf16, hipStream_t s) {
+  if (a.total == 0) return hipSuccess;
+  if (bf16)
+    mx4_quantize_kernel<bf16_t><<<convert_grid(a.total), 256, 0, s>>>(a);
+  else
+    mx4_quantize_kernel<float><<<convert_grid(a.total), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_dequantize(const Mx4Convert &a, bool bf16, hipStream_t s) {
+  if (a.total == 0) return hipSuccess;
+  if (bf16)
+    mx4_dequantize_kernel<bf16_t><<<convert_grid(a.total), 256, 0, s>>>(a);
+  else
+    mx4_dequantize_kernel<float><<<convert_grid(a.total), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace ace

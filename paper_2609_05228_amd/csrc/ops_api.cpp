@@ -203,6 +203,31 @@ bool bad_alias(const Span &out, const Span &in, bool may_equal) {
   return overlap(out, in) && !(may_equal && out.p == in.p && out.bytes == in.bytes);
 }
 
+constexpr int32_t kMx4 = 32;  // numbers of a block
+
+ace_status mx4_desc(const ace_mx4_desc *d, bool gated) {
+  if (!d || (gated && d->activation != ACE_ACT_SILU && d->activation != ACE_ACT_GELU)) return ACE_ERR_INVALID_ARG;
+  const ace_grouped_desc g{d->S, d->N, d->M, d->K, ACE_BF16, d->flags};
+  const ace_status st = grouped_desc(&g);
+  return st == ACE_OK && d->K % kMx4 != 0 ? ACE_ERR_UNSUPPORTED : st;
+}
+
+// bytes of a row
+size_t mx4_code_row(int32_t K) { return static_cast<size_t>(K) / 2; }
+size_t mx4_scale_row(int32_t K) { return (static_cast<size_t>(K) + 127) / 128 * 4; }
+
+ace::Mx4Args mx4_args(const ace_mx4_desc &d, bool gated) {
+  ace::Mx4Args m{};
+  m.g.S = d.S;
+  m.g.N = d.N;
+  m.g.M = d.M;
+  m.g.K = d.K;
+  m.g.act = d.activation == ACE_ACT_GELU ? ace::kActGelu : ace::kActSilu;
+  m.g.fill = (d.flags & ACE_ZERO_REST) ? 1 : 0;
+  m.gated = gated;
+  return m;
+}
+
 // a result on an input, or on another result
 bool any_overlap(const Span *outs, int n_out, const Span *ins, int n_in) {
   for (int i = 0; i < n_out; ++i) {
@@ -212,6 +237,56 @@ bool any_overlap(const Span *outs, int n_out, const Span *ins, int n_in) {
       if (overlap(outs[i], outs[j])) return true;
   }
   return false;
+}
+
+// gated: two matrices
+ace_status mx4(const ace_mx4_desc *desc, bool gated, const void *x, const uint8_t *x_scales, const ace_mx4 *w,
+               const ace_mx4 *w_up, const int32_t *offsets, void *out, void *workspace, size_t workspace_bytes,
+               void *stream) {
+  const ace_status st = mx4_desc(desc, gated);
+  if (st != ACE_OK) return st;
+  const ace_mx4_desc &d = *desc;
+  if (d.S == 0) return ACE_OK;
+  if (!w || (gated && !w_up) || !usable(x, 16) || !usable(out, 16) || !usable(offsets, 4) || (x_scales && !usable(x_scales, 4)))
+    return ACE_ERR_INVALID_ARG;
+  const ace_mx4 none{}, &up = gated ? *w_up : none;
+  if (!usable(w->codes, 16) || !usable(w->scales, 4) || (gated && (!usable(up.codes, 16) || !usable(up.scales, 4))))
+    return ACE_ERR_INVALID_ARG;
+  const size_t S = d.S, rows = static_cast<size_t>(d.N) * d.M, cr = mx4_code_row(d.K), sr = mx4_scale_row(d.K);
+  const Span o{out, 2 * S * d.M};
+  const Span ins[] = {{x, x_scales ? S * cr : 2 * S * d.K}, {x_scales, S * sr}, {w->codes, rows * cr}, {w->scales, rows * sr},
+                      {up.codes, rows * cr}, {up.scales, rows * sr}, {offsets, (d.N + 1u) * size_t{4}}};
+  if (any_overlap(&o, 1, ins, 7)) return ACE_ERR_INVALID_ARG;
+  ace::Mx4Args m = mx4_args(d, gated);
+  const size_t need = ace::mx4_part_bytes(m);
+  if (need > 0 && (!usable(workspace, 256) || workspace_bytes < need)) return ACE_ERR_WORKSPACE;
+  m.g.x = x;
+  m.g.w_gate = w->codes;
+  m.g.w_up = up.codes;
+  m.g.offsets = offsets;
+  m.g.a = out;
+  m.g.part = static_cast<float *>(workspace);
+  m.x_scales = x_scales;
+  m.gate_scales = w->scales;
+  m.up_scales = up.scales;
+  return status_of(ace::launch_mx4(m, static_cast<hipStream_t>(stream)));
+}
+
+// the parts of a conversion, or nothing to do (total = 0)
+ace_status mx4_convert(int64_t rows, int32_t K, int32_t dtype, const void *x, const uint8_t *codes, const uint8_t *scales,
+                       bool to_codes, ace::Mx4Convert *c) {
+  if (rows < 0 || K <= 0 || !is_dtype(dtype)) return ACE_ERR_INVALID_ARG;
+  const int64_t parts = (K + int64_t{127}) / 128;
+  if (K % kMx4 != 0 || K > kMaxWidth || rows >= (int64_t{1} << 31) / parts) return ACE_ERR_UNSUPPORTED;
+  *c = ace::Mx4Convert{x, const_cast<uint8_t *>(codes), const_cast<uint8_t *>(scales), K, static_cast<uint32_t>(parts),
+                       static_cast<uint32_t>(rows * parts)};
+  if (rows == 0) return ACE_OK;
+  if (!usable(x, 16) || !usable(codes, 16) || !usable(scales, 4)) return ACE_ERR_INVALID_ARG;
+  const size_t n = static_cast<size_t>(rows);
+  const Span a{x, n * K * elem_bytes(dtype)}, b{codes, n * mx4_code_row(K)}, s{scales, n * mx4_scale_row(K)};
+  // the codes' and scales' order does not matter where both are inputs
+  if (overlap(a, b) || overlap(a, s) || (to_codes && overlap(b, s))) return ACE_ERR_INVALID_ARG;
+  return ACE_OK;
 }
 
 }  // namespace
@@ -330,6 +405,37 @@ ace_status ace_grouped_gated_grad(const ace_gated_desc *desc, const void *da, co
   e = ace::launch_gated_grad_x(p, bf16, s);
   if (e != hipSuccess || !weights) return status_of(e);
   return status_of(ace::launch_grouped_weights(gated_weights_args(d, p.dg, p.du, x, offsets, dw_gate, dw_up, p.part), bf16, s));
+}
+
+ace_status ace_mx4_quantize(int64_t rows, int32_t K, int32_t dtype, const void *x, uint8_t *codes, uint8_t *scales,
+                            void *stream) {
+  ace::Mx4Convert c;
+  const ace_status st = mx4_convert(rows, K, dtype, x, codes, scales, true, &c);
+  return st != ACE_OK ? st : status_of(ace::launch_mx4_quantize(c, dtype == ACE_BF16, static_cast<hipStream_t>(stream)));
+}
+
+ace_status ace_mx4_dequantize(int64_t rows, int32_t K, int32_t dtype, const uint8_t *codes, const uint8_t *scales,
+                              void *x, void *stream) {
+  ace::Mx4Convert c;
+  const ace_status st = mx4_convert(rows, K, dtype, x, codes, scales, false, &c);
+  return st != ACE_OK ? st : status_of(ace::launch_mx4_dequantize(c, dtype == ACE_BF16, static_cast<hipStream_t>(stream)));
+}
+
+size_t ace_grouped_mx4_workspace_size(const ace_mx4_desc *desc, int gated) {
+  if (mx4_desc(desc, gated != 0) != ACE_OK) return 0;
+  return ace::mx4_part_bytes(mx4_args(*desc, gated != 0));
+}
+
+ace_status ace_grouped_matmul_mx4(const ace_mx4_desc *desc, const void *x, const uint8_t *x_scales, const ace_mx4 *w,
+                                  const int32_t *offsets, void *y, void *workspace, size_t workspace_bytes,
+                                  void *stream) {
+  return mx4(desc, false, x, x_scales, w, nullptr, offsets, y, workspace, workspace_bytes, stream);
+}
+
+ace_status ace_grouped_gated_mx4(const ace_mx4_desc *desc, const void *x, const uint8_t *x_scales,
+                                 const ace_mx4 *w_gate, const ace_mx4 *w_up, const int32_t *offsets, void *a,
+                                 void *workspace, size_t workspace_bytes, void *stream) {
+  return mx4(desc, true, x, x_scales, w_gate, w_up, offsets, a, workspace, workspace_bytes, stream);
 }
 
 ace_status ace_block_norm(const ace_norm_desc *desc, const ace_norm_inputs *in, void *h_out, void *n_out,

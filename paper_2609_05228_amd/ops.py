@@ -1,15 +1,18 @@
 """torch-facing wrappers of the operators around the layer: matrix products grouped by
-expert with ragged sizes, the norms before and after a block fused with its gate and residual
+expert with ragged sizes, the experts' gated feed-forward block, weights in microscaled 4-bit
+floating point for both, the norms before and after a block fused with its gate and residual
 scale, and low-rank adapters of many requests at once.
 
 Like `moe_forward` they marshal device tensors into the C ABI of libace.so and enqueue on the
 current HIP stream of the tensors' device.  They record no autograd graph: the gradients are
-entry points of their own (`grouped_matmul_grad_x`, `grouped_matmul_grad_w`, `block_norm_grad`),
+entry points of their own (`grouped_matmul_grad_x`, `grouped_matmul_grad_w`, `grouped_gated_grad`, `block_norm_grad`),
 and inputs that require a gradient are refused while autograd is on, inputs with a forward-mode
 tangent always.  Workspaces come from torch's allocator with every call, so captured graphs share
 none.
 """
 from __future__ import annotations
+
+from typing import NamedTuple
 
 import torch
 from torch.autograd import forward_ad
@@ -49,7 +52,8 @@ def _check_all(dev, dtype, named):
         if t.device != dev:
             raise ValueError(f"{name} is on {t.device}, expected {dev}")
         raise ValueError(f"{name} requires a gradient, and no graph is recorded: call under torch.no_grad() (gradients of "
-                         "grouped_matmul and block_norm: the *_grad functions; adapter_add has none)")
+                         "grouped_matmul, grouped_gated and block_norm: the *_grad functions; adapter_add has none, nor do "
+                         "weights in 4 bits)")
     if dev.type != "cuda":
         raise ValueError(f"the tensors are on {dev}: a GPU is needed")
 
@@ -104,6 +108,107 @@ def _grouped(way, rows, other, offsets, S, N, M, K, shape, names, shapes, out):
     return out
 
 
+class Mx4(NamedTuple):
+    """Numbers [..., K] in microscaled 4-bit floating point, blocks of 32 along the last dimension (K a multiple of 32):
+
+    codes   [..., K / 2] uint8, two numbers a byte, the even one in the low half: a sign (8) and 0, .5, 1, 1.5, 2, 3, 4, 6
+    scales  [..., 4 ceil(K / 128)] uint8: 2^(byte - 127) for each block, 255: the block stands for NaN; the bytes
+            from K / 32 on mean nothing"""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+_BLOCK = 32
+
+
+def _scale_bytes(K):
+    return (K + 127) // 128 * 4
+
+
+def _mx4_of(name, q, dims):
+    """K of an Mx4 with `dims` dimensions (None: any)."""
+    _need(isinstance(q, Mx4), f"{name} must be an Mx4")
+    _need(isinstance(q.codes, torch.Tensor) and isinstance(q.scales, torch.Tensor)
+          and q.codes.dim() >= 1 and (dims is None or q.codes.dim() == dims),
+          f"{name} must hold tensors" + ("" if dims is None else f" of {dims} dimensions"))
+    return 2 * q.codes.shape[-1]
+
+
+def _mx4_named(name, q, shape):
+    """What `_check_all` has to find for an Mx4 of numbers of that shape."""
+    return [(f"{name}.codes", q.codes, (*shape[:-1], shape[-1] // 2), torch.uint8),
+            (f"{name}.scales", q.scales, (*shape[:-1], _scale_bytes(shape[-1])), torch.uint8)]
+
+
+def mx4_quantize(x):
+    """x [..., K] bf16 or fp32 in microscaled 4-bit floating point: per block of 32 a scale 2^e with e = floor(log2 of
+    the largest magnitude) - 2, at least -127; each number over it to the nearest of 0, .5, 1, 1.5, 2, 3, 4, 6 with its sign (ties
+    to the even code, above 6 to 6).  A block that holds a NaN or an infinity stands for NaN.  Returns an `Mx4`."""
+    _need(isinstance(x, torch.Tensor) and x.dim() >= 1, "x must be a tensor of 1 dimension or more")
+    dtype, K = _dtype_of("x", x, x.dim()), x.shape[-1]
+    _need(K > 0 and K % _BLOCK == 0, f"the last dimension, {K}, is not a multiple of {_BLOCK}")
+    dev = x.device
+    _sizes(K)
+    _check_all(dev, dtype, [("x", x, x.shape, None)])
+    q = Mx4(torch.empty((*x.shape[:-1], K // 2), dtype=torch.uint8, device=dev),
+            torch.empty((*x.shape[:-1], _scale_bytes(K)), dtype=torch.uint8, device=dev))
+    _enqueue(dev, _lib.lib().ace_mx4_quantize, x.numel() // K, K, _DT[dtype], x.data_ptr(), q.codes.data_ptr(),
+             q.scales.data_ptr())
+    return q
+
+
+def mx4_dequantize(q, dtype=torch.bfloat16):
+    """The numbers [..., K] that an `Mx4` stands for, exactly, as bf16 or fp32."""
+    K = _mx4_of("q", q, None)
+    _need(dtype in _DT, f"unsupported dtype {dtype}")
+    _need(K > 0 and K % _BLOCK == 0, f"the last dimension, {K}, is not a multiple of {_BLOCK}")
+    dev, shape = q.codes.device, (*q.codes.shape[:-1], K)
+    _sizes(K)
+    _check_all(dev, torch.uint8, _mx4_named("q", q, shape))
+    out = torch.empty(shape, dtype=dtype, device=dev)
+    _enqueue(dev, _lib.lib().ace_mx4_dequantize, out.numel() // K, K, _DT[dtype], q.codes.data_ptr(), q.scales.data_ptr(),
+             out.data_ptr())
+    return out
+
+
+def _mx4_call(x, weights, offsets, out, act, names):
+    """y = w x, or with two weights the gated block, on weights in 4 bits."""
+    K = _mx4_of(names[0], weights[0], 3)
+    N, M = weights[0].codes.shape[:2]
+    if isinstance(x, Mx4):
+        _mx4_of("x", x, 2)
+        S, lead = x.codes.shape[0], x.codes
+        named = _mx4_named("x", x, (S, K))
+    else:
+        _need(_dtype_of("x", x, 2) is torch.bfloat16, "x: bf16 or Mx4 with weights in 4 bits")
+        S, lead = x.shape[0], x
+        named = [("x", x, (S, K), torch.bfloat16)]
+    _need(K % _BLOCK == 0, f"K = {K} is not a multiple of {_BLOCK}")
+    size = _sizes(S, N, M, K)
+    for name, w in zip(names, weights):
+        _mx4_of(name, w, 3)
+        named += _mx4_named(name, w, (N, M, K))
+    named.append(("offsets", offsets, (N + 1,), torch.int32))
+    flags = 0
+    if out is not None:
+        named.append(("out", out, (S, M), torch.bfloat16))
+    dev = lead.device
+    _check_all(dev, torch.bfloat16, named)
+    if out is None:
+        out = torch.empty((S, M), dtype=torch.bfloat16, device=dev)
+        flags = _lib.ACE_ZERO_REST
+    desc = _lib.Mx4Desc(*size, act, flags)
+    lib = _lib.lib()
+    gated = len(weights) == 2
+    n = lib.ace_grouped_mx4_workspace_size(desc, gated)
+    ws = _scratch(n, dev)
+    xs = x.scales.data_ptr() if isinstance(x, Mx4) else None
+    w = [_lib.Mx4Ptr(q.codes.data_ptr(), q.scales.data_ptr()) for q in weights]
+    _enqueue(dev, lib.ace_grouped_gated_mx4 if gated else lib.ace_grouped_matmul_mx4, desc, lead.data_ptr(), xs, *w,
+             offsets.data_ptr(), out.data_ptr(), _ptr(ws), n)
+    return out
+
+
 def _groups_of(offsets):
     _need(isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.shape[0] >= 2,
           "offsets must hold at least one group: [N + 1] int32")
@@ -119,7 +224,10 @@ def grouped_matmul(x, w, offsets, *, out=None):
              (the `offsets` of `moe_forward`'s plan)
     out      [S, M] or None.  Rows of no group stay as they are in `out`; a fresh result
              holds zeros there.
-    K and M are multiples of 8 (fp32: 4).  Returns y [S, M]."""
+    K and M are multiples of 8 (fp32: 4).  Returns y [S, M].
+    w may be an `Mx4` of [N, M, K]; then x is bf16 or an `Mx4` of [S, K], y and out are bf16, and there is no gradient."""
+    if isinstance(w, Mx4):
+        return _mx4_call(x, (w,), offsets, out, 0, ("w",))
     _dtype_of("x", x, 2)
     _dtype_of("w", w, 3)
     N, M, K = w.shape
@@ -177,7 +285,12 @@ def grouped_gated(x, w_gate, w_up, offsets, *, activation="silu", keep=False, ou
     keep     also return g and u, for `grouped_gated_grad`
     out      None, or tensors in the shape of the result.  Rows of no group stay as they are in them; a fresh
              result holds zeros there.
-    K and M are multiples of 8 (fp32: 4).  Returns a [S, M], with keep (a, (g, u))."""
+    K and M are multiples of 8 (fp32: 4).  Returns a [S, M], with keep (a, (g, u)).
+    Both weights may be an `Mx4` of [N, M, K]; then x is bf16 or an `Mx4` of [S, K], a and out are bf16, and there is
+    no gradient, so nothing to keep."""
+    if isinstance(w_gate, Mx4) or isinstance(w_up, Mx4):
+        _need(not keep, "keep: weights in 4 bits have no gradient")
+        return _mx4_call(x, (w_gate, w_up), offsets, out, _activation(activation), ("w_gate", "w_up"))
     dtype = _dtype_of("x", x, 2)
     _dtype_of("w_gate", w_gate, 3)
     act = _activation(activation)

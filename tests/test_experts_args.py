@@ -135,3 +135,94 @@ def test_gated_sizes_past_32_bits_are_refused():
                  lambda: ace.grouped_gated_grad(m(n, 8), m(n, 16), w, w, o)):
         with pytest.raises(ValueError, match="size of"):
             call()
+
+
+def _convert(back=False, rows=64, K=64, dtype=_lib.ACE_BF16, x=P[0], codes=P[1], scales=P[2]):
+    if back:
+        return ace.lib().ace_mx4_dequantize(rows, K, dtype, codes, scales, x, None)
+    return ace.lib().ace_mx4_quantize(rows, K, dtype, x, codes, scales, None)
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_mx4_conversion_refusals(back):
+    for kw in (dict(rows=-1), dict(K=0), dict(K=-32), dict(dtype=5), dict(x=0), dict(codes=0), dict(scales=0), dict(x=P[0] + 8),
+               dict(codes=P[1] + 8), dict(scales=P[2] + 2), dict(codes=P[0]), dict(scales=P[0] + 64)):
+        assert _convert(back, **kw) == BAD, kw
+    assert _convert(scales=P[1]) == BAD  # both are results
+    for kw in (dict(K=48), dict(K=65568), dict(rows=1 << 31), dict(rows=1 << 30, K=256), dict(rows=1 << 62)):
+        assert _convert(back, **kw) == UNS, kw
+    assert _convert(back, rows=0, x=0, codes=0, scales=0) == _lib.ACE_OK
+
+
+def _mx4(gated=False, x=P[0], xs=P[1], wc=P[2], wsc=P[3], uc=P[4], usc=P[5], offsets=P[6], out=P[7], null=False, ws=P[15],
+         ws_bytes=1 << 40, **kw):
+    d = dict(S=64, N=4, M=64, K=64, activation=0, flags=0)
+    d.update(kw)
+    desc = None if null else ctypes.byref(_lib.Mx4Desc(*d.values()))
+    w, u = (None if c is None else ctypes.byref(_lib.Mx4Ptr(c, s)) for c, s in ((wc, wsc), (uc, usc)))
+    if gated:
+        return ace.lib().ace_grouped_gated_mx4(desc, x, xs, w, u, offsets, out, ws, ws_bytes, None)
+    return ace.lib().ace_grouped_matmul_mx4(desc, x, xs, w, offsets, out, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_mx4_product_refusals(gated):
+    bad = [dict(S=-1), dict(N=0), dict(M=0), dict(K=-32), dict(flags=2), dict(null=True), dict(x=0), dict(wc=None), dict(wc=0),
+           dict(wsc=0), dict(offsets=0), dict(out=0), dict(x=P[0] + 8), dict(xs=P[1] + 2), dict(wc=P[2] + 4), dict(wsc=P[3] + 1),
+           dict(offsets=P[6] + 2), dict(out=P[7] + 8), dict(out=P[0]), dict(out=P[1]), dict(out=P[2] + 64), dict(out=P[3]),
+           dict(out=P[6])]
+    if gated:
+        bad += [dict(activation=2), dict(activation=-1), dict(uc=None), dict(uc=0), dict(usc=0), dict(uc=P[4] + 8), dict(out=P[4]),
+                dict(out=P[5])]
+    for kw in bad:
+        assert _mx4(gated, **kw) == BAD, kw
+    for kw in (dict(S=BIG), dict(N=4097), dict(M=65544), dict(K=65568), dict(M=12), dict(K=48), dict(K=8)):
+        assert _mx4(gated, **kw) == UNS, kw
+    few = dict(S=16, N=2, M=128, K=4096)
+    size = ace.lib().ace_grouped_mx4_workspace_size
+    n = size(_lib.Mx4Desc(*few.values(), 0, 0), int(gated))
+    assert n > 0 and n % (16 * 128 * 4 * (2 if gated else 1)) == 0
+    for kw in (dict(ws=0), dict(ws=P[15] + 16), dict(ws_bytes=n - 1)):
+        assert _mx4(gated, **few, **kw) == WSP, kw
+    assert size(_lib.Mx4Desc(32768, 128, 768, 2048, 0, 0), int(gated)) == 0
+    assert size(_lib.Mx4Desc(64, 4, 64, 48, 0, 0), int(gated)) == 0
+    assert _mx4(gated, S=0, x=0, xs=0, wc=None, uc=None, out=0, offsets=0) == _lib.ACE_OK
+
+
+def test_mx4_wrappers_refuse():
+    u8 = torch.uint8
+    x, o = _z(6, 64), _o(0, 2, 6)
+    w = ace.Mx4(_z(2, 8, 32, dtype=u8), _z(2, 8, 4, dtype=u8))
+    q = ace.Mx4(_z(6, 32, dtype=u8), _z(6, 4, dtype=u8))
+    refused([
+        (lambda: ace.mx4_quantize(x), "GPU"),
+        (lambda: ace.mx4_quantize(_z(6, 48)), "multiple of 32"),
+        (lambda: ace.mx4_quantize(_z(6, 0)), "multiple of 32"),
+        (lambda: ace.mx4_quantize(torch.zeros(())), "1 dimension"),
+        (lambda: ace.mx4_quantize(x.half()), "dtype"),
+        (lambda: ace.mx4_quantize(_z(64, 6).t()), "contiguous"),
+        (lambda: ace.mx4_quantize(x.clone().requires_grad_()), "no_grad"),
+        (lambda: ace.mx4_dequantize(q), "GPU"),
+        (lambda: ace.mx4_dequantize(x), "Mx4"),
+        (lambda: ace.mx4_dequantize(q, torch.float16), "dtype"),
+        (lambda: ace.mx4_dequantize(ace.Mx4(q.codes, q.scales[:, :2])), "q.scales: shape"),
+        (lambda: ace.mx4_dequantize(ace.Mx4(q.codes.int(), q.scales)), "q.codes: dtype"),
+        (lambda: ace.mx4_dequantize(ace.Mx4(q.codes[:, :24], q.scales)), "multiple of 32"),
+        (lambda: ace.grouped_matmul(x, w, o), "GPU"),
+        (lambda: ace.grouped_matmul(q, w, o), "GPU"),
+        (lambda: ace.grouped_matmul(x.float(), w, o), "bf16 or Mx4"),
+        (lambda: ace.grouped_matmul(_z(6, 96), w, o), "x: shape"),
+        (lambda: ace.grouped_matmul(q, _z(2, 8, 64), o), "2 dimensions"),
+        (lambda: ace.grouped_matmul(ace.Mx4(q.codes[0], q.scales[0]), w, o), "2 dimensions"),
+        (lambda: ace.grouped_matmul(x, ace.Mx4(w.codes[0], w.scales[0]), o), "3 dimensions"),
+        (lambda: ace.grouped_matmul(x, w, _o(0, 6)), "offsets: shape"),
+        (lambda: ace.grouped_matmul(x, w, o, out=_z(6, 8, dtype=torch.float32)), "out: dtype"),
+        (lambda: ace.grouped_matmul_grad_x(_z(6, 8), w, o), "3 dimensions"),
+        (lambda: ace.grouped_gated(x, w, _z(2, 8, 64), o), "w_up must be an Mx4"),
+        (lambda: ace.grouped_gated(x, _z(2, 8, 64), w, o), "w_gate must be an Mx4"),
+        (lambda: ace.grouped_gated(x, w, w, o, keep=True), "no gradient"),
+        (lambda: ace.grouped_gated(x, w, w, o, activation="tanh"), "activation"),
+        (lambda: ace.grouped_gated(x, w, ace.Mx4(w.codes[:, :4], w.scales[:, :4]), o), "w_up.codes: shape"),
+        (lambda: ace.grouped_gated(x, w, w, o), "GPU"),
+        (lambda: ace.grouped_gated_grad(_z(6, 8), x, w, w, o), "3 dimensions"),
+    ])

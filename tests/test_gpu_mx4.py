@@ -1,0 +1,334 @@
+"""4-bit weights: quantisation bit by bit against the format's definition, products and the gated block against
+64 bits on the values that the codes stand for, with NaN scales and infinities wherever nothing may be read."""
+import pytest
+import torch
+
+import experts_oracle as ref
+import mx4_oracle as fmt
+import ops_oracle
+import paper_2609_05228_amd as ace
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+BF16 = torch.bfloat16
+NAN = float("nan")
+
+
+def dev(q):
+    return ace.Mx4(*(t.to(DEV) for t in q))
+
+
+def test_every_code_and_scale_has_its_value():
+    """256 scales x 16 codes, in both types: exact, infinite past the type's largest, NaN for 255."""
+    s = torch.arange(256, dtype=torch.uint8)
+    codes = torch.zeros((256, 16), dtype=torch.uint8)
+    codes[:, :8] = (2 * torch.arange(8) + 16 * (2 * torch.arange(8) + 1)).to(torch.uint8)
+    scales = torch.full((256, 4), 255, dtype=torch.uint8)  # the padding means nothing
+    scales[:, 0] = s
+    want = fmt.values(codes, scales)
+    for dt in DT.values():
+        got = ace.mx4_dequantize(dev((codes, scales)), dt).cpu()
+        assert torch.equal(got[:255], want[:255].to(dt)) and bool(got[255].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 32), (3, 64), (5, 96), (2, 3, 160), (32,), (70, 128), (1, 4096), (129, 2080), (0, 64)],
+                         ids=str)
+def test_quantize(shape, dtype):
+    gen = torch.Generator().manual_seed(sum(shape))
+    x = torch.randn(shape, generator=gen) * torch.exp2(torch.randint(-20, 20, (*shape[:-1], 1), generator=gen).float())
+    x = x.to(DT[dtype])
+    q = ace.mx4_quantize(x.to(DEV))
+    codes, scales = fmt.quantize(x)
+    assert torch.equal(q.codes.cpu(), codes) and torch.equal(q.scales.cpu(), scales)
+    back = ace.mx4_dequantize(q, DT[dtype])
+    assert back.shape == x.shape and torch.equal(back.cpu().double(), fmt.values(codes, scales))
+    again = ace.mx4_quantize(back)  # what the format holds, it gives back
+    assert torch.equal(ace.mx4_dequantize(again, DT[dtype]), back)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_borders(dtype):
+    """Every halfway point, its neighbours and both signs, at scales from the least to the largest of the type; blocks
+    of zeros, of the type's extremes and subnormals."""
+    dt = DT[dtype]
+    pts = [0.0, 0.25, 0.5, 0.75, 1.0, 1.25, 1.5, 1.75, 2.0, 2.5, 3.0, 3.5, 4.0, 5.0, 6.0, 7.0]
+    base = torch.tensor(pts, dtype=dt)
+    one = torch.tensor(1.0, dtype=dt)
+    up, down = (torch.nextafter(base.float(), torch.full((), d)).to(dt) if dt is torch.float32
+                else (base * (1 + d * torch.finfo(dt).eps)) for d in ((float("inf"), 0.0) if dt is torch.float32 else (1, -0.5)))
+    rows = []
+    for e in (0, 1, -1, 30, -60, 125, -126):
+        for t in (base, up, down):
+            b = torch.zeros(32, dtype=dt)
+            b[:16] = t
+            b[16:] = -t
+            b[0], b[16] = 4.0, -0.0  # the block's largest lies in [4, 8): scale one
+            rows.append((b.double() * 2.0 ** e).to(dt))
+    tiny, big = torch.finfo(dt).smallest_normal, torch.finfo(dt).max
+    for vals in ([0.0], [-0.0], [tiny], [tiny / 2, -tiny / 4], [big, -big, big / 2], [tiny * torch.finfo(dt).eps],
+                 [big, tiny], [2.0 ** -126, 2.0 ** -127, 2.0 ** -128, 3 * 2.0 ** -128]):
+        b = torch.zeros(32, dtype=torch.float64)
+        b[:len(vals)] = torch.tensor(vals, dtype=torch.float64)
+        rows.append(b.to(dt))
+    x = torch.stack(rows)
+    assert one == 1
+    q = ace.mx4_quantize(x.to(DEV))
+    codes, scales = fmt.quantize(x)
+    assert torch.equal(q.scales.cpu(), scales)
+    assert torch.equal(q.codes.cpu(), codes)
+    assert torch.equal(ace.mx4_dequantize(q, dt).cpu().double(), fmt.values(codes, scales))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nan_and_infinity_stay_in_their_block(dtype):
+    x = torch.randn((4, 96), generator=torch.Generator().manual_seed(1)).to(DT[dtype])
+    x[0, 40], x[1, 0], x[2, 95], x[3, 31] = NAN, float("inf"), -float("inf"), -NAN
+    q = ace.mx4_quantize(x.to(DEV))
+    codes, scales = fmt.quantize(x)
+    assert torch.equal(q.codes.cpu(), codes) and torch.equal(q.scales.cpu(), scales)
+    back = ace.mx4_dequantize(q, DT[dtype]).cpu()
+    bad = torch.zeros((4, 3), dtype=torch.bool)
+    bad[0, 1] = bad[1, 0] = bad[2, 2] = bad[3, 0] = True
+    assert torch.equal(back.isnan().view(4, 3, 32), bad[..., None].expand(4, 3, 32))
+
+
+# group sizes, rows before the first and behind the last group, M, K
+SHAPES = [
+    ([1], 0, 0, 8, 32),
+    ([1, 1, 1], 0, 1, 64, 64),
+    ([0, 3, 0, 0, 5, 0], 2, 4, 72, 160),
+    ([16, 17, 15, 33], 0, 0, 128, 128),
+    ([0, 0], 3, 0, 40, 32),
+    ([65, 1, 0, 130, 63], 1, 70, 136, 224),
+    ([257, 3, 256, 255], 0, 9, 264, 96),
+    ([300], 0, 0, 520, 352),
+    ([5] * 70 + [0] * 60 + [2] * 5, 0, 3, 48, 96),
+    ([700, 0, 1, 90], 0, 0, 32, 1056),
+    ([2, 0, 1], 0, 0, 1032, 2080),
+    ([100] * 9 + [220] * 5, 0, 0, 1096, 96),
+    ([60] * 20, 0, 0, 584, 288),
+    ([37] * 40, 0, 0, 456, 64),
+]
+
+
+def make(sizes, head, tail, M, K, rows, seed=0):
+    """x (bf16, or codes and scales), two weights, offsets; NaN in the rows of no group, the weights of empty groups,
+    and the bytes behind a row's last scale."""
+    gen = torch.Generator().manual_seed(seed + M + K + len(sizes))
+    S, N = head + sum(sizes) + tail, len(sizes)
+    offs = [head]
+    for n in sizes:
+        offs.append(offs[-1] + n)
+    x = torch.randn((S, K), generator=gen)
+    ws = []
+    for _ in range(2):
+        w = torch.randn((N, M, K), generator=gen) * K ** -0.5 * 2
+        # channels and blocks of different sizes
+        w *= torch.exp2(torch.randint(-2, 3, (N, M, K // 32, 1), generator=gen).float()).expand(-1, -1, -1, 32).reshape(w.shape)
+        codes, scales = fmt.quantize(w)
+        for e, n in enumerate(sizes):
+            if n == 0:
+                scales[e] = 255
+        scales[..., K // 32:] = 255
+        ws.append((codes, scales))
+    if rows == "mx4":
+        codes, scales = fmt.quantize(x)
+        scales[:head] = 255
+        scales[offs[-1]:] = 255
+        scales[:, K // 32:] = 255
+        x, xv = (codes, scales), fmt.values(codes, scales)
+    else:
+        x = x.to(BF16)
+        x[:head] = NAN
+        x[offs[-1]:] = float("inf")
+        xv = x.double()
+    return x, xv, ws, torch.tensor(offs, dtype=torch.int32)
+
+
+def rest(offs, S):
+    m = torch.ones(S, dtype=torch.bool)
+    m[int(offs[0]):int(offs[-1])] = False
+    return m
+
+
+def rows_of(x):
+    return dev(x) if isinstance(x, tuple) else x.to(DEV)
+
+
+@pytest.mark.parametrize("rows", ["bf16", "mx4"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"{len(s[0])}g_{sum(s[0])}r_{s[3]}x{s[4]}")
+def test_products(shape, rows):
+    x, xv, ws, offs = make(*shape, rows)
+    gap = rest(offs, xv.shape[0])
+    xd, o = rows_of(x), offs.to(DEV)
+    w = [dev(q) for q in ws]
+    y = ace.grouped_matmul(xd, w[0], o)
+    torch.cuda.synchronize()
+    wv = [fmt.values(*q) for q in ws]
+    want, err = ref.both(xv, wv[0], offs)
+    ref.within(y[~gap], want[~gap], err[~gap], BF16, "y")
+    assert not y[gap].any()
+    buf = torch.full_like(y, 7)
+    assert ace.grouped_matmul(xd, w[0], o, out=buf) is buf
+    for act in ("silu", "gelu"):
+        a = ace.grouped_gated(xd, w[0], w[1], o, activation=act)
+        abuf = torch.full_like(a, 7)
+        assert ace.grouped_gated(xd, w[0], w[1], o, activation=act, out=abuf) is abuf
+        torch.cuda.synchronize()
+        want, err = ref.gated(xv, wv[0], wv[1], offs, act)
+        ref.within(a[~gap], want["a"][~gap], err["a"][~gap], BF16, act)
+        assert not a[gap].any()
+        assert bool((abuf[gap] == 7).all()) and torch.equal(abuf[~gap], a[~gap])
+    assert bool((buf[gap] == 7).all()) and torch.equal(buf[~gap], y[~gap])
+
+
+@pytest.mark.parametrize("rows", ["bf16", "mx4"])
+def test_as_the_dequantized_weights(rows):
+    """The same product as grouped_matmul of the weights taken back to bf16, to the sums' rounding."""
+    x, xv, ws, offs = make([40, 0, 200, 7], 0, 0, 264, 416, rows)
+    w = dev(ws[0])
+    y = ace.grouped_matmul(rows_of(x), w, offs.to(DEV))
+    xb = ace.mx4_dequantize(rows_of(x)) if rows == "mx4" else rows_of(x)
+    z = ace.grouped_matmul(xb, ace.mx4_dequantize(w), offs.to(DEV))
+    _, err = ref.both(xv, fmt.values(*ws[0]), offs)
+    d = (y.double() - z.double()).abs().cpu()
+    assert bool((d <= 2 * err + ops_oracle.HALF[BF16] * (y.double().abs() + z.double().abs()).cpu()).all())
+
+
+def test_nan_reaches_its_column_only():
+    """A weight block that stands for NaN makes its column NaN, in its group; a row's block its row."""
+    x, xv, ws, offs = make([40, 30], 0, 0, 64, 160, "mx4")
+    codes, scales = ws[0]
+    scales[1, 5, 2] = 255
+    x[1][3, 4] = 255
+    y = ace.grouped_matmul(dev(x), dev((codes, scales)), offs.to(DEV)).cpu()
+    bad = torch.zeros((70, 64), dtype=torch.bool)
+    bad[40:, 5] = True
+    bad[3] = True
+    assert torch.equal(y.isnan(), bad)
+    xb = torch.randn((70, 160), generator=torch.Generator().manual_seed(5)).to(BF16)
+    xb[3, 7] = float("inf")
+    y = ace.grouped_matmul(xb.to(DEV), dev((codes, scales)), offs.to(DEV)).cpu()
+    bad[3] = False
+    assert torch.equal(y.isnan()[torch.arange(70) != 3], bad[torch.arange(70) != 3]) and not y[3].isfinite().any()
+
+
+@pytest.mark.parametrize("rows", ["bf16", "mx4"])
+@pytest.mark.parametrize("lo,hi", [(0, 6), (120, 134), (190, 200)])
+def test_scales_far_from_one(rows, lo, hi):
+    """Scales near either end of the byte: products within the sums' rounding, as long as bf16 holds them."""
+    x, xv, ws, offs = make([20, 3], 0, 0, 40, 96, rows)
+    codes, scales = ws[0]
+    scales[..., :3] = torch.randint(lo, hi, scales[..., :3].shape, generator=torch.Generator().manual_seed(2)).to(torch.uint8)
+    wv = fmt.values(codes, scales)
+    y = ace.grouped_matmul(rows_of(x), dev((codes, scales)), offs.to(DEV))
+    want, err = ref.both(xv, wv, offs)
+    # numbers and products below the least normal one of 32 bits may be lost, each by less than that times its factor
+    under = (xv.abs().sum(dim=1, keepdim=True) + 96) * 2.0 ** -126
+    ref.within(y, want, err + under, BF16, "y")
+
+
+@pytest.mark.parametrize("rows", ["bf16", "mx4"])
+@pytest.mark.parametrize("offs", [[0, 9, 4, 40], [-5, 3, 90, 200], [40, 20, 10, 0], [7, 7, 7, 2 ** 31 - 1],
+                                  [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1]])
+def test_bad_offsets_stay_inside(offs, rows):
+    S, M, pad = 40, 24, 64
+    x, _, ws, _ = make([S, 0, 0], 0, 0, M, 64, rows)
+    o = torch.tensor(offs, dtype=torch.int32, device=DEV)
+    buf = torch.full((S * M + 2 * pad,), 5.0, dtype=BF16, device=DEV)
+    out = buf[pad:-pad].view(S, M)
+    w = [dev(q) for q in ws]
+    ace.grouped_matmul(rows_of(x), w[0], o, out=out)
+    ace.grouped_gated(rows_of(x), *w, o, out=out)
+    torch.cuda.synchronize()
+    assert bool((buf[:pad] == 5).all()) and bool((buf[-pad:] == 5).all())
+
+
+@pytest.mark.parametrize("rows", ["bf16", "mx4"])
+def test_no_rows(rows):
+    x, _, ws, offs = make([0, 0, 0], 0, 0, 16, 64, rows)
+    w = [dev(q) for q in ws]
+    assert ace.grouped_matmul(rows_of(x), w[0], offs.to(DEV)).shape == (0, 16)
+    assert ace.grouped_gated(rows_of(x), *w, offs.to(DEV)).shape == (0, 16)
+
+
+def test_numbers_past_two_to_the_32():
+    """Codes whose byte offsets pass 2^32, and numbers past 2^33: the last rows are right."""
+    K = 4096
+    rows = (1 << 32) // (K // 2) + 301
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.zeros((rows, K), dtype=BF16, device=DEV)
+    tail = torch.randn((200, K), generator=gen, device=DEV).to(BF16)
+    x[-200:] = tail
+    q = ace.mx4_quantize(x)
+    torch.cuda.synchronize()
+    codes, scales = fmt.quantize(tail.cpu())
+    assert torch.equal(q.codes[-200:].cpu(), codes) and torch.equal(q.scales[-200:].cpu(), scales)
+    assert not q.codes[:-200].any()
+    x.fill_(1)
+    back = ace.mx4_dequantize(q)
+    torch.cuda.synchronize()
+    assert torch.equal(back[-200:].cpu().double(), fmt.values(codes, scales)) and not back[-300:-200].any()
+    del x, back
+    # the same codes as rows of a product, and as weights
+    w = dev(fmt.quantize(torch.randn((1, 8, K), generator=torch.Generator().manual_seed(4)) * K ** -0.5))
+    offs = torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+    y = ace.grouped_matmul(q, w, offs)
+    torch.cuda.synchronize()
+    cut = torch.tensor([0, 200], dtype=torch.int32)
+    wv = fmt.values(*(t.cpu() for t in w))
+    want, err = ref.both(fmt.values(codes, scales), wv, cut)
+    ref.within(y[-200:], want, err, BF16, "rows")
+    assert not y[:-200].any()
+    N, M = 4096, 512  # 2^32 bytes in as many groups as there may be
+    big = ace.Mx4(q.codes[rows - N * M:].view(N, M, -1), q.scales[rows - N * M:].view(N, M, -1))
+    xr = torch.randn((6, K), generator=torch.Generator().manual_seed(6)).to(BF16)
+    o = torch.zeros(N + 1, dtype=torch.int32, device=DEV)
+    o[-3:] = torch.tensor([2, 4, 6], dtype=torch.int32, device=DEV)
+    y = ace.grouped_matmul(xr.to(DEV), big, o)
+    torch.cuda.synchronize()
+    last = tuple(t[-3:].cpu() for t in big)
+    want, err = ref.both(xr, fmt.values(*last), torch.tensor([0, 2, 4, 6], dtype=torch.int32))
+    ref.within(y, want, err, BF16, "weights")
+
+
+@pytest.mark.parametrize("rows", ["bf16", "mx4"])
+def test_streams_graphs_and_repeats(rows):
+    """Equal bits twice, on another stream, and from two captured graphs over changed inputs."""
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    _, _, ws, offs = make([30, 0, 5, 200], 0, 0, 72, 2080, rows)
+    S, K = 235, 2080
+    x = torch.randn((S, K), generator=gen, device=DEV).to(BF16)
+    w, o = [dev(q) for q in ws], offs.to(DEV)
+
+    def step():
+        r = ace.mx4_quantize(x) if rows == "mx4" else x
+        a = ace.grouped_gated(r, *w, o)
+        return [ace.grouped_matmul(r, w[0], o), a, ace.mx4_dequantize(ace.mx4_quantize(x), torch.float32)]
+
+    first = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(first, second))
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step()
+        graphs.append((g, out))
+    for i in range(3):
+        x.mul_(-0.75)
+        want = step()
+        torch.cuda.synchronize()
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for _, out in graphs:
+            assert all(torch.equal(p, q) for p, q in zip(out, want)), i
