@@ -80,6 +80,7 @@ template <typename T, bool DOWN, int BLK, bool PAIR, int W, int MATS = 1> struct
   static constexpr int UNITS = 2 * BLK;              // per stage
   static constexpr int NU = (UNITS + W - 1) / W;     // per wave
   static constexpr int COPIES = NU;                  // copies of a wave per stage
+  static constexpr int PANEL = 0, PANEL_STAGES = 1;  // nothing that comes for several stages at once (see mx4_tile.h)
   static constexpr int OU = DOWN ? BLK * 16 / BK : 1;  // k down: units across
   static constexpr int BYTES = UNITS * kUnitBytes;
   static_assert(UNITS % W == 0, "units spread evenly over the waves");
@@ -129,7 +130,7 @@ template <typename T, bool DOWN, int BLK, bool PAIR, int W, int MATS = 1> struct
   }
 
   // the copies of stage s into LDS at `lds`; once: no other tile reads this data
-  __device__ __forceinline__ void issue(int s, uint32_t lds, int wave, bool once) const {
+  __device__ __forceinline__ void issue(int s, uint32_t lds, uint32_t, int wave, bool once) const {
     bool in = true;
     const int left = klen - s * BK;  // k from this stage on
     auto rsrc_of = [&](const uint8_t *b) {
@@ -210,11 +211,19 @@ template <typename T, class SA = Mats<1>, class SB = Mats<1>> struct TileRef {
   bool once;       // b is read by no other tile
 };
 
+// Stage that a tile of nk stages starts with: groups start at different ones, and whole panels apart
+template <class Op> __device__ __forceinline__ int first_stage(int rot, int nk) {
+  constexpr int P = Op::PANEL_STAGES;
+  return nk > 0 ? rot % ((nk + P - 1) / P) * P : 0;
+}
+
 // The copying side of one operand: the stages of the list's tiles in order (of the segments of their
-// reductions, `n` in all), through a ring of D LDS slots
+// reductions, `n` in all), through a ring of D LDS slots.  A panel, what an operand has for PANEL_STAGES stages at
+// once, is copied ahead of the first of them, through a ring of its own with as many slots: no more than D
+// panels are in use or under way, since each belongs to one of D stages at least.
 template <class Op, int D, bool IS_A> struct Feed {
   Op op;
-  int pi = -1, ps = 0, pnk = 0, prot = 0, slot = 0;
+  int pi = -1, ps = 0, pnk = 0, prot = 0, slot = 0, pslot = 0;
   bool once = false;
 
   // on to the next tile that has stages, if the present one has none left
@@ -228,13 +237,20 @@ template <class Op, int D, bool IS_A> struct Feed {
         op.init(t.b, ld, t.cols, t.klen, wave, lane);
       pnk = (t.klen + Op::BK - 1) / Op::BK;
       ps = 0;
-      prot = pnk > 0 ? t.rot % pnk : 0;
+      prot = first_stage<Op>(t.rot, pnk);
       once = !IS_A && t.once;
     }
   }
-  // the next stage's copies
+  // the next stage's copies, and those of its panel where it is the first that needs it
   __device__ __forceinline__ void issue(uint32_t lds, int wave) {
-    op.issue(ps + prot < pnk ? ps + prot : ps + prot - pnk, lds + slot * Op::BYTES, wave, once);
+    const int s = ps + prot < pnk ? ps + prot : ps + prot - pnk;
+    uint32_t panel = 0;
+    if constexpr (Op::PANEL > 0)
+      if (s % Op::PANEL_STAGES == 0) {
+        panel = lds + D * Op::BYTES + pslot * Op::PANEL;
+        pslot = pslot + 1 == D ? 0 : pslot + 1;
+      }
+    op.issue(s, lds + slot * Op::BYTES, panel, wave, once);
     slot = slot + 1 == D ? 0 : slot + 1;
     ++ps;
   }
@@ -348,8 +364,8 @@ struct DenseTile {
   using Ref = TileRef<T, typename A::Src, typename B::Src>;
 
   // adds a stage's products; blocks past the tile's rows are read too and not multiplied
-  static __device__ __forceinline__ void multiply(const uint8_t *pa, const uint8_t *pb, int wr, int wc, int lane, int rows,
-                                                  int, f32x4_t (&acc)[MW][NW]) {
+  static __device__ __forceinline__ void multiply(const uint8_t *pa, const uint8_t *pb, const uint8_t *, const uint8_t *,
+                                                  int wr, int wc, int lane, int rows, int, int, f32x4_t (&acc)[MW][NW]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       typename B::frag_t bf[NW];
@@ -386,7 +402,8 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
   constexpr bool PAIR = sizeof(T) == 2;
   constexpr int BK = A::BK;
   // copies that may be outstanding when stage c is needed: those after the copies of A(c), that
-  // is of iterations c - DA + 1 (its B only, which lies ahead of B(c)) to c - 1
+  // is of iterations c - DA + 1 (its B only, which lies ahead of B(c)) to c - 1.  Panels are not counted: those
+  // among them only make the wait longer
   constexpr int PENDING = (DB > DA ? B::COPIES : 0) + (DA - 2) * (A::COPIES + B::COPIES);
   static_assert(A::BK == B::BK, "stages of the same k");
   static_assert(MB % WR == 0 && NB % WC == 0 && (!PAIR || NW % 2 == 0), "whole blocks, in bf16 pairs of column blocks, per wave");
@@ -394,7 +411,8 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave / WC, wc = wave % WC;
-  const uint32_t ldsa = lds_addr(smem), ldsb = ldsa + DA * A::BYTES;
+  constexpr int RING_A = DA * (A::BYTES + A::PANEL);
+  const uint32_t ldsa = lds_addr(smem), ldsb = ldsa + RING_A;
   auto at = [&](int i) {
     const int seg = i % SEG;
     i /= SEG;
@@ -419,7 +437,8 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
 #pragma unroll
   for (int s = 0; s < DA - 1; ++s)
     if (fa.pi < SEG * n) issue_a();
-  int sa = 0, sb = 0;  // slots of the stage multiplied next
+  int sa = 0, sb = 0;                                               // slots of the stage multiplied next
+  [[maybe_unused]] int qa = DA - 1, qb = DB - 1;                    // and of its panels
   int warm = DA - 1;   // the first stages wait for everything
   for (int ci = 0; ci < n; ++ci) {
     f32x4_t acc[MW][NW];
@@ -446,7 +465,7 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
     if constexpr (sizeof(T) == 4) clear(total);
     for (int seg = 0; seg < SEG; ++seg) {
       const auto t = at(ci * SEG + seg);
-      const int nk = (t.klen + BK - 1) / BK, rot = nk > 0 ? t.rot % nk : 0;
+      const int nk = (t.klen + BK - 1) / BK, rot = first_stage<B>(t.rot, nk);
       for (int kt = 0; kt < nk; ++kt) {
         // this stage landed for every wave, and every wave is done with the slots refilled next;
         // while B still had a stage to copy one iteration ago, the count is the constant one
@@ -461,8 +480,11 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
         } else {
           warm = 1;
         }
-        const int at_k = (kt + rot < nk ? kt + rot : kt + rot - nk) * BK;
-        S::multiply(smem + sa * A::BYTES, smem + DA * A::BYTES + sb * B::BYTES, wr, wc, lane, t.rows, t.klen - at_k, acc);
+        const int ks = kt + rot < nk ? kt + rot : kt + rot - nk;
+        if (A::PANEL > 0 && ks % A::PANEL_STAGES == 0) qa = qa + 1 == DA ? 0 : qa + 1;
+        if (B::PANEL > 0 && ks % B::PANEL_STAGES == 0) qb = qb + 1 == DB ? 0 : qb + 1;
+        S::multiply(smem + sa * A::BYTES, smem + RING_A + sb * B::BYTES, smem + DA * A::BYTES + qa * A::PANEL,
+                    smem + RING_A + DB * B::BYTES + qb * B::PANEL, wr, wc, lane, t.rows, ks * BK, t.klen, acc);
         if (sizeof(T) == 4 && (kt + 1) % kFlush == 0) flush();
         sa = sa + 1 == DA ? 0 : sa + 1;
         sb = sb + 1 == DB ? 0 : sb + 1;

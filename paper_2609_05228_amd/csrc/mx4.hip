@@ -87,9 +87,9 @@ template <typename T> __global__ __launch_bounds__(256) void mx4_dequantize_kern
 }
 
 // Tiles of 16 MB rows of one group x 16 NB columns (gated, MATS = 2: 8 NB features of both projections)
-template <bool ROWS4, bool LINES, int MATS, int MB, int NB, int WR, int WC, int DA, int DB>
+template <bool ROWS4, bool LINES, int MATS, int BK, int MB, int NB, int WR, int WC, int DA, int DB>
 __global__ __launch_bounds__(WR *WC * 64) void mx4_rows_kernel(Mx4Args m) {
-  using S = Mx4Tile<ROWS4, MB, NB, WR, WC, DA, DB, MATS>;
+  using S = Mx4Tile<ROWS4, BK, MB, NB, WR, WC, DA, DB, MATS>;
   static_assert(MATS == 1 || S::NW % 4 == 0, "gated: a wave holds whole pairs of feature blocks");
   constexpr int BF = 16 * NB / MATS;
   __shared__ __align__(16) uint8_t smem[S::LDS];
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(WR *WC * 64) void mx4_rows_kernel(Mx4Args m) {
   const uint32_t code_row = static_cast<uint32_t>(g.K) / 2, scale_row = mx4_scale_row(g.K);
   auto ref = [&](const Item &it, int) {
     const int f0 = it.tile * BF;
-    const Part k = part_of<kMx4Stage>(it.group < 0 ? 0 : g.K, it.split, g.splits);
+    const Part k = part_of<128>(it.group < 0 ? 0 : g.K, it.split, g.splits);
     GatedRef<S> t;
     if constexpr (ROWS4) {
       t.a.codes[0] = static_cast<const uint8_t *>(g.x) + static_cast<size_t>(it.row0) * code_row + k.k0 / 2;
@@ -139,23 +139,22 @@ __global__ __launch_bounds__(WR *WC * 64) void mx4_rows_kernel(Mx4Args m) {
   }
 }
 
-template <bool ROWS4_, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_> struct Mx4Shape {
+template <bool ROWS4_, int BK_, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_> struct Mx4Shape {
   static constexpr bool ROWS4 = ROWS4_;
-  static constexpr int MB = MB_, NB = NB_, WR = WR_, WC = WC_, DA = DA_, DB = DB_;
+  static constexpr int BK = BK_, MB = MB_, NB = NB_, WR = WR_, WC = WC_, DA = DA_, DB = DB_;
   static constexpr int TM = 16 * MB, TN = 16 * NB, THREADS = WR * WC * 64;
-  // the larger of the plain and the gated tile, which differ in the scales' place only
-  static constexpr int LDS1 = Mx4Tile<ROWS4, MB, NB, WR, WC, DA, DB, 1>::LDS, LDS2 = Mx4Tile<ROWS4, MB, NB, WR, WC, DA, DB, 2>::LDS;
-  static constexpr int PER_CU = 160 * 1024 / (LDS1 > LDS2 ? LDS1 : LDS2);
+  static constexpr int LDS = Mx4Tile<ROWS4, BK, MB, NB, WR, WC, DA, DB, NB % 4 == 0 ? 2 : 1>::LDS;
+  static constexpr int PER_CU = 160 * 1024 / LDS;
   static_assert(PER_CU >= 1, "fits a CU");
 };
 // bf16 rows
-using Wide16 = Mx4Shape<false, 1, 16, 1, 4, 3, 3>;
-using Wide64 = Mx4Shape<false, 4, 8, 2, 2, 3, 3>;
-using Wide192 = Mx4Shape<false, 12, 16, 2, 4, 2, 2>;
+using Wide16 = Mx4Shape<false, 128, 1, 16, 1, 4, 3, 3>;
+using Wide64 = Mx4Shape<false, 128, 4, 8, 2, 2, 3, 3>;
+using Wide256 = Mx4Shape<false, 64, 16, 16, 4, 2, 3, 3>;
 // rows in 4 bits
-using Four16 = Mx4Shape<true, 1, 16, 1, 4, 4, 4>;
-using Four64 = Mx4Shape<true, 4, 8, 2, 2, 4, 4>;
-using Four256 = Mx4Shape<true, 16, 16, 2, 4, 4, 4>;
+using Four16 = Mx4Shape<true, 128, 1, 16, 1, 4, 3, 3>;
+using Four64 = Mx4Shape<true, 128, 4, 8, 2, 2, 4, 4>;
+using Four256 = Mx4Shape<true, 128, 16, 16, 2, 4, 3, 3>;
 
 enum class Kind { k16, k64, kLarge };
 struct Plan {
@@ -181,9 +180,9 @@ template <class Sh, int MATS> void launch_shape(const Mx4Args &m, hipStream_t s)
   const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(g.M, Sh::TN / MATS) * g.splits;
   auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(m); };
   if (g.M % 64 == 0 && reinterpret_cast<uintptr_t>(g.a) % 128 == 0)
-    launch(mx4_rows_kernel<Sh::ROWS4, true, MATS, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+    launch(mx4_rows_kernel<Sh::ROWS4, true, MATS, Sh::BK, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
   else
-    launch(mx4_rows_kernel<Sh::ROWS4, false, MATS, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+    launch(mx4_rows_kernel<Sh::ROWS4, false, MATS, Sh::BK, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
 }
 template <class Sh> void launch_kind(const Mx4Args &m, hipStream_t s) {
   m.gated ? launch_shape<Sh, 2>(m, s) : launch_shape<Sh, 1>(m, s);
@@ -207,7 +206,7 @@ hipError_t launch_mx4(Mx4Args m, hipStream_t s) {
   switch (p.kind) {
     case Kind::k16: four ? launch_kind<Four16>(m, s) : launch_kind<Wide16>(m, s); break;
     case Kind::k64: four ? launch_kind<Four64>(m, s) : launch_kind<Wide64>(m, s); break;
-    case Kind::kLarge: four ? launch_kind<Four256>(m, s) : launch_kind<Wide192>(m, s); break;
+    case Kind::kLarge: four ? launch_kind<Four256>(m, s) : launch_kind<Wide256>(m, s); break;
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;

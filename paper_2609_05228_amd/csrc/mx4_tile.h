@@ -4,11 +4,14 @@
 //   codes  [rows, K / 2] bytes, the even number of a pair in the low half
 //   scales [rows, K / 32 rounded up to four] bytes; those past K / 32 are never used
 //
-// A stage is 128 k: per row 64 bytes of codes and four scales.  Lane (row r, group g) of a
-// matrix instruction holds 32 consecutive k of a row, which is one block with one scale byte: in
-// v_mfma_scale_f32_16x16x128_f8f6f4 by its definition, and in four v_mfma_f32_16x16x32_bf16, step j of which
-// multiplies k 8 j .. 8 j + 7 of every lane's block, since the order of k is free as long as both operands
-// agree.  So a block is read from LDS once, 16 bytes, and its scale once, wherever it goes.
+// Lane (row r, group g) of a matrix instruction takes consecutive k of one block: in
+// v_mfma_scale_f32_16x16x128_f8f6f4 k 32 g .. 32 g + 31, a block with its scale, by definition; in bf16 instructions,
+// whose order of k is free as long as both operands agree, the lane's k of two or four instructions lie side by side:
+// a stage of 64 k (two v_mfma_f32_16x16x32_bf16) has k 16 g .. 16 g + 15, one of 128 k 32 g .. 32 g + 31.  So a lane
+// reads its codes of a stage from LDS at once and one scale for them.
+//
+// Scales come in panels of 512 k, 16 bytes a row: a stage's own four (two) bytes of each row would be as many trips to
+// the cache as the codes.
 #pragma once
 
 #include "grouped_tile.h"
@@ -16,49 +19,41 @@
 namespace ace {
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kMx4Block = 32;
-constexpr int kMx4Stage = 128;  // k of a stage
+constexpr int kMx4Panel = 512;  // k of a panel of scales
 
 __host__ __device__ constexpr uint32_t mx4_scale_row(int K) { return static_cast<uint32_t>((K + 127) / 128) * 4u; }
-
-// 4 bytes per lane from descriptor + off into LDS at lds + 4 * lane (see dma16)
-__device__ __forceinline__ void dma4_buf(i32x4_rsrc rsrc, uint32_t off, uint32_t lds) {
-  asm volatile(
-      "s_mov_b32 m0, %2\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dword %0, %1, 0 offen lds"
-      :
-      : "v"(off), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(lds))
-      : "memory", "m0");
-}
 
 template <int MATS> struct Mx4Mats {
   const uint8_t *codes[MATS], *scales[MATS];
 };
 
-// BLK 16-row blocks in 4 bits.  A unit is a block's 16 rows x 64 bytes: copy lane i brings a 16-byte chunk of row
-// i / 4 to byte 16 i, chunk c of row r in slot c ^ (r / 4), so that the 16 lanes that read one chunk of all rows
-// cover 256 bytes.  The scales of 64 rows are one copy of four bytes a lane.  Waves that have no unit or no rows of
-// scales left copy zeros into a place of their own behind the rest, so that every wave waits for equal counts.
-template <int BLK, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
+// BLK 16-row blocks in 4 bits, in stages of BK (64 or 128) k.  With two matrices block b is block b / 2 of matrix b % 2; in
+// LDS all of the first one's come first.  A unit is 1 KB: 32 or 16 rows of BK / 2 bytes, copy lane i brings a 16-byte
+// chunk of row i / CH to byte 16 i, with the chunks of a row swapped so that the 16 lanes that read one chunk
+// each (of 8 or 16 bytes) of a block's rows cover all banks.  Waves that have no unit left copy zeros into a place behind
+// the rest, so that every wave waits for equal counts.  A panel is 64 rows a copy, 16 bytes a lane (its rows are padded to
+// 4 bytes only, so the addresses are multiples of 4).
+template <int BLK, int BK_, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
   using Src = Mx4Mats<MATS>;
-  static constexpr int BK = kMx4Stage;
-  static constexpr int UNITS = BLK, NU = (UNITS + W - 1) / W;
-  static constexpr int GROUPS = (16 * BLK / MATS + 63) / 64;         // 64 rows of scales, of one matrix
-  static constexpr int NS = (MATS * GROUPS + W - 1) / W;             // copies of scales of a wave
-  static constexpr int COPIES = NU + NS;
-  static constexpr int SCALES = UNITS * kUnitBytes;                  // where the scales lie
-  static constexpr int SPARE = SCALES + MATS * GROUPS * 256;         // and what nobody reads
-  static constexpr int BYTES = SPARE + (UNITS % W ? kUnitBytes : (MATS * GROUPS) % W ? 256 : 0);
-  static_assert(MATS == 1 || NU == 1 || NU % 2 == 0, "two matrices: a wave's units see issue");
+  static constexpr int BK = BK_, CH = BK / 32, RU = 64 / CH;  // chunks of a row, rows of a unit
+  static constexpr int UNITS = 16 * BLK / RU, NU = (UNITS + W - 1) / W, COPIES = NU;
+  static constexpr int BYTES = (UNITS + (UNITS % W ? 1 : 0)) * kUnitBytes;
+  static constexpr int ROWS = 16 * BLK / MATS, GROUPS = (ROWS + 63) / 64;  // of one matrix; copies of its panel
+  static constexpr int NP = (MATS * GROUPS + W - 1) / W;
+  static constexpr int PANEL = MATS * GROUPS * kUnitBytes, PANEL_STAGES = kMx4Panel / BK;
+  static_assert(BK == 64 || BK == 128, "a lane's k lie in one block");
+  static_assert(16 * BLK % RU == 0 && UNITS % MATS == 0 && (MATS == 1 || UNITS / MATS % NU == 0),
+                "units of one matrix, all of a wave's of the same");
 
-  const uint8_t *codes[MATS], *scales[NS];
+  const uint8_t *codes, *scales[NP];
   uint32_t code_row, scale_row;  // bytes
   uint32_t code_span, scale_span;
   int klen, chunk_k;
-  uint32_t voff[NU], soff[NS];
+  uint32_t voff[NU], poff[NP];
 
   __device__ __forceinline__ void init(const Src &src, int ld, int valid, int k, int wave, int lane) {
     klen = k;
@@ -66,69 +61,76 @@ template <int BLK, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
     scale_row = mx4_scale_row(ld);
     code_span = static_cast<uint32_t>(valid) * code_row;
     scale_span = static_cast<uint32_t>(valid) * scale_row;
-#pragma unroll
-    for (int m = 0; m < MATS; ++m) codes[m] = src.codes[m];
     // offsets, not choices between pointers: those would be indexes into the arrays at run time and put them in memory
-    if (MATS == 2 && NU == 1) codes[0] += (src.codes[MATS - 1] - src.codes[0]) * (wave % 2);
-    const int r = lane >> 2, chunk = (lane & 3) ^ (r >> 2);
-    chunk_k = kMx4Block * chunk;
+    codes = src.codes[0];
+    if (MATS == 2) codes += (src.codes[MATS - 1] - src.codes[0]) * (wave * NU >= UNITS / MATS);
+    const int r = lane / CH, chunk = (lane % CH) ^ swap(r & 15);
+    chunk_k = 32 * chunk;
 #pragma unroll
     for (int t = 0; t < NU; ++t) {
-      const int u = wave * NU + t;
-      voff[t] = u < UNITS ? static_cast<uint32_t>(block_row<PAIR>(u / MATS, r)) * code_row + 16u * chunk : kOutside;
+      const int u = wave * NU + t, p = u % (UNITS / MATS) * RU + r;  // row among the matrix's
+      voff[t] = u < UNITS ? static_cast<uint32_t>(block_row<PAIR>(p >> 4, p & 15)) * code_row + 16u * chunk : kOutside;
     }
 #pragma unroll
-    for (int t = 0; t < NS; ++t) {
-      const int i = wave * NS + t, p = (i % GROUPS) * 64 + lane;
-      const bool in = i < MATS * GROUPS && p < 16 * BLK / MATS;
-      soff[t] = in ? static_cast<uint32_t>(block_row<PAIR>(p >> 4, p & 15)) * scale_row : kOutside;
-      scales[t] = src.scales[0] + (MATS == 2 ? (src.scales[MATS - 1] - src.scales[0]) * min(i / GROUPS, 1) : 0);
+    for (int t = 0; t < NP; ++t) {
+      const int i = wave * NP + t, p = i % GROUPS * 64 + lane;
+      poff[t] = p < ROWS ? static_cast<uint32_t>(block_row<PAIR>(p >> 4, p & 15)) * scale_row : kOutside;
+      scales[t] = src.scales[0];
+      if (MATS == 2) scales[t] += (src.scales[MATS - 1] - src.scales[0]) * (i >= GROUPS);
     }
   }
+  static __device__ __forceinline__ int swap(int r) { return CH == 4 ? r >> 2 : r >> 3; }
 
-  // the copies of stage s, which is within k
-  __device__ __forceinline__ void issue(int s, uint32_t lds, int wave, bool once) const {
+  // the copies of stage s, which is within k, and of its panel where there is a place for it
+  __device__ __forceinline__ void issue(int s, uint32_t lds, uint32_t panel, int wave, bool once) const {
+    if (panel) {
+      const uint32_t at = static_cast<uint32_t>(s / PANEL_STAGES) * 16u;
+#pragma unroll
+      for (int t = 0; t < NP; ++t)
+        if (wave * NP + t < MATS * GROUPS)
+          dma16_buf(make_rsrc(scales[t] + at, scale_span - at), poff[t], panel + (wave * NP + t) * kUnitBytes);
+    }
     const bool in = chunk_k < klen - s * BK;
-    const uint32_t at = static_cast<uint32_t>(s) * 64u;
-    const i32x4_rsrc first = make_rsrc(codes[0] + at, code_span - at);
-    const i32x4_rsrc second = MATS == 2 && NU > 1 ? make_rsrc(codes[MATS - 1] + at, code_span - at) : first;
+    const uint32_t at = static_cast<uint32_t>(s) * (BK / 2);
+    const i32x4_rsrc rsrc = make_rsrc(codes + at, code_span - at);
 #pragma unroll
     for (int t = 0; t < NU; ++t) {
-      const int u = wave * NU + t;
-      const uint32_t to = lds + (u < UNITS ? u * kUnitBytes : SPARE);
+      const uint32_t to = lds + min(wave * NU + t, UNITS) * kUnitBytes;
       if (once)
-        dma16_buf_stream(t % 2 ? second : first, in ? voff[t] : kOutside, to);
+        dma16_buf_stream(rsrc, in ? voff[t] : kOutside, to);
       else
-        dma16_buf(t % 2 ? second : first, in ? voff[t] : kOutside, to);
-    }
-#pragma unroll
-    for (int t = 0; t < NS; ++t) {
-      const int i = wave * NS + t;
-      // four scales, of which those past the end of k are not used
-      dma4_buf(make_rsrc(scales[t] + 4 * s, scale_span - 4u * s), soff[t], lds + (i < MATS * GROUPS ? SCALES + i * 256 : SPARE));
+        dma16_buf(rsrc, in ? voff[t] : kOutside, to);
     }
   }
 
-  // block of lane (r, g) = (lane % 16, lane / 16) in 16-row block blk: k 32 g .. 32 g + 31 of row r
-  static __device__ __forceinline__ i32x4_t read(const uint8_t *s, int blk, int lane) {
-    const int r = lane & 15, g = lane >> 4;
-    return *reinterpret_cast<const i32x4_t *>(s + blk * kUnitBytes + r * 64 + ((g ^ (r >> 2)) << 4));
+  // row r = lane % 16 of block blk among the rows in LDS
+  static __device__ __forceinline__ int at(int blk, int lane) {
+    return (blk % MATS * (BLK / MATS) + blk / MATS) * 16 + (lane & 15);
   }
-  // its scale; `blocks` of the stage's four are within k (the others' codes are zeros)
-  static __device__ __forceinline__ int read_scale(const uint8_t *s, int blk, int lane, int blocks) {
+  // the lane's codes, g = lane / 16: k 32 g .. 32 g + 31 or (two words) 16 g .. 16 g + 15
+  typedef std::conditional_t<BK == 128, i32x4_t, i32x2_t> codes_t;
+  static __device__ __forceinline__ codes_t read(const uint8_t *s, int blk, int lane) {
     const int r = lane & 15, g = lane >> 4;
-    const int v = s[SCALES + ((blk % MATS) * GROUPS * 64 + (blk / MATS) * 16 + r) * 4 + g];
-    return g < blocks ? v : 0;
+    if constexpr (BK == 128)
+      return *reinterpret_cast<const codes_t *>(s + at(blk, lane) * 64 + ((g ^ swap(r)) << 4));
+    else
+      return *reinterpret_cast<const codes_t *>(s + at(blk, lane) * 32 + (((g >> 1) ^ swap(r)) << 4) + 8 * (g & 1));
+  }
+  // their scale, for the stage from k on of klen: one that is not of a block within klen (whose codes are zeros) may
+  // be anything, and is 0 here
+  static __device__ __forceinline__ int read_scale(const uint8_t *panel, int blk, int lane, int k, int klen) {
+    const int b = BK == 128 ? lane >> 4 : lane >> 5;  // of the stage's blocks
+    const int v = panel[at(blk, lane) * 16 + (k % kMx4Panel / kMx4Block + b)];
+    return k + kMx4Block * b < klen ? v : 0;
   }
 };
 
-// BLK 16-row blocks of bf16 rows, staged 128 k at a time: two halves of 64 k, each in units of 8 rows x 128 bytes as
-// Operand has them
-template <int BLK, int W> struct WideRows {
+// BLK 16-row blocks of bf16 rows in stages of 64 or 128 k: halves of 64 k, each in units of 8 rows x 128 bytes as Operand
+// has them
+template <int BLK, int BK_, int W> struct Mx4Rows {
   using Src = Mats<1>;
-  static constexpr int BK = kMx4Stage;
-  static constexpr int UNITS = 4 * BLK, NU = UNITS / W, COPIES = NU;
-  static constexpr int BYTES = UNITS * kUnitBytes;
+  static constexpr int BK = BK_, UNITS = 2 * BLK * (BK / 64), NU = UNITS / W, COPIES = NU;
+  static constexpr int BYTES = UNITS * kUnitBytes, PANEL = 0, PANEL_STAGES = kMx4Panel / BK;
   static_assert(UNITS % W == 0, "units spread evenly over the waves");
 
   const uint8_t *base;
@@ -149,9 +151,9 @@ template <int BLK, int W> struct WideRows {
       voff[t] = static_cast<uint32_t>(row) * row_bytes + static_cast<uint32_t>(128 * (u / (2 * BLK)) + 2 * chunk_k);
     }
   }
-  __device__ __forceinline__ void issue(int s, uint32_t lds, int wave, bool) const {
+  __device__ __forceinline__ void issue(int s, uint32_t lds, uint32_t, int wave, bool) const {
     const int left = klen - s * BK;
-    const uint32_t at = static_cast<uint32_t>(s) * 256u;
+    const uint32_t at = static_cast<uint32_t>(s) * (2 * BK);
     const i32x4_rsrc rsrc = make_rsrc(base + at, span - at);
 #pragma unroll
     for (int t = 0; t < NU; ++t) {
@@ -159,11 +161,11 @@ template <int BLK, int W> struct WideRows {
       dma16_buf(rsrc, 64 * (u / (2 * BLK)) + chunk_k < left ? voff[t] : kOutside, lds + u * kUnitBytes);
     }
   }
-  // k 32 g + 8 j .. + 7 of row lane % 16 of block blk, g = lane / 16
+  // the lane's k of instruction j (BK / 4 of them from BK / 4 g on, 8 each) of row lane % 16 of block blk
   static __device__ __forceinline__ bf16x8_t read(const uint8_t *s, int blk, int j, int lane) {
-    const int r = lane & 15, g = lane >> 4, rlo = r & 7;
-    return *reinterpret_cast<const bf16x8_t *>(s + ((g >> 1) * 2 * BLK + 2 * blk + (r >> 3)) * kUnitBytes + rlo * 128 +
-                                               (((4 * (g & 1) + j) ^ rlo) << 4));
+    const int r = lane & 15, rlo = r & 7, c = (BK / 32) * (lane >> 4) + j;  // 16-byte chunk of the row
+    return *reinterpret_cast<const bf16x8_t *>(s + ((c >> 3) * 2 * BLK + 2 * blk + (r >> 3)) * kUnitBytes + rlo * 128 +
+                                               (((c & 7) ^ rlo) << 4));
   }
 };
 
@@ -182,24 +184,25 @@ __device__ __forceinline__ bf16x8_t mx4_to_bf16(uint32_t codes, float scale) {
 
 // Tiles of bf16 results (see DenseTile) on 4-bit weights: rows in bf16 (ROWS4 = false) by bf16 matrix instructions on
 // the weights' exact values, or rows in 4 bits too, by the scaled instruction
-template <bool ROWS4, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_, int MATS> struct Mx4Tile {
+template <bool ROWS4, int BK, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_, int MATS> struct Mx4Tile {
   using T = bf16_t;
   static constexpr int MB = MB_, NB = NB_, WR = WR_, WC = WC_, DA = DA_, DB = DB_, SEG = 1;
   static constexpr int MW = MB / WR, NW = NB / WC;
-  using A = std::conditional_t<ROWS4, Mx4Operand<MB, false, WR * WC>, WideRows<MB, WR * WC>>;
-  using B = Mx4Operand<NB, true, WR * WC, MATS>;
+  using A = std::conditional_t<ROWS4, Mx4Operand<MB, BK, false, WR * WC>, Mx4Rows<MB, BK, WR * WC>>;
+  using B = Mx4Operand<NB, BK, true, WR * WC, MATS>;
   using Ref = TileRef<T, typename A::Src, typename B::Src>;
-  static constexpr int LDS = DA * A::BYTES + DB * B::BYTES;
+  static constexpr int LDS = DA * (A::BYTES + A::PANEL) + DB * (B::BYTES + B::PANEL);
+  static_assert(!ROWS4 || BK == 128, "the scaled instruction's k");
 
-  static __device__ __forceinline__ void multiply(const uint8_t *pa, const uint8_t *pb, int wr, int wc, int lane, int rows,
-                                                  int left, f32x4_t (&acc)[MW][NW]) {
-    const int blocks = left / kMx4Block;
-    i32x4_t bq[NW];
+  static __device__ __forceinline__ void multiply(const uint8_t *pa, const uint8_t *pb, const uint8_t *qa, const uint8_t *qb,
+                                                  int wr, int wc, int lane, int rows, int k, int klen,
+                                                  f32x4_t (&acc)[MW][NW]) {
+    typename B::codes_t bq[NW];
     int bs[NW];
 #pragma unroll
     for (int j = 0; j < NW; ++j) {
       bq[j] = B::read(pb, wc * NW + j, lane);
-      bs[j] = B::read_scale(pb, wc * NW + j, lane, blocks);
+      bs[j] = B::read_scale(qb, wc * NW + j, lane, k, klen);
     }
     if constexpr (ROWS4) {
       i32x4_t aq[MW];
@@ -207,7 +210,7 @@ template <bool ROWS4, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_, int 
 #pragma unroll
       for (int i = 0; i < MW; ++i) {
         aq[i] = A::read(pa, wr + WR * i, lane);
-        as[i] = A::read_scale(pa, wr + WR * i, lane, blocks);
+        as[i] = A::read_scale(qa, wr + WR * i, lane, k, klen);
       }
       auto wide = [](i32x4_t v) { return i32x8_t{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; };
 #pragma unroll
@@ -220,7 +223,7 @@ template <bool ROWS4, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_, int 
         }
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < BK / 32; ++j) {
         bf16x8_t bf[NW], af[MW];
 #pragma unroll
         for (int i = 0; i < MW; ++i) af[i] = A::read(pa, wr + WR * i, j, lane);

@@ -27,8 +27,8 @@ inline long long ragged_max_tiles(long long S, long long N, int tm) {
 // `gaps` is set; with `each`, a group without rows has one tile of none.  Offsets are clamped to 0 .. S, so whatever they hold, rows outside the
 // array are never named.  Lane l counts the tiles of `per` consecutive groups, one wave
 // scan places them: `per` + 2 loads and one scan, against a launch of its own for a tile
-// list.  Each load stands behind a condition of its own, so they come one after the other: three trips to the
-// cache up to 62 groups, some 70 for 4096, and `per` more to find a tile where it is over 1.
+// list.  Every load is made, at a place that is there, and what it does not count for dropped, so that a lane's loads
+// go out together: a trip to the cache for four of them, and again to find a tile where `per` is over 1.
 struct RaggedTiles {
   const int32_t *offsets;
   int N, S, tm, per, cnt, inc, total;
@@ -38,7 +38,8 @@ struct RaggedTiles {
 
   // boundary i of the N + 2 groups: 0, offsets[0], .., offsets[N], S
   __device__ __forceinline__ int bound(int i) const {
-    return i <= 0 ? 0 : i > N + 1 ? S : min(max(offsets[i - 1], 0), S);
+    const int v = min(max(offsets[min(max(i - 1, 0), N)], 0), S);
+    return i <= 0 ? 0 : i > N + 1 ? S : v;
   }
   __device__ __forceinline__ int tiles(int p, int lo, int hi) const {
     if (p > N + 1 || ((p == 0 || p == N + 1) && !gaps)) return 0;
