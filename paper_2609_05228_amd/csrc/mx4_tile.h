@@ -82,7 +82,7 @@ template <int BLK, int BK_, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
   static __device__ __forceinline__ int swap(int r) { return CH == 4 ? r >> 2 : r >> 3; }
 
   // the copies of stage s, which is within k, and of its panel where there is a place for it
-  __device__ __forceinline__ void issue(int s, uint32_t lds, uint32_t panel, int wave, bool once) const {
+  __device__ __forceinline__ void issue(int s, uint32_t lds, uint32_t panel, int wave, bool) const {
     if (panel) {
       const uint32_t at = static_cast<uint32_t>(s / PANEL_STAGES) * 16u;
 #pragma unroll
@@ -96,10 +96,9 @@ template <int BLK, int BK_, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
 #pragma unroll
     for (int t = 0; t < NU; ++t) {
       const uint32_t to = lds + min(wave * NU + t, UNITS) * kUnitBytes;
-      if (once)
-        dma16_buf_stream(rsrc, in ? voff[t] : kOutside, to);
-      else
-        dma16_buf(rsrc, in ? voff[t] : kOutside, to);
+      // no non-temporal hint: a stage takes half or a quarter of a line of each row, and the next ones the rest (products
+      // of 256 rows in 128 groups, 2048 x 768: 35.4 us with the hint, 29.1 without)
+      dma16_buf(rsrc, in ? voff[t] : kOutside, to);
     }
   }
 
