@@ -363,11 +363,14 @@ struct DenseTile {
   using B = Operand<T, BDOWN, NB, sizeof(T) == 2, WR * WC, MATS>;
   using Ref = TileRef<T, typename A::Src, typename B::Src>;
 
-  // adds a stage's products; blocks past the tile's rows are read too and not multiplied
+  // adds a stage's products, and calls mid halfway; blocks past the tile's rows are read too and not multiplied
+  template <typename M>
   static __device__ __forceinline__ void multiply(const uint8_t *pa, const uint8_t *pb, const uint8_t *, const uint8_t *,
-                                                  int wr, int wc, int lane, int rows, int, int, f32x4_t (&acc)[MW][NW]) {
+                                                  int wr, int wc, int lane, int rows, int, int, f32x4_t (&acc)[MW][NW],
+                                                  M mid) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+      if (h == 1) mid();
       typename B::frag_t bf[NW];
       typename A::frag_t af[MW];
 #pragma unroll
@@ -440,6 +443,17 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
   int sa = 0, sb = 0;                                               // slots of the stage multiplied next
   [[maybe_unused]] int qa = DA - 1, qb = DB - 1;                    // and of its panels
   int warm = DA - 1;   // the first stages wait for everything
+  auto copies = [&]() {
+    if (fa.pi < SEG * n) issue_a();
+    if (fb.pi < SEG * n) {
+      issue_b();
+      warm = max(warm - 1, 0);
+    } else {
+      warm = 1;
+    }
+  };
+  // of the two waves of a SIMD one copies before its products and one between them
+  const bool late = S::WR * S::WC == 8 && wave >= 4;
   for (int ci = 0; ci < n; ++ci) {
     f32x4_t acc[MW][NW];
     auto clear = [](f32x4_t (&c)[MW][NW]) {
@@ -473,18 +487,14 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
           stage_barrier<PENDING>();
         else
           stage_barrier<0>();
-        if (fa.pi < SEG * n) issue_a();
-        if (fb.pi < SEG * n) {
-          issue_b();
-          warm = max(warm - 1, 0);
-        } else {
-          warm = 1;
-        }
+        if (!late) copies();
         const int ks = kt + rot < nk ? kt + rot : kt + rot - nk;
         if (A::PANEL > 0 && ks % A::PANEL_STAGES == 0) qa = qa + 1 == DA ? 0 : qa + 1;
         if (B::PANEL > 0 && ks % B::PANEL_STAGES == 0) qb = qb + 1 == DB ? 0 : qb + 1;
         S::multiply(smem + sa * A::BYTES, smem + RING_A + sb * B::BYTES, smem + DA * A::BYTES + qa * A::PANEL,
-                    smem + RING_A + DB * B::BYTES + qb * B::PANEL, wr, wc, lane, t.rows, ks * BK, t.klen, acc);
+                    smem + RING_A + DB * B::BYTES + qb * B::PANEL, wr, wc, lane, t.rows, ks * BK, t.klen, acc, [&]() {
+                      if (late) copies();
+                    });
         if (sizeof(T) == 4 && (kt + 1) % kFlush == 0) flush();
         sa = sa + 1 == DA ? 0 : sa + 1;
         sb = sb + 1 == DB ? 0 : sb + 1;

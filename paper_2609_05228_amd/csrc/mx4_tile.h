@@ -193,9 +193,10 @@ template <bool ROWS4, int BK, int MB_, int NB_, int WR_, int WC_, int DA_, int D
   static constexpr int LDS = DA * (A::BYTES + A::PANEL) + DB * (B::BYTES + B::PANEL);
   static_assert(!ROWS4 || BK == 128, "the scaled instruction's k");
 
+  template <typename M>
   static __device__ __forceinline__ void multiply(const uint8_t *pa, const uint8_t *pb, const uint8_t *qa, const uint8_t *qb,
                                                   int wr, int wc, int lane, int rows, int k, int klen,
-                                                  f32x4_t (&acc)[MW][NW]) {
+                                                  f32x4_t (&acc)[MW][NW], M mid) {
     typename B::codes_t bq[NW];
     int bs[NW];
 #pragma unroll
@@ -213,16 +214,19 @@ template <bool ROWS4, int BK, int MB_, int NB_, int WR_, int WC_, int DA_, int D
       }
       auto wide = [](i32x4_t v) { return i32x8_t{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; };
 #pragma unroll
-      for (int i = 0; i < MW; ++i)
+      for (int i = 0; i < MW; ++i) {
+        if (i == MW / 2) mid();
         if (16 * (wr + WR * i) < rows) {  // wave-uniform
 #pragma unroll
           for (int j = 0; j < NW; ++j)    // 4: both operands in this format
             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(bq[j]), wide(aq[i]), acc[i][j], 4, 4, 0, bs[j],
                                                                         0, as[i]);
         }
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < BK / 32; ++j) {
+        if (j == BK / 64) mid();
         bf16x8_t bf[NW], af[MW];
 #pragma unroll
         for (int i = 0; i < MW; ++i) af[i] = A::read(pa, wr + WR * i, j, lane);
