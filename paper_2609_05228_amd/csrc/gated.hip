@@ -63,6 +63,29 @@ __global__ __launch_bounds__(WR *WC * 64) void gated_rows_kernel(GatedArgs g) {
   gated_rows<T, LINES, MB, NB, WR, WC, DA, DB>(g, RaggedTiles(g.offsets, g.N, g.S, 16 * MB, g.fill), smem);
 }
 
+// The same with the tile's height taken here, from the groups' sizes that only the device knows: a group's last row tile
+// costs about a full one.  Rounds of a CU times the time of a stage in units of 50 ns, measured on 128 groups of 768 x
+// 2048 with 128 and 256 rows (the weights' way from memory in it): 192 rows 1.5 us, 256 1.8, 320 2.5.  32768 rows with g
+// and u kept: 286, 312 and 264 us; 16384 rows without: 155, 165 and 176.
+template <bool LINES> __global__ __launch_bounds__(512) void gated_shapes_kernel(GatedArgs g) {
+  __shared__ __align__(16) uint8_t smem[160 * 1024];
+  const int heights[3] = {192, 256, 320};
+  int tiles[3];
+  RaggedTiles::count(g.offsets, g.N, g.S, heights, tiles, g.fill);
+  const int slots = static_cast<int>(gridDim.x);
+  auto cost = [&](int h, int stage) {
+    const long long items = static_cast<long long>(tiles[h]) * ((g.M + 127) / 128);
+    return (items + slots - 1) / slots * stage;
+  };
+  const long long c192 = cost(0, 30), c256 = cost(1, 36), c320 = cost(2, 50);
+  if (c192 <= min(c256, c320))
+    gated_rows<bf16_t, LINES, 12, 16, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 192, g.fill), smem);
+  else if (c256 <= c320)
+    gated_rows<bf16_t, LINES, 16, 16, 4, 2, 2, 3>(g, RaggedTiles(g.offsets, g.N, g.S, 256, g.fill), smem);
+  else
+    gated_rows<bf16_t, LINES, 20, 16, 4, 2, 2, 2>(g, RaggedTiles(g.offsets, g.N, g.S, 320, g.fill), smem);
+}
+
 // What the epilogue does, from the fp32 parts of g and u (summed in order) or the kept g and u: 4 features a thread.
 // Rows of no group: zeros into a, g and u with `fill`, else they stay (dg and du of them are never read).
 template <typename T, int ACT> __global__ __launch_bounds__(256) void gated_join_kernel(GatedArgs g) {
@@ -159,10 +182,10 @@ using Gated64 = TileShape<4, 4, 4, 1, 4, 4>;     // bf16: few tiles, deep rings
 using GradX64 = TileShape<4, 4, 2, 2, 4, 4>;
 using Gated64x128 = TileShape<4, 8, 2, 2, 3, 3>;  // bf16: a few rows a group
 using Gated128 = TileShape<8, 8, 2, 2, 2, 3>;     // bf16
-using Gated256 = TileShape<16, 16, 4, 2, 2, 3>;   // bf16
+using GradX256 = TileShape<16, 16, 4, 2, 2, 3>;   // bf16
 using GatedF32 = TileShape<2, 4, 2, 2, 3, 3>;     // fp32
 
-enum class Kind { k64, k64x128, k128, k256, kF32 };
+enum class Kind { k64, k64x128, k128, kLarge, kF32 };
 struct Plan {
   Kind kind;
   int splits;
@@ -181,7 +204,7 @@ Plan plan_rows(long long S, long long N, int cols, long long klen, size_t elems,
   if (S <= 32 * N) return {Kind::k64x128, 1};
   const long long items = about_tiles(S, N, Gated128::TM) * tiles_of(cols, Gated128::TN);
   const bool large = S > 80 * N && items >= kCUs * Gated128::PER_CU;
-  return {large ? Kind::k256 : Kind::k128, 1};
+  return {large ? Kind::kLarge : Kind::k128, 1};
 }
 Plan plan_gated(const GatedArgs &g, bool bf16) {
   return plan_rows(g.S, g.N, 2 * g.M, g.K, 2 * static_cast<size_t>(g.S) * g.M, bf16);
@@ -192,11 +215,15 @@ Plan plan_grad_x(const GatedArgs &g, bool bf16) {
 
 bool lines(const void *p) { return reinterpret_cast<uintptr_t>(p) % 128 == 0; }
 
+// whether rows of all that the projections' kernel writes are whole 128-byte lines (see put16)
+bool gated_lines(const GatedArgs &g, size_t es) {
+  return g.M * es % 128 == 0 && lines(g.a) && lines(g.g) && lines(g.u) && lines(g.dg) && lines(g.du);
+}
+
 template <typename T, class Sh> void launch_gated_shape(const GatedArgs &g, hipStream_t s) {
   const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(g.M, Sh::TN / 2) * g.splits;
   auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(g); };
-  const bool whole = g.M * sizeof(T) % 128 == 0 && lines(g.a) && lines(g.g) && lines(g.u) && lines(g.dg) && lines(g.du);
-  if (whole)
+  if (gated_lines(g, sizeof(T)))
     launch(gated_rows_kernel<T, true, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
   else
     launch(gated_rows_kernel<T, false, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
@@ -242,7 +269,12 @@ hipError_t launch_gated(GatedArgs g, bool bf16, hipStream_t s) {
     case Kind::k64: launch_gated_shape<bf16_t, Gated64>(g, s); break;
     case Kind::k64x128: launch_gated_shape<bf16_t, Gated64x128>(g, s); break;
     case Kind::k128: launch_gated_shape<bf16_t, Gated128>(g, s); break;
-    case Kind::k256: launch_gated_shape<bf16_t, Gated256>(g, s); break;
+    case Kind::kLarge:
+      if (gated_lines(g, 2))
+        gated_shapes_kernel<true><<<kCUs, 512, 0, s>>>(g);
+      else
+        gated_shapes_kernel<false><<<kCUs, 512, 0, s>>>(g);
+      break;
     case Kind::kF32: launch_gated_shape<float, GatedF32>(g, s); break;
   }
   const hipError_t e = hipGetLastError();
@@ -264,7 +296,7 @@ hipError_t launch_gated_grad_x(GatedArgs g, bool bf16, hipStream_t s) {
     case Kind::k64: launch_grad_x_shape<bf16_t, GradX64>(g, s); break;
     case Kind::k64x128: launch_grad_x_shape<bf16_t, Gated64x128>(g, s); break;
     case Kind::k128: launch_grad_x_shape<bf16_t, Gated128>(g, s); break;
-    case Kind::k256: launch_grad_x_shape<bf16_t, Gated256>(g, s); break;
+    case Kind::kLarge: launch_grad_x_shape<bf16_t, GradX256>(g, s); break;
     case Kind::kF32: launch_grad_x_shape<float, GatedF32>(g, s); break;
   }
   const hipError_t e = hipGetLastError();

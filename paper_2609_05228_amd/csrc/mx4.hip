@@ -86,15 +86,15 @@ template <typename T> __global__ __launch_bounds__(256) void mx4_dequantize_kern
   }
 }
 
-// Tiles of 16 MB rows of one group x 16 NB columns (gated, MATS = 2: 8 NB features of both projections)
-template <bool ROWS4, bool LINES, int MATS, int BK, int MB, int NB, int WR, int WC, int DA, int DB>
-__global__ __launch_bounds__(WR *WC * 64) void mx4_rows_kernel(Mx4Args m) {
-  using S = Mx4Tile<ROWS4, BK, MB, NB, WR, WC, DA, DB, MATS>;
+// Tiles of 16 MB rows of one group x 16 NB columns (gated, MATS = 2: 8 NB features of both projections), the whole work
+// of a workgroup
+template <class S, bool LINES, int MATS>
+__device__ __forceinline__ void mx4_rows(const Mx4Args &m, uint8_t *smem) {
   static_assert(MATS == 1 || S::NW % 4 == 0, "gated: a wave holds whole pairs of feature blocks");
-  constexpr int BF = 16 * NB / MATS;
-  __shared__ __align__(16) uint8_t smem[S::LDS];
+  constexpr bool ROWS4 = S::ROWS4;
+  constexpr int BF = 16 * S::NB / MATS;
   const GatedArgs &g = m.g;
-  const RaggedTiles tiles(g.offsets, g.N, g.S, 16 * MB, g.fill);
+  const RaggedTiles tiles(g.offsets, g.N, g.S, 16 * S::MB, g.fill);
   const int nN = (g.M + BF - 1) / BF, per = nN * g.splits;
   const Share share(static_cast<long long>(tiles.total) * per);
   const uint32_t code_row = static_cast<uint32_t>(g.K) / 2, scale_row = mx4_scale_row(g.K);
@@ -139,22 +139,50 @@ __global__ __launch_bounds__(WR *WC * 64) void mx4_rows_kernel(Mx4Args m) {
   }
 }
 
-template <bool ROWS4_, int BK_, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_> struct Mx4Shape {
-  static constexpr bool ROWS4 = ROWS4_;
-  static constexpr int BK = BK_, MB = MB_, NB = NB_, WR = WR_, WC = WC_, DA = DA_, DB = DB_;
-  static constexpr int TM = 16 * MB, TN = 16 * NB, THREADS = WR * WC * 64;
-  static constexpr int LDS = Mx4Tile<ROWS4, BK, MB, NB, WR, WC, DA, DB, NB % 4 == 0 ? 2 : 1>::LDS;
-  static constexpr int PER_CU = 160 * 1024 / LDS;
+template <class Sh, bool LINES, int MATS> __global__ __launch_bounds__(Sh::THREADS) void mx4_rows_kernel(Mx4Args m) {
+  using S = typename Sh::template Tile<MATS>;
+  __shared__ __align__(16) uint8_t smem[S::LDS];
+  mx4_rows<S, LINES, MATS>(m, smem);
+}
+
+// The same with one of two shapes taken here, from the groups' sizes that only the device knows
+template <class Low, class High, bool LINES, int MATS>
+__global__ __launch_bounds__(512) void mx4_shapes_kernel(Mx4Args m) {
+  using SL = typename Low::template Tile<MATS>;
+  using SH = typename High::template Tile<MATS>;
+  static_assert(Low::THREADS == 512 && High::THREADS == 512, "one launch");
+  __shared__ __align__(16) uint8_t smem[SL::LDS > SH::LDS ? SL::LDS : SH::LDS];
+  const GatedArgs &g = m.g;
+  const int heights[2] = {Low::TM, High::TM};
+  int tiles[2];
+  RaggedTiles::count(g.offsets, g.N, g.S, heights, tiles, g.fill);
+  const int slots = static_cast<int>(gridDim.x);
+  auto cost = [&](int h, int width, int k128) {
+    const long long items = static_cast<long long>(tiles[h]) * ((MATS * g.M + width - 1) / width);
+    return (items + slots - 1) / slots * k128;
+  };
+  if (cost(0, Low::TN, Low::COST) <= cost(1, High::TN, High::COST))
+    mx4_rows<SL, LINES, MATS>(m, smem);
+  else
+    mx4_rows<SH, LINES, MATS>(m, smem);
+}
+
+// COST: time of 128 k of a tile with every CU busy, in units of 50 ns
+template <bool ROWS4, int BK, int MB, int NB, int WR, int WC, int DA, int DB, int COST_ = 0> struct Mx4Shape {
+  template <int MATS> using Tile = Mx4Tile<ROWS4, BK, MB, NB, WR, WC, DA, DB, MATS>;
+  static constexpr int TM = 16 * MB, TN = 16 * NB, THREADS = WR * WC * 64, COST = COST_;
+  static constexpr int PER_CU = 160 * 1024 / Tile<1>::LDS;
   static_assert(PER_CU >= 1, "fits a CU");
 };
 // bf16 rows
 using Wide16 = Mx4Shape<false, 128, 1, 16, 1, 4, 3, 3>;
 using Wide64 = Mx4Shape<false, 128, 4, 8, 2, 2, 3, 3>;
-using Wide256 = Mx4Shape<false, 64, 16, 16, 4, 2, 3, 3>;
+using Wide192 = Mx4Shape<false, 128, 12, 16, 2, 4, 2, 2>;
 // rows in 4 bits
 using Four16 = Mx4Shape<true, 128, 1, 16, 1, 4, 3, 3>;
 using Four64 = Mx4Shape<true, 128, 4, 8, 2, 2, 4, 4>;
-using Four256 = Mx4Shape<true, 128, 16, 16, 2, 4, 3, 3>;
+using Four256 = Mx4Shape<true, 128, 16, 16, 4, 2, 3, 3, 30>;
+using Four320 = Mx4Shape<true, 128, 20, 12, 4, 2, 3, 3, 38>;
 
 enum class Kind { k16, k64, kLarge };
 struct Plan {
@@ -175,17 +203,20 @@ Plan plan_mx4(const Mx4Args &m) {
   return {g.S <= 96ll * g.N ? Kind::k64 : Kind::kLarge, 1};
 }
 
+bool lines(const GatedArgs &g) { return g.M % 64 == 0 && reinterpret_cast<uintptr_t>(g.a) % 128 == 0; }
+
 template <class Sh, int MATS> void launch_shape(const Mx4Args &m, hipStream_t s) {
   const GatedArgs &g = m.g;
-  const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(g.M, Sh::TN / MATS) * g.splits;
+  const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(MATS * g.M, Sh::TN) * g.splits;
   auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(m); };
-  if (g.M % 64 == 0 && reinterpret_cast<uintptr_t>(g.a) % 128 == 0)
-    launch(mx4_rows_kernel<Sh::ROWS4, true, MATS, Sh::BK, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
-  else
-    launch(mx4_rows_kernel<Sh::ROWS4, false, MATS, Sh::BK, Sh::MB, Sh::NB, Sh::WR, Sh::WC, Sh::DA, Sh::DB>);
+  lines(g) ? launch(mx4_rows_kernel<Sh, true, MATS>) : launch(mx4_rows_kernel<Sh, false, MATS>);
 }
 template <class Sh> void launch_kind(const Mx4Args &m, hipStream_t s) {
   m.gated ? launch_shape<Sh, 2>(m, s) : launch_shape<Sh, 1>(m, s);
+}
+template <class Low, class High, int MATS> void launch_shapes(const Mx4Args &m, hipStream_t s) {
+  auto launch = [&](auto kernel) { kernel<<<kCUs, 512, 0, s>>>(m); };
+  lines(m.g) ? launch(mx4_shapes_kernel<Low, High, true, MATS>) : launch(mx4_shapes_kernel<Low, High, false, MATS>);
 }
 
 unsigned convert_grid(uint32_t total) { return std::min<uint32_t>((total + 15) / 16, 16 * kCUs); }
@@ -206,7 +237,12 @@ hipError_t launch_mx4(Mx4Args m, hipStream_t s) {
   switch (p.kind) {
     case Kind::k16: four ? launch_kind<Four16>(m, s) : launch_kind<Wide16>(m, s); break;
     case Kind::k64: four ? launch_kind<Four64>(m, s) : launch_kind<Wide64>(m, s); break;
-    case Kind::kLarge: four ? launch_kind<Four256>(m, s) : launch_kind<Wide256>(m, s); break;
+    case Kind::kLarge:
+      if (four)
+        m.gated ? launch_shape<Four256, 2>(m, s) : launch_shapes<Four256, Four320, 1>(m, s);
+      else
+        launch_kind<Wide192>(m, s);
+      break;
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;

@@ -183,8 +183,9 @@ __device__ __forceinline__ bf16x8_t mx4_to_bf16(uint32_t codes, float scale) {
 
 // Tiles of bf16 results (see DenseTile) on 4-bit weights: rows in bf16 (ROWS4 = false) by bf16 matrix instructions on
 // the weights' exact values, or rows in 4 bits too, by the scaled instruction
-template <bool ROWS4, int BK, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_, int MATS> struct Mx4Tile {
+template <bool ROWS4_, int BK, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_, int MATS> struct Mx4Tile {
   using T = bf16_t;
+  static constexpr bool ROWS4 = ROWS4_;
   static constexpr int MB = MB_, NB = NB_, WR = WR_, WC = WC_, DA = DA_, DB = DB_, SEG = 1;
   static constexpr int MW = MB / WR, NW = NB / WC;
   using A = std::conditional_t<ROWS4, Mx4Operand<MB, BK, false, WR * WC>, Mx4Rows<MB, BK, WR * WC>>;
