@@ -370,7 +370,12 @@ struct DenseTile {
                                                   M mid) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (h == 1) mid();
+      if (h == 1) {
+        mid();
+        // fp32: keeps the halves apart; as one block the compiler moves the sums from and to the accumulation registers with
+        // every stage (products of 2069 rows in 32 groups of 512 x 1024: 50.8 us, 45.9 so)
+        if (sizeof(T) == 4) asm volatile("" ::: "memory");
+      }
       typename B::frag_t bf[NW];
       typename A::frag_t af[MW];
 #pragma unroll
