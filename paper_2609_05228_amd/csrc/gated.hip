@@ -20,8 +20,9 @@ namespace ace {
 
 namespace {
 
-// Both projections in tiles of 16 MB rows of one group x 8 NB features: the whole work of a workgroup
-template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
+// Both projections in tiles of 16 MB rows of one group x 8 NB features: the whole work of a workgroup.  KS > 1 (shapes of
+// one wave): its KS waves split the reduction of each tile.
+template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB, int KS = 1>
 __device__ __forceinline__ void gated_rows(const GatedArgs &g, const RaggedTiles &tiles, uint8_t *smem) {
   using S = DenseTile<T, false, false, MB, NB, WR, WC, DA, DB, 2>;
   static_assert(sizeof(T) == 4 || S::NW % 4 == 0, "a wave holds whole pairs of feature blocks");
@@ -30,7 +31,9 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &g, const RaggedTiles
   const Share share(static_cast<long long>(tiles.total) * per);
   auto ref = [&](const Item &it, int) {
     const int f0 = it.tile * BF;
-    const Part k = part_of<S::A::BK>(it.group < 0 ? 0 : g.K, it.split, g.splits);
+    const int klen = it.group < 0 ? 0 : g.K;
+    const Part k = KS > 1 ? part_of<S::A::BK>(klen, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), KS)
+                          : part_of<S::A::BK>(klen, it.split, g.splits);
     const size_t w = (static_cast<size_t>(max(it.group, 0)) * g.M + f0) * g.K + k.k0;
     GatedRef<S> t;
     t.a.p[0] = static_cast<const T *>(g.x) + static_cast<size_t>(it.row0) * g.K + k.k0;
@@ -51,10 +54,25 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &g, const RaggedTiles
     const long long i = share.item(done);
     const RaggedTile t = tiles.find(static_cast<int>(i / per));
     const int q = static_cast<int>(i % per);
+    const Item item{t.group, t.row0, t.rows, q % nN, t.only, q / nN};
     __syncthreads();  // every wave is done with the rings
-    grouped_items<S>(Item{t.group, t.row0, t.rows, q % nN, t.only, q / nN}, n, g.K, g.K, smem, ref,
-                     GatedStore<T, LINES, S>{g});
+    if constexpr (KS > 1) {
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      grouped_items<S>(item, n, g.K, g.K, smem + wave * S::LDS, ref,
+                       JoinStore<S, KS, GatedStore<T, LINES, S>>{{g}, smem + KS * S::LDS, 0});
+    } else {
+      grouped_items<S>(item, n, g.K, g.K, smem, ref, GatedStore<T, LINES, S>{g});
+    }
   }
+}
+
+// Few rows: tiles of 16, the reduction over the workgroup's four waves
+constexpr int kSplitWaves = 4;
+template <bool LINES> __global__ __launch_bounds__(64 * kSplitWaves) void gated_few_kernel(GatedArgs g) {
+  using S = DenseTile<bf16_t, false, false, 1, 4, 1, 1, 3, 3, 2>;
+  using J = JoinStore<S, kSplitWaves, GatedStore<bf16_t, LINES, S>>;
+  __shared__ __align__(16) uint8_t smem[kSplitWaves * S::LDS + J::LDS];
+  gated_rows<bf16_t, LINES, 1, 4, 1, 1, 3, 3, kSplitWaves>(g, RaggedTiles(g.offsets, g.N, g.S, 16, g.fill), smem);
 }
 
 template <typename T, bool LINES, int MB, int NB, int WR, int WC, int DA, int DB>
@@ -97,6 +115,7 @@ template <typename T, int ACT> __global__ __launch_bounds__(256) void gated_join
     f32x4_t vg{0.f, 0.f, 0.f, 0.f}, vu = vg;
     if (i >= first && i < last) {
       if (g.splits > 1) {
+#pragma unroll 4
         for (int s = 0; s < g.splits; ++s) {
           const float *p = g.part + 2 * s * total + i;
           const f32x4_t a = *reinterpret_cast<const f32x4_t *>(p), b = *reinterpret_cast<const f32x4_t *>(p + total);
@@ -185,7 +204,7 @@ using Gated128 = TileShape<8, 8, 2, 2, 2, 3>;     // bf16
 using GradX256 = TileShape<16, 16, 4, 2, 2, 3>;   // bf16
 using GatedF32 = TileShape<2, 4, 2, 2, 3, 3>;     // fp32
 
-enum class Kind { k64, k64x128, k128, kLarge, kF32 };
+enum class Kind { kFew, k64, k64x128, k128, kLarge, kF32 };
 struct Plan {
   Kind kind;
   int splits;
@@ -207,6 +226,12 @@ Plan plan_rows(long long S, long long N, int cols, long long klen, size_t elems,
   return {large ? Kind::kLarge : Kind::k128, 1};
 }
 Plan plan_gated(const GatedArgs &g, bool bf16) {
+  // a few rows a group: tiles of 16 with the reduction over the waves of a workgroup, against larger ones with parts of the
+  // reduction and a launch that adds them (kernel times on 128 groups of 768 x 2048: 8 rows 13.7 us against 21.4, 256 rows
+  // 113 against 119, 1024 rows 126 against 123; one group of 4096 x 4096: 16 rows 18.1 against 21.4, 64 rows of half of
+  // it 23 against 20.4)
+  if (bf16 && (g.S <= 4ll * g.N || (g.S <= 16ll * g.N && about_tiles(g.S, g.N, 16) * tiles_of(g.M, 32) <= 2 * kCUs)))
+    return {Kind::kFew, 1};
   return plan_rows(g.S, g.N, 2 * g.M, g.K, 2 * static_cast<size_t>(g.S) * g.M, bf16);
 }
 Plan plan_grad_x(const GatedArgs &g, bool bf16) {
@@ -266,6 +291,14 @@ hipError_t launch_gated(GatedArgs g, bool bf16, hipStream_t s) {
   const Plan p = plan_gated(g, bf16);
   g.splits = p.splits;
   switch (p.kind) {
+    case Kind::kFew: {
+      const unsigned grid = grouped_grid(ragged_max_tiles(g.S, g.N, 16) * tiles_of(g.M, 32), 1);
+      if (gated_lines(g, 2))
+        gated_few_kernel<true><<<grid, 64 * kSplitWaves, 0, s>>>(g);
+      else
+        gated_few_kernel<false><<<grid, 64 * kSplitWaves, 0, s>>>(g);
+      break;
+    }
     case Kind::k64: launch_gated_shape<bf16_t, Gated64>(g, s); break;
     case Kind::k64x128: launch_gated_shape<bf16_t, Gated64x128>(g, s); break;
     case Kind::k128: launch_gated_shape<bf16_t, Gated128>(g, s); break;
@@ -293,6 +326,7 @@ hipError_t launch_gated_grad_x(GatedArgs g, bool bf16, hipStream_t s) {
   const Plan p = plan_grad_x(g, bf16);
   g.splits = p.splits;
   switch (p.kind) {
+    case Kind::kFew:
     case Kind::k64: launch_grad_x_shape<bf16_t, GradX64>(g, s); break;
     case Kind::k64x128: launch_grad_x_shape<bf16_t, Gated64x128>(g, s); break;
     case Kind::k128: launch_grad_x_shape<bf16_t, Gated128>(g, s); break;

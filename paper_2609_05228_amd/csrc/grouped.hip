@@ -183,6 +183,7 @@ template <typename T> __global__ __launch_bounds__(256) void grouped_join_kernel
 #pragma unroll
     for (int j = 0; j < E; ++j) v[j] = 0.f;
     if (i >= first && i < last) {
+#pragma unroll 4
       for (int s = 0; s < g.splits; ++s) {
         const float *p = g.part + s * total + i;
 #pragma unroll

@@ -183,9 +183,12 @@ template <typename T, bool DOWN, int BLK, bool PAIR, int W, int MATS = 1> struct
   }
 };
 
-// waits for this wave's LDS reads and all but n of its copies, then for the workgroup
-template <int N> __device__ __forceinline__ void stage_barrier() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+// waits for this wave's LDS reads and all but n of its copies, then for the workgroup (ALONE: the rings are the wave's own)
+template <int N, bool ALONE> __device__ __forceinline__ void stage_barrier() {
+  if constexpr (ALONE)
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  else
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 // One tile of C in a workgroup's list: rows and columns of the output, and the group
@@ -358,7 +361,7 @@ template <typename T_, bool ADOWN, bool BDOWN, int MB_, int NB_, int WR_, int WC
 struct DenseTile {
   using T = T_;
   static constexpr int MB = MB_, NB = NB_, WR = WR_, WC = WC_, DA = DA_, DB = DB_, SEG = SEG_;
-  static constexpr int MW = MB / WR, NW = NB / WC;
+  static constexpr int MW = MB / WR, NW = NB / WC, LDS = (DA * MB + DB * NB) * 2 * kUnitBytes;
   using A = Operand<T, ADOWN, MB, false, WR * WC>;
   using B = Operand<T, BDOWN, NB, sizeof(T) == 2, WR * WC, MATS>;
   using Ref = TileRef<T, typename A::Src, typename B::Src>;
@@ -398,7 +401,8 @@ struct DenseTile {
 // stages of a tile's operands are copied DA - 1 and DB - 1 ahead of their use through rings of DA
 // and DB LDS slots, and across the end of a tile, so the next tile's first stages are under way
 // while a tile ends and stores.  Where PENDING is 0 (both rings two deep: the weights' gradient in 256 x 256 tiles) the
-// next tile's first products wait for those stores.  ref(item, segment) gives a tile's operands; lda, ldb are common;
+// next tile's first products wait for those stores.  A shape of one wave is a pipeline of its own for each wave, which
+// waits for no other; smem is then that wave's.  ref(item, segment) gives a tile's operands; lda, ldb are common;
 // store(ref, sums, wr, wc, lane) puts a wave's share of the sums where they belong.
 template <class S, typename F, typename E>
 __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, int ldb, uint8_t *smem, F ref, E store) {
@@ -417,7 +421,8 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
   static_assert(MB % WR == 0 && NB % WC == 0 && (!PAIR || NW % 2 == 0), "whole blocks, in bf16 pairs of column blocks, per wave");
   static_assert(DA >= 2 && DB >= DA && PENDING <= 63, "ring depths, outstanding copies within the wait counter");
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr bool ALONE = WR * WC == 1;
+  const int wave = ALONE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave / WC, wc = wave % WC;
   constexpr int RING_A = DA * (A::BYTES + A::PANEL);
   const uint32_t ldsa = lds_addr(smem), ldsb = ldsa + RING_A;
@@ -489,9 +494,9 @@ __device__ __forceinline__ void grouped_items(const Item &list, int n, int lda, 
         // this stage landed for every wave, and every wave is done with the slots refilled next;
         // while B still had a stage to copy one iteration ago, the count is the constant one
         if (PENDING > 0 && warm == 0)
-          stage_barrier<PENDING>();
+          stage_barrier<PENDING, ALONE>();
         else
-          stage_barrier<0>();
+          stage_barrier<0, ALONE>();
         if (!late) copies();
         const int ks = kt + rot < nk ? kt + rot : kt + rot - nk;
         if (A::PANEL > 0 && ks % A::PANEL_STAGES == 0) qa = qa + 1 == DA ? 0 : qa + 1;
@@ -525,6 +530,42 @@ template <typename T, bool LINES, class S> struct StoreTile {
       store_part<T, S::MW, S::NW, S::WR>(t.part, t.rows, t.cols, ldo, sum, wr, 16 * wc * S::NW, lane);
     else
       store_rows<T, LINES, S::MW, S::NW, S::WR>(t.out, t.rows, t.cols, ldo, sum, wr, 16 * wc * S::NW, lane);
+  }
+};
+
+// The reduction of a tile of 16 rows split over the KS waves of a workgroup, each with a pipeline of its own (shapes of
+// one wave): their sums meet in LDS, the first wave adds them up in order and stores.  Two places in turn, so that one wait
+// per tile is enough: the first wave has read a place before it comes to the wait behind which it is written again.
+template <class S, int KS, class E> struct JoinStore {
+  static constexpr int PLACE = (KS - 1) * 64 * 16 * S::NW, LDS = 2 * PLACE;
+  static_assert(S::MW == 1 && S::WR * S::WC == 1 && sizeof(typename S::T) == 2, "tiles of one wave, 16 rows");
+  E store;
+  uint8_t *smem;
+  int turn;
+  template <class R>
+  __device__ __forceinline__ void operator()(const R &t, const f32x4_t (&sum)[1][S::NW], int wr, int wc, int lane) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    f32x4_t *place = reinterpret_cast<f32x4_t *>(smem + turn * PLACE) + lane;
+    turn ^= 1;
+    if (wave > 0) {
+#pragma unroll
+      for (int j = 0; j < S::NW; ++j) place[((wave - 1) * S::NW + j) * 64] = sum[0][j];
+    }
+    // LDS writes done; the copies under way need no wait
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (wave > 0) return;
+    f32x4_t all[1][S::NW];
+#pragma unroll
+    for (int j = 0; j < S::NW; ++j) {
+      all[0][j] = sum[0][j];
+#pragma unroll
+      for (int w = 0; w < KS - 1; ++w) {
+        const f32x4_t v = place[(w * S::NW + j) * 64];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) all[0][j][q] += v[q];
+      }
+    }
+    store(t, all, wr, wc, lane);
   }
 };
 

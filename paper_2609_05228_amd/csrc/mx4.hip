@@ -87,8 +87,8 @@ template <typename T> __global__ __launch_bounds__(256) void mx4_dequantize_kern
 }
 
 // Tiles of 16 MB rows of one group x 16 NB columns (gated, MATS = 2: 8 NB features of both projections), the whole work
-// of a workgroup
-template <class S, bool LINES, int MATS>
+// of a workgroup.  KS > 1 (shapes of one wave): its KS waves split the reduction of each tile.
+template <class S, bool LINES, int MATS, int KS = 1>
 __device__ __forceinline__ void mx4_rows(const Mx4Args &m, uint8_t *smem) {
   static_assert(MATS == 1 || S::NW % 4 == 0, "gated: a wave holds whole pairs of feature blocks");
   constexpr bool ROWS4 = S::ROWS4;
@@ -100,7 +100,9 @@ __device__ __forceinline__ void mx4_rows(const Mx4Args &m, uint8_t *smem) {
   const uint32_t code_row = static_cast<uint32_t>(g.K) / 2, scale_row = mx4_scale_row(g.K);
   auto ref = [&](const Item &it, int) {
     const int f0 = it.tile * BF;
-    const Part k = part_of<128>(it.group < 0 ? 0 : g.K, it.split, g.splits);
+    const int klen = it.group < 0 ? 0 : g.K, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // parts of whole 128 k: their scales are whole words
+    const Part k = KS > 1 ? part_of<128>(klen, wave, KS) : part_of<128>(klen, it.split, g.splits);
     GatedRef<S> t;
     if constexpr (ROWS4) {
       t.a.codes[0] = static_cast<const uint8_t *>(g.x) + static_cast<size_t>(it.row0) * code_row + k.k0 / 2;
@@ -132,11 +134,28 @@ __device__ __forceinline__ void mx4_rows(const Mx4Args &m, uint8_t *smem) {
     const int q = static_cast<int>(i % per);
     const Item item{t.group, t.row0, t.rows, q % nN, t.only, q / nN};
     __syncthreads();  // every wave is done with the rings
-    if constexpr (MATS == 2)
-      grouped_items<S>(item, n, g.K, g.K, smem, ref, GatedStore<bf16_t, LINES, S>{g});
-    else
-      grouped_items<S>(item, n, g.K, g.K, smem, ref, StoreTile<bf16_t, LINES, S>{static_cast<size_t>(g.M)});
+    using Store = std::conditional_t<MATS == 2, GatedStore<bf16_t, LINES, S>, StoreTile<bf16_t, LINES, S>>;
+    const Store store = [&]() -> Store {
+      if constexpr (MATS == 2)
+        return {g};
+      else
+        return {static_cast<size_t>(g.M)};
+    }();
+    if constexpr (KS > 1) {
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      grouped_items<S>(item, n, g.K, g.K, smem + wave * S::LDS, ref, JoinStore<S, KS, Store>{store, smem + KS * S::LDS, 0});
+    } else {
+      grouped_items<S>(item, n, g.K, g.K, smem, ref, store);
+    }
   }
+}
+
+// Few rows: tiles of 16, the reduction over the workgroup's four waves
+constexpr int kSplitWaves = 4;
+template <bool ROWS4, bool LINES, int MATS> __global__ __launch_bounds__(64 * kSplitWaves) void mx4_few_kernel(Mx4Args m) {
+  using S = Mx4Tile<ROWS4, 128, 1, 4, 1, 1, 3, 3, MATS>;
+  __shared__ __align__(16) uint8_t smem[kSplitWaves * S::LDS + JoinStore<S, kSplitWaves, int>::LDS];
+  mx4_rows<S, LINES, MATS, kSplitWaves>(m, smem);
 }
 
 template <class Sh, bool LINES, int MATS> __global__ __launch_bounds__(Sh::THREADS) void mx4_rows_kernel(Mx4Args m) {
@@ -184,15 +203,20 @@ using Four64 = Mx4Shape<true, 128, 4, 8, 2, 2, 4, 4>;
 using Four256 = Mx4Shape<true, 128, 16, 16, 4, 2, 3, 3, 30>;
 using Four320 = Mx4Shape<true, 128, 20, 12, 4, 2, 3, 3, 38>;
 
-enum class Kind { k16, k64, kLarge };
+enum class Kind { kFew, k16, k64, kLarge };
 struct Plan {
   Kind kind;
   int splits;
 };
 
+// Which kernel.  Few tiles of 16 rows x 64 columns: those, the reduction over the waves of a workgroup, against parts of the
+// reduction and a launch that adds them (kernel times: 8 rows in 128 groups of 768 x 2048 8.6 us against 12.8, 64 rows
+// in 64 groups 16.8 against 20.5, in one of 2048 x 4096 11.4 against 15.0).  More of them: 16 x 256 tiles up to 16 rows a
+// group (256 rows in 128 groups: 30 us against 34 in the small ones), 64 x 128 up to 96, then the large shapes.
 Plan plan_mx4(const Mx4Args &m) {
   const GatedArgs &g = m.g;
   const int mats = m.gated ? 2 : 1, cols = mats * g.M;
+  if (g.S <= 64ll * g.N && about_tiles(g.S, g.N, 16) * tiles_of(cols, 64) <= 4 * kCUs) return {Kind::kFew, 1};
   if (g.S <= 16ll * g.N || g.S <= 16) {
     const long long items = about_tiles(g.S, g.N, 16) * tiles_of(cols, Wide16::TN);
     return {Kind::k16, pick_splits(items, kCUs * Wide16::PER_CU, tiles_of(g.K, 128), static_cast<size_t>(g.S) * cols, 0.6)};
@@ -210,6 +234,11 @@ template <class Sh, int MATS> void launch_shape(const Mx4Args &m, hipStream_t s)
   const long long items = ragged_max_tiles(g.S, g.N, Sh::TM) * tiles_of(MATS * g.M, Sh::TN) * g.splits;
   auto launch = [&](auto kernel) { kernel<<<grouped_grid(items, Sh::PER_CU), Sh::THREADS, 0, s>>>(m); };
   lines(g) ? launch(mx4_rows_kernel<Sh, true, MATS>) : launch(mx4_rows_kernel<Sh, false, MATS>);
+}
+template <bool ROWS4, int MATS> void launch_few(const Mx4Args &m, hipStream_t s) {
+  const unsigned grid = grouped_grid(ragged_max_tiles(m.g.S, m.g.N, 16) * tiles_of(MATS * m.g.M, 64), 1);
+  auto launch = [&](auto kernel) { kernel<<<grid, 64 * kSplitWaves, 0, s>>>(m); };
+  lines(m.g) ? launch(mx4_few_kernel<ROWS4, true, MATS>) : launch(mx4_few_kernel<ROWS4, false, MATS>);
 }
 template <class Sh> void launch_kind(const Mx4Args &m, hipStream_t s) {
   m.gated ? launch_shape<Sh, 2>(m, s) : launch_shape<Sh, 1>(m, s);
@@ -235,6 +264,12 @@ hipError_t launch_mx4(Mx4Args m, hipStream_t s) {
   g.splits = p.splits;
   const bool four = m.x_scales != nullptr;
   switch (p.kind) {
+    case Kind::kFew:
+      if (four)
+        m.gated ? launch_few<true, 2>(m, s) : launch_few<true, 1>(m, s);
+      else
+        m.gated ? launch_few<false, 2>(m, s) : launch_few<false, 1>(m, s);
+      break;
     case Kind::k16: four ? launch_kind<Four16>(m, s) : launch_kind<Wide16>(m, s); break;
     case Kind::k64: four ? launch_kind<Four64>(m, s) : launch_kind<Wide64>(m, s); break;
     case Kind::kLarge:

@@ -46,10 +46,10 @@ template <int BLK, int BK_, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
   static constexpr int NP = (MATS * GROUPS + W - 1) / W;
   static constexpr int PANEL = MATS * GROUPS * kUnitBytes, PANEL_STAGES = kMx4Panel / BK;
   static_assert(BK == 64 || BK == 128, "a lane's k lie in one block");
-  static_assert(16 * BLK % RU == 0 && UNITS % MATS == 0 && (MATS == 1 || UNITS / MATS % NU == 0),
-                "units of one matrix, all of a wave's of the same");
+  static_assert(16 * BLK % RU == 0 && UNITS % MATS == 0 && (MATS == 1 || W == 1 || UNITS / MATS % NU == 0),
+                "units of one matrix, all of a wave's of the same where there are several waves");
 
-  const uint8_t *codes, *scales[NP];
+  const uint8_t *codes, *codes2, *scales[NP];
   uint32_t code_row, scale_row;  // bytes
   uint32_t code_span, scale_span;
   int klen, chunk_k;
@@ -63,7 +63,8 @@ template <int BLK, int BK_, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
     scale_span = static_cast<uint32_t>(valid) * scale_row;
     // offsets, not choices between pointers: those would be indexes into the arrays at run time and put them in memory
     codes = src.codes[0];
-    if (MATS == 2) codes += (src.codes[MATS - 1] - src.codes[0]) * (wave * NU >= UNITS / MATS);
+    codes2 = src.codes[MATS - 1];  // a lone wave's second half of units
+    if (MATS == 2 && W > 1) codes += (src.codes[MATS - 1] - src.codes[0]) * (wave * NU >= UNITS / MATS);
     const int r = lane / CH, chunk = (lane % CH) ^ swap(r & 15);
     chunk_k = 32 * chunk;
 #pragma unroll
@@ -92,13 +93,14 @@ template <int BLK, int BK_, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
     }
     const bool in = chunk_k < klen - s * BK;
     const uint32_t at = static_cast<uint32_t>(s) * (BK / 2);
-    const i32x4_rsrc rsrc = make_rsrc(codes + at, code_span - at);
+    const i32x4_rsrc first = make_rsrc(codes + at, code_span - at);
+    const i32x4_rsrc second = MATS == 2 && W == 1 ? make_rsrc(codes2 + at, code_span - at) : first;
 #pragma unroll
     for (int t = 0; t < NU; ++t) {
       const uint32_t to = lds + min(wave * NU + t, UNITS) * kUnitBytes;
       // no non-temporal hint: a stage takes half or a quarter of a line of each row, and the next ones the rest (products
       // of 256 rows in 128 groups, 2048 x 768: 35.4 us with the hint, 29.1 without)
-      dma16_buf(rsrc, in ? voff[t] : kOutside, to);
+      dma16_buf(t < UNITS / MATS ? first : second, in ? voff[t] : kOutside, to);
     }
   }
 
@@ -119,7 +121,8 @@ template <int BLK, int BK_, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
   // be anything, and is 0 here
   static __device__ __forceinline__ int read_scale(const uint8_t *panel, int blk, int lane, int k, int klen) {
     const int b = BK == 128 ? lane >> 4 : lane >> 5;  // of the stage's blocks
-    const int v = panel[at(blk, lane) * 16 + (k % kMx4Panel / kMx4Block + b)];
+    const int row = blk % MATS * (GROUPS * 64) + blk / MATS * 16 + (lane & 15);
+    const int v = panel[row * 16 + (k % kMx4Panel / kMx4Block + b)];
     return k + kMx4Block * b < klen ? v : 0;
   }
 };

@@ -47,7 +47,7 @@ def test_gated_refusals():
         assert _gated(**kw) == BAD, kw
     for kw in SIZES_UNS:
         assert _gated(**kw) == UNS, kw
-    few = dict(S=64, N=2, M=128, K=4096)
+    few = dict(S=64, N=2, M=128, K=4096, dtype=_lib.ACE_F32)
     n = ace.lib().ace_grouped_gated_workspace_size(_gated_desc(dict(few)))
     assert n > 0 and n % (2 * 64 * 128 * 4) == 0
     for kw in (dict(ws=0), dict(ws=P[15] + 16), dict(ws_bytes=n - 1)):
@@ -178,10 +178,10 @@ def test_mx4_product_refusals(gated):
         assert _mx4(gated, **kw) == BAD, kw
     for kw in (dict(S=BIG), dict(N=4097), dict(M=65544), dict(K=65568), dict(M=12), dict(K=48), dict(K=8)):
         assert _mx4(gated, **kw) == UNS, kw
-    few = dict(S=16, N=2, M=128, K=4096)
+    few = dict(S=512, N=1, M=512, K=4096)
     size = ace.lib().ace_grouped_mx4_workspace_size
     n = size(_lib.Mx4Desc(*few.values(), 0, 0), int(gated))
-    assert n > 0 and n % (16 * 128 * 4 * (2 if gated else 1)) == 0
+    assert n > 0 and n % (512 * 512 * 4 * (2 if gated else 1)) == 0
     for kw in (dict(ws=0), dict(ws=P[15] + 16), dict(ws_bytes=n - 1)):
         assert _mx4(gated, **few, **kw) == WSP, kw
     assert size(_lib.Mx4Desc(32768, 128, 768, 2048, 0, 0), int(gated)) == 0
