@@ -36,15 +36,33 @@ __device__ __forceinline__ void load8(const bf16_t *p, float (&v)[8]) {
   }
 }
 
-// 16 lanes take 128 numbers of a row, 8 each: 4 lanes a block, their four scales one dword.  Bound by memory.
-// `parts` of 128 numbers (the last one may be short) in a row.
-template <typename T> __global__ __launch_bounds__(256) void mx4_quantize_kernel(Mx4Convert a) {
+// A part is 128 numbers of a row (the last may be short), taken by 16 lanes, 8 numbers each: 4 lanes a block, their four
+// scales one dword.  WHOLE: rows are whole parts, so a part's place needs no division.  Bound by memory: 98304 rows of
+// 2048 in bf16 94 us there and 86 back (4.3 and 5.9 TB/s; the results' non-temporal stores leave the caches clean for
+// whoever comes next: 128 us there after a way back without them).  Two or four parts a lane under way: slower (98, 96
+// and 94, 99).
+template <bool WHOLE> struct Mx4Part {
+  size_t x;  // where the lane's numbers start; their codes at half of it
+  bool in;
+  __device__ __forceinline__ Mx4Part(const Mx4Convert &a, uint32_t i) {
+    const uint32_t l16 = threadIdx.x & 15;
+    if (WHOLE) {
+      in = true;
+      x = static_cast<size_t>(i) * 128 + 8 * l16;
+    } else {
+      const uint32_t row = i / a.parts, k = (i - row * a.parts) * 128 + 8 * l16;
+      in = k < static_cast<uint32_t>(a.K);
+      x = static_cast<size_t>(row) * a.K + k;
+    }
+  }
+};
+
+template <typename T, bool WHOLE> __global__ __launch_bounds__(256) void mx4_quantize_kernel(Mx4Convert a) {
   const uint32_t l16 = threadIdx.x & 15, step = gridDim.x * 16;
   for (uint32_t i = blockIdx.x * 16 + (threadIdx.x >> 4); i < a.total; i += step) {
-    const uint32_t row = i / a.parts, k = (i - row * a.parts) * 128 + 8 * l16;
-    const bool in = k < static_cast<uint32_t>(a.K);
+    const Mx4Part<WHOLE> p(a, i);
     float v[8] = {};
-    if (in) load8(static_cast<const T *>(a.x) + static_cast<size_t>(row) * a.K + k, v);
+    if (p.in) load8(static_cast<const T *>(a.x) + p.x, v);
     uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
@@ -57,31 +75,33 @@ template <typename T> __global__ __launch_bounds__(256) void mx4_quantize_kernel
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
     if (s == 255) c = 0;
-    if (in) *reinterpret_cast<uint32_t *>(a.codes + static_cast<size_t>(row) * (a.K / 2) + k / 2) = c;
+    if (p.in) *reinterpret_cast<uint32_t *>(a.codes + p.x / 2) = c;
     // lanes 0, 4, 8, 12 of the 16 hold the blocks' scales
-    uint32_t four = in ? s << (8 * (l16 >> 2)) : 0;
+    uint32_t four = p.in ? s << (8 * (l16 >> 2)) : 0;
     four |= static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(four), 0x124, 0xf, 0xf, true));  // row_ror:4
     four |= static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(four), 0x128, 0xf, 0xf, true));  // row_ror:8
     if (l16 == 0) reinterpret_cast<uint32_t *>(a.scales)[i] = four;
   }
 }
 
-template <typename T> __global__ __launch_bounds__(256) void mx4_dequantize_kernel(Mx4Convert a) {
+template <typename T, bool WHOLE> __global__ __launch_bounds__(256) void mx4_dequantize_kernel(Mx4Convert a) {
   const uint32_t l16 = threadIdx.x & 15, step = gridDim.x * 16;
   for (uint32_t i = blockIdx.x * 16 + (threadIdx.x >> 4); i < a.total; i += step) {
-    const uint32_t row = i / a.parts, k = (i - row * a.parts) * 128 + 8 * l16;
-    if (k >= static_cast<uint32_t>(a.K)) continue;
-    const uint32_t c = *reinterpret_cast<const uint32_t *>(a.codes + static_cast<size_t>(row) * (a.K / 2) + k / 2);
+    const Mx4Part<WHOLE> p(a, i);
+    if (!p.in) continue;
+    const uint32_t c = *reinterpret_cast<const uint32_t *>(a.codes + p.x / 2);
     const float scale = __uint_as_float(static_cast<uint32_t>(a.scales[static_cast<size_t>(i) * 4 + (l16 >> 2)]) << 23);
-    T *o = static_cast<T *>(const_cast<void *>(a.x)) + static_cast<size_t>(row) * a.K + k;
+    T *o = static_cast<T *>(const_cast<void *>(a.x)) + p.x;
     if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<bf16x8_t *>(o) = mx4_to_bf16(c, scale);
+      put16<WHOLE>(o, __builtin_bit_cast(uint4, mx4_to_bf16(c, scale)));
     } else {
       typedef float f32x2_v __attribute__((ext_vector_type(2)));
-      const f32x2_v p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
-      const f32x2_v r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
-      reinterpret_cast<f32x4_t *>(o)[0] = f32x4_t{p[0], p[1], q[0], q[1]};
-      reinterpret_cast<f32x4_t *>(o)[1] = f32x4_t{r[0], r[1], t[0], t[1]};
+      const f32x2_v v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0);
+      const f32x2_v v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
+      const f32x2_v v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2);
+      const f32x2_v v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
+      put16<WHOLE>(o, __builtin_bit_cast(uint4, f32x4_t{v0[0], v0[1], v1[0], v1[1]}));
+      put16<WHOLE>(o + 4, __builtin_bit_cast(uint4, f32x4_t{v2[0], v2[1], v3[0], v3[1]}));
     }
   }
 }
@@ -250,6 +270,11 @@ template <class Low, class High, int MATS> void launch_shapes(const Mx4Args &m, 
 
 unsigned convert_grid(uint32_t total) { return std::min<uint32_t>((total + 15) / 16, 16 * kCUs); }
 
+template <typename F> hipError_t launch_convert(const Mx4Convert &a, hipStream_t s, F kernel) {
+  if (a.total > 0) kernel<<<convert_grid(a.total), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 size_t mx4_part_bytes(const Mx4Args &m) {
@@ -294,21 +319,15 @@ hipError_t launch_mx4(Mx4Args m, hipStream_t s) {
 }
 
 hipError_t launch_mx4_quantize(const Mx4Convert &a, bool bf16, hipStream_t s) {
-  if (a.total == 0) return hipSuccess;
-  if (bf16)
-    mx4_quantize_kernel<bf16_t><<<convert_grid(a.total), 256, 0, s>>>(a);
-  else
-    mx4_quantize_kernel<float><<<convert_grid(a.total), 256, 0, s>>>(a);
-  return hipGetLastError();
+  if (a.K % 128 == 0)
+    return launch_convert(a, s, bf16 ? mx4_quantize_kernel<bf16_t, true> : mx4_quantize_kernel<float, true>);
+  return launch_convert(a, s, bf16 ? mx4_quantize_kernel<bf16_t, false> : mx4_quantize_kernel<float, false>);
 }
 
 hipError_t launch_mx4_dequantize(const Mx4Convert &a, bool bf16, hipStream_t s) {
-  if (a.total == 0) return hipSuccess;
-  if (bf16)
-    mx4_dequantize_kernel<bf16_t><<<convert_grid(a.total), 256, 0, s>>>(a);
-  else
-    mx4_dequantize_kernel<float><<<convert_grid(a.total), 256, 0, s>>>(a);
-  return hipGetLastError();
+  if (a.K % 128 == 0)
+    return launch_convert(a, s, bf16 ? mx4_dequantize_kernel<bf16_t, true> : mx4_dequantize_kernel<float, true>);
+  return launch_convert(a, s, bf16 ? mx4_dequantize_kernel<bf16_t, false> : mx4_dequantize_kernel<float, false>);
 }
 
 }  // namespace ace

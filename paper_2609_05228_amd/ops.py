@@ -150,8 +150,8 @@ def mx4_quantize(x):
     dev = x.device
     _sizes(K)
     _check_all(dev, dtype, [("x", x, x.shape, None)])
-    q = Mx4(torch.empty((*x.shape[:-1], K // 2), dtype=torch.uint8, device=dev),
-            torch.empty((*x.shape[:-1], _scale_bytes(K)), dtype=torch.uint8, device=dev))
+    lead = x.shape[:-1]
+    q = Mx4(x.new_empty((*lead, K // 2), dtype=torch.uint8), x.new_empty((*lead, _scale_bytes(K)), dtype=torch.uint8))
     _enqueue(dev, _lib.lib().ace_mx4_quantize, x.numel() // K, K, _DT[dtype], x.data_ptr(), q.codes.data_ptr(),
              q.scales.data_ptr())
     return q
@@ -165,7 +165,7 @@ def mx4_dequantize(q, dtype=torch.bfloat16):
     dev, shape = q.codes.device, (*q.codes.shape[:-1], K)
     _sizes(K)
     _check_all(dev, torch.uint8, _mx4_named("q", q, shape))
-    out = torch.empty(shape, dtype=dtype, device=dev)
+    out = q.codes.new_empty(shape, dtype=dtype)
     _enqueue(dev, _lib.lib().ace_mx4_dequantize, out.numel() // K, K, _DT[dtype], q.codes.data_ptr(), q.scales.data_ptr(),
              out.data_ptr())
     return out
