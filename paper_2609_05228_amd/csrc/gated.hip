@@ -202,19 +202,23 @@ using GradX64 = TileShape<4, 4, 2, 2, 4, 4>;
 using Gated64x128 = TileShape<4, 8, 2, 2, 3, 3>;  // bf16: a few rows a group
 using Gated128 = TileShape<8, 8, 2, 2, 2, 3>;     // bf16
 using GradX256 = TileShape<16, 16, 4, 2, 2, 3>;   // bf16
-using GatedF32 = TileShape<2, 4, 2, 2, 3, 3>;     // fp32
+using GatedF32 = TileShape<2, 4, 2, 2, 3, 3>;      // fp32
+using GatedF32Many = TileShape<2, 4, 2, 2, 2, 2>;  // fp32: more than a round
 
-enum class Kind { kFew, k64, k64x128, k128, kLarge, kF32 };
+enum class Kind { kFew, k64, k64x128, k128, kLarge, kF32, kF32Many };
 struct Plan {
   Kind kind;
   int splits;
 };
 
 // Kernel and parts of the reduction for S rows in N groups by `cols` columns (both projections' features, or dx's), over
-// klen, with `elems` sums in a part
+// klen, with `elems` sums in a part.  fp32: the matrix cores bound all but the smallest, so past a round of the CUs six
+// workgroups a CU with rings of two stages, else four with three (kernel times of the projections: 2069 rows in 32 groups of
+// 512 x 1024 70.7 us against 75.7, 8192 rows in 16 190 against 201, 64 rows in 8 of 512 x 256 11.5 against 10.4).
 Plan plan_rows(long long S, long long N, int cols, long long klen, size_t elems, bool bf16) {
   if (!bf16) {
     const long long items = about_tiles(S, N, GatedF32::TM) * tiles_of(cols, GatedF32::TN);
+    if (items > kCUs * GatedF32::PER_CU) return {Kind::kF32Many, 1};
     return {Kind::kF32, pick_splits(items, kCUs * GatedF32::PER_CU, tiles_of(klen, 32), elems, 0.6)};
   }
   const long long small = about_tiles(S, N, Gated64::TM) * tiles_of(cols, Gated64::TN);
@@ -309,6 +313,7 @@ hipError_t launch_gated(GatedArgs g, bool bf16, hipStream_t s) {
         gated_shapes_kernel<false><<<kCUs, 512, 0, s>>>(g);
       break;
     case Kind::kF32: launch_gated_shape<float, GatedF32>(g, s); break;
+    case Kind::kF32Many: launch_gated_shape<float, GatedF32Many>(g, s); break;
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
@@ -332,6 +337,7 @@ hipError_t launch_gated_grad_x(GatedArgs g, bool bf16, hipStream_t s) {
     case Kind::k128: launch_grad_x_shape<bf16_t, Gated128>(g, s); break;
     case Kind::kLarge: launch_grad_x_shape<bf16_t, GradX256>(g, s); break;
     case Kind::kF32: launch_grad_x_shape<float, GatedF32>(g, s); break;
+    case Kind::kF32Many: launch_grad_x_shape<float, GatedF32Many>(g, s); break;
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
