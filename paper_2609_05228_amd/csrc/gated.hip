@@ -211,6 +211,11 @@ struct Plan {
   int splits;
 };
 
+// bf16: 64 x 64 tiles while they are at most a round, 64 x 128 up to 32 rows a group, then 128 x 128, and the large shapes
+// past 40 rows a group where they fill most CUs (projections of 128 groups of 768 x 2048, kernel times with 32, 48, 96
+// and 128 rows: 64 x 128 131, 142, 204, 233 us; 128 x 128 132, 135, 147, 205; large 129, 131, 134, 140; one group of 2048 x
+// 2048 with 2048 rows, 128 large tiles: 128 x 128 44, large 51; 16 groups of 1024 x 1024 with 4096, about 192: 41.5 and
+// 32.8).
 // Kernel and parts of the reduction for S rows in N groups by `cols` columns (both projections' features, or dx's), over
 // klen, with `elems` sums in a part.  fp32: the matrix cores bound all but the smallest, so past a round of the CUs six
 // workgroups a CU with rings of two stages, else four with three (kernel times of the projections: 2069 rows in 32 groups of
@@ -225,8 +230,7 @@ Plan plan_rows(long long S, long long N, int cols, long long klen, size_t elems,
   if (small <= kCUs * Gated64::PER_CU)
     return {Kind::k64, pick_splits(small, kCUs * Gated64::PER_CU, tiles_of(klen, 64), elems, 0.45)};
   if (S <= 32 * N) return {Kind::k64x128, 1};
-  const long long items = about_tiles(S, N, Gated128::TM) * tiles_of(cols, Gated128::TN);
-  const bool large = S > 80 * N && items >= kCUs * Gated128::PER_CU;
+  const bool large = S > 40 * N && about_tiles(S, N, 256) * tiles_of(cols, 256) >= kCUs * 5 / 8;
   return {large ? Kind::kLarge : Kind::k128, 1};
 }
 Plan plan_gated(const GatedArgs &g, bool bf16) {
