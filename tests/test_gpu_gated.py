@@ -25,8 +25,14 @@ SHAPES = [
     ([5] * 70 + [0] * 60 + [2] * 5, 0, 3, 48, 88),
     ([700, 0, 1, 90], 0, 0, 32, 1032),
     ([2, 0, 1], 0, 0, 1032, 2056),
-    ([100] * 9 + [220] * 5, 0, 0, 1096, 72),  # enough tiles for the largest shape
+    ([100] * 9 + [220] * 5, 0, 0, 1096, 72),
     ([37] * 40, 0, 0, 456, 40),
+    ([40], 0, 2, 72, 4104),  # the reduction in parts
+    # the large shapes by their heights, whole lines and not; of the rows' gradient
+    ([150] * 14, 0, 3, 2056, 72),
+    ([150] * 12 + [200, 256], 1, 0, 2048, 72),
+    ([310] * 9 + [17], 0, 2, 2056, 40),
+    ([130] * 20, 2, 0, 40, 2056),
 ]
 
 
@@ -104,6 +110,26 @@ def test_gradient(shape, kept, dtype, act):
     for n in ("w_gate", "w_up"):
         ref.within(got[n], want[n], err[n], DT[dtype], n)
     assert torch.equal(got["x"], only["x"])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("shape", [([3, 0, 40], 1, 2, 12, 20), ([33], 0, 0, 4, 4), ([7] * 30, 0, 1, 68, 132)],
+                         ids=lambda s: f"{len(s[0])}g_{s[3]}x{s[4]}")
+def test_fp32_in_fours(shape, act):
+    """fp32 features come in multiples of four."""
+    x, wg, wu, da, offs = make(*shape, "f32")
+    gap = rest(offs, x.shape[0])
+    d = [t.to(DEV) for t in (x, wg, wu, offs)]
+    a, kept = ace.grouped_gated(*d, activation=act, keep=True)
+    want, err = ref.gated(x, wg, wu, offs, act)
+    for n, t in (("a", a), ("g", kept[0]), ("u", kept[1])):
+        ref.within(t[~gap], want[n][~gap], err[n][~gap], torch.float32, n)
+    for k in (None, kept):
+        got = ace.grouped_gated_grad(da.to(DEV), *d, kept=k, activation=act)
+        want, err = ref.gated_grad(da, x, wg, wu, offs, act, None if k is None else tuple(v.cpu() for v in k))
+        ref.within(got["x"][~gap], want["x"][~gap], err["x"][~gap], torch.float32, "x")
+        for n in ("w_gate", "w_up"):
+            ref.within(got[n], want[n], err[n], torch.float32, n)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -111,6 +111,11 @@ SHAPES = [
     ([100] * 9 + [220] * 5, 0, 0, 1096, 96),
     ([60] * 20, 0, 0, 584, 288),
     ([37] * 40, 0, 0, 456, 64),
+    ([300], 0, 3, 520, 2080),  # the reduction in parts
+    # the large shapes, whole lines and not, and rows in 4 bits by both heights
+    ([150] * 14, 0, 3, 2056, 160),
+    ([150] * 12 + [200, 256], 1, 0, 2048, 544),
+    ([300] * 15 + [17], 0, 2, 2056, 96),
 ]
 
 
@@ -245,6 +250,19 @@ def test_bad_offsets_stay_inside(offs, rows):
     ace.grouped_gated(rows_of(x), *w, o, out=out)
     torch.cuda.synchronize()
     assert bool((buf[:pad] == 5).all()) and bool((buf[-pad:] == 5).all())
+
+
+@pytest.mark.parametrize("rows", ["bf16", "mx4"])
+def test_offsets_that_go_back_and_forth(rows):
+    """2048 groups that each claim the whole array or nothing: no more work than the array is worth."""
+    S, n, M, K = 3000, 2048, 24, 64
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn((S, K), generator=gen, device=DEV).bfloat16()
+    w = ace.mx4_quantize(torch.randn((n, M, K), generator=gen, device=DEV).bfloat16())
+    r = ace.mx4_quantize(x) if rows == "mx4" else x
+    o = torch.tensor([0, S] * (n // 2) + [0], dtype=torch.int32, device=DEV)
+    assert ace.grouped_matmul(r, w, o).shape == ace.grouped_gated(r, w, w, o).shape == (S, M)
+    torch.cuda.synchronize()
 
 
 @pytest.mark.parametrize("rows", ["bf16", "mx4"])
