@@ -173,7 +173,7 @@ __device__ __forceinline__ void mx4_rows(const Mx4Args &m, uint8_t *smem) {
 // Few rows: tiles of 16, the reduction over the workgroup's four waves
 constexpr int kSplitWaves = 4;
 template <bool ROWS4, bool LINES, int MATS> __global__ __launch_bounds__(64 * kSplitWaves) void mx4_few_kernel(Mx4Args m) {
-  using S = Mx4Tile<ROWS4, 128, 1, 4, 1, 1, 3, 3, MATS>;
+  using S = Mx4Tile<ROWS4, 1, 4, 1, 1, 3, 3, MATS>;
   __shared__ __align__(16) uint8_t smem[kSplitWaves * S::LDS + JoinStore<S, kSplitWaves, int>::LDS];
   mx4_rows<S, LINES, MATS, kSplitWaves>(m, smem);
 }
@@ -196,9 +196,9 @@ __global__ __launch_bounds__(512) void mx4_shapes_kernel(Mx4Args m) {
   int tiles[2];
   RaggedTiles::count(g.offsets, g.N, g.S, heights, tiles, g.fill);
   const int slots = static_cast<int>(gridDim.x);
-  auto cost = [&](int h, int width, int k128) {
+  auto cost = [&](int h, int width, int stage) {
     const long long items = static_cast<long long>(tiles[h]) * ((MATS * g.M + width - 1) / width);
-    return (items + slots - 1) / slots * k128;
+    return (items + slots - 1) / slots * stage;
   };
   if (cost(0, Low::TN, Low::COST) <= cost(1, High::TN, High::COST))
     mx4_rows<SL, LINES, MATS>(m, smem);
@@ -206,22 +206,22 @@ __global__ __launch_bounds__(512) void mx4_shapes_kernel(Mx4Args m) {
     mx4_rows<SH, LINES, MATS>(m, smem);
 }
 
-// COST: time of 128 k of a tile with every CU busy, in units of 50 ns
-template <bool ROWS4, int BK, int MB, int NB, int WR, int WC, int DA, int DB, int COST_ = 0> struct Mx4Shape {
-  template <int MATS> using Tile = Mx4Tile<ROWS4, BK, MB, NB, WR, WC, DA, DB, MATS>;
+// COST: time of a stage of a tile with every CU busy, in units of 50 ns
+template <bool ROWS4, int MB, int NB, int WR, int WC, int DA, int DB, int COST_ = 0> struct Mx4Shape {
+  template <int MATS> using Tile = Mx4Tile<ROWS4, MB, NB, WR, WC, DA, DB, MATS>;
   static constexpr int TM = 16 * MB, TN = 16 * NB, THREADS = WR * WC * 64, COST = COST_;
   static constexpr int PER_CU = 160 * 1024 / Tile<1>::LDS;
   static_assert(PER_CU >= 1, "fits a CU");
 };
 // bf16 rows
-using Wide16 = Mx4Shape<false, 128, 1, 16, 1, 4, 3, 3>;
-using Wide64 = Mx4Shape<false, 128, 4, 8, 2, 2, 3, 3>;
-using Wide192 = Mx4Shape<false, 128, 12, 16, 2, 4, 2, 2>;
+using Wide16 = Mx4Shape<false, 1, 16, 1, 4, 3, 3>;
+using Wide64 = Mx4Shape<false, 4, 8, 2, 2, 3, 3>;
+using Wide192 = Mx4Shape<false, 12, 16, 2, 4, 2, 2>;
 // rows in 4 bits
-using Four16 = Mx4Shape<true, 128, 1, 16, 1, 4, 3, 3>;
-using Four64 = Mx4Shape<true, 128, 4, 8, 2, 2, 4, 4>;
-using Four256 = Mx4Shape<true, 128, 16, 16, 4, 2, 3, 3, 30>;
-using Four320 = Mx4Shape<true, 128, 20, 12, 4, 2, 3, 3, 38>;
+using Four16 = Mx4Shape<true, 1, 16, 1, 4, 3, 3>;
+using Four64 = Mx4Shape<true, 4, 8, 2, 2, 4, 4>;
+using Four256 = Mx4Shape<true, 16, 16, 4, 2, 3, 3, 30>;
+using Four320 = Mx4Shape<true, 20, 12, 4, 2, 3, 3, 38>;
 
 enum class Kind { kFew, k16, k64, kLarge };
 struct Plan {
