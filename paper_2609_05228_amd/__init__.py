@@ -12,7 +12,9 @@ ratios (App. C.1); and `build_tables` computes the offline GSP / RCR tables
 
 Around the layer, for the decoder that contains it and for fine-tuning it:
 `grouped_matmul` (matrix products grouped by expert with ragged sizes) with its
-gradients, `block_norm` (the norms before and after a block with its gate and
+gradients, `grouped_gated` (the experts' gated feed-forward block) with its gradient,
+weights in microscaled 4-bit floating point for both (`Mx4`, `mx4_quantize`,
+`mx4_dequantize`; forward only), `block_norm` (the norms before and after a block with its gate and
 residual scale) with its gradient, and, for serving only, `adapter_add` (low-rank
 adapters of many requests beside a shared projection).
 """

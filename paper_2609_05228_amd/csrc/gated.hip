@@ -14,6 +14,10 @@
 // product with a reduction of two segments (dg with w_gate, then du with w_up), summed in the same
 // accumulators and rounded once; both gradients of the weights are one launch, where the tiles of a group
 // share its rows of x in an XCD's L2.
+//
+// What bounds it, on 128 groups of 768 x 2048 in bf16: the weights' way from and to memory.  The projections of 8 rows take
+// 13.6 us (3.6 TB/s of what the call needs), of 32768 with g and u kept 252 us (4.3 TB/s at 0.82 PFLOP/s); the
+// gradient of 16384 from kept projections 430 us (4.2 TB/s: 24 dg and du, 170 dx, 210 to 240 the weights').
 #include "gated_tile.h"
 
 namespace ace {
@@ -104,7 +108,8 @@ template <bool LINES> __global__ __launch_bounds__(512) void gated_shapes_kernel
     gated_rows<bf16_t, LINES, 20, 16, 4, 2, 2, 2>(g, RaggedTiles(g.offsets, g.N, g.S, 320, g.fill), smem);
 }
 
-// What the epilogue does, from the fp32 parts of g and u (summed in order) or the kept g and u: 4 features a thread.
+// What the epilogue does, from the fp32 parts of g and u (summed in order) or the kept g and u: 4 features a thread.  Bound
+// by memory: dg and du of 16384 rows of 768 in bf16 24 us, 5.2 TB/s.
 // Rows of no group: zeros into a, g and u with `fill`, else they stay (dg and du of them are never read).
 template <typename T, int ACT> __global__ __launch_bounds__(256) void gated_join_kernel(GatedArgs g) {
   const size_t total = static_cast<size_t>(g.S) * g.M;

@@ -57,8 +57,9 @@ __global__ __launch_bounds__(WR *WC * 64) void grouped_rows_kernel(GroupedArgs g
 
 // The same with the tile shape taken here, from the groups' sizes that only the device knows: a
 // group's last row tile costs about a full one, so which height wastes least goes by them.
-// Rounds of a CU times the time of a stage, in units of 50 ns as measured with every CU busy.  Four tile bodies
-// in one kernel spill 43 vector registers in the rows' gradient.
+// Rounds of a CU times the time of a stage, in units of 50 ns as measured with every CU busy (all of them some 6% less
+// since the second wave of a SIMD copies between its products).  Four tile bodies
+// in one kernel spill 39 vector registers in the rows' gradient and 2 in the forward.
 template <bool GX, bool LINES> __global__ __launch_bounds__(512) void grouped_shapes_kernel(GroupedArgs g) {
   __shared__ __align__(16) uint8_t smem[160 * 1024];
   const int cols = GX ? g.K : g.M;
@@ -228,8 +229,8 @@ struct Plan {
 
 // Which kernel for the forward and the rows' gradient.  us on 128 groups of 768 x 2048 (forward):
 //   rows a group               2    16    48    96   128   256  1024
-//   128 x 128 (two a CU)      66    68    73    81   119   173   543
-//   large (best of its four)  64    71    74    82    94   140   478
+//   128 x 128 (two a CU)      67    74    77    86   117   169   531
+//   large (best of its four)  65    76    79    86    92   127   407
 // and 16 groups of 1024 x 1024 with 1, 16, 128 and 512 rows: 64 x 64 12.8, 14.2, -, -; 128 x 128 15.2, 16.4, 20, 25;
 // large 17, 18, 23, 31.  Few rows a group, where its weights' way from memory bounds all of them: 64 x 128 tiles with
 // deeper rings, 128 groups of 2048 x 768 with 2, 16, 32 rows 63, 70, 72.6 against 68, 71, 73.7 with 128 x 128;
@@ -252,7 +253,7 @@ Plan plan_rows(const GroupedArgs &g, bool grad, bool bf16) {
   return {large ? Kind::kLarge : Kind::k128, 1, elems};
 }
 
-// ... and for the weights' gradient.  128 groups of 768 x 2048 and 128 rows: 256 x 256 tiles 114 us, 128 x 128 134
+// ... and for the weights' gradient.  128 groups of 768 x 2048 and 128 rows: 256 x 256 tiles 105 us, 128 x 128 134
 // (the former spill 12 registers and wait for each tile's stores).
 // A group of more than p.chunk rows is summed in parts of at most that many, which a second launch adds: a few
 // long groups would otherwise be a few workgroups' work.  Parts are four times the mean group (2048 rows at least),

@@ -213,6 +213,14 @@ template <bool ROWS4, int MB, int NB, int WR, int WC, int DA, int DB, int COST_ 
   static constexpr int PER_CU = 160 * 1024 / Tile<1>::LDS;
   static_assert(PER_CU >= 1, "fits a CU");
 };
+// What they reach, on 128 groups of 768 x 2048 unless said otherwise (kernel times).  The small ones are bound by the
+// weights' way from memory: 256 rows through gate and up 44 us, 4.2 TB/s of the 187 MB that the call needs (two workgroups a
+// CU with rings of three; one with four 53, with six 56).  The large ones by the matrix cores and what a stage costs beside them:
+//   bf16 rows   32768: 192 x 256 117 us (0.88 PFLOP/s; others: 160 x 256 121, 128 x 256 141, 320 x 192 by 64 k 145, 256 x 256
+//               by 64 k 187); 8192 in one group of 4096 x 4096 233 (1.18 PFLOP/s; 160 x 256 261)
+//   4-bit rows  32768: 320 x 192 66 us (1.57 PFLOP/s), 256 x 256 90; 8192 in one group of 4096 x 4096 140 and 99 (2.8)
+// Codes become bf16 two at a time by an instruction of 4 cycles, in every wave that needs the column: waves as 2 x 4 turn
+// each of them twice, as 4 x 2 four times.
 // bf16 rows
 using Wide16 = Mx4Shape<false, 1, 16, 1, 4, 3, 3>;
 using Wide64 = Mx4Shape<false, 4, 8, 2, 2, 3, 3>;
@@ -237,10 +245,7 @@ Plan plan_mx4(const Mx4Args &m) {
   const GatedArgs &g = m.g;
   const int mats = m.gated ? 2 : 1, cols = mats * g.M;
   if (g.S <= 64ll * g.N && about_tiles(g.S, g.N, 16) * tiles_of(cols, 64) <= 4 * kCUs) return {Kind::kFew, 1};
-  if (g.S <= 16ll * g.N || g.S <= 16) {
-    const long long items = about_tiles(g.S, g.N, 16) * tiles_of(cols, Wide16::TN);
-    return {Kind::k16, pick_splits(items, kCUs * Wide16::PER_CU, tiles_of(g.K, 128), static_cast<size_t>(g.S) * cols, 0.6)};
-  }
+  if (g.S <= 16ll * g.N) return {Kind::k16, 1};
   const long long items = about_tiles(g.S, g.N, 64) * tiles_of(cols, Wide64::TN);
   if (items <= 2 * kCUs)
     return {Kind::k64, pick_splits(items, kCUs * Wide64::PER_CU, tiles_of(g.K, 128), static_cast<size_t>(g.S) * cols, 0.8)};
