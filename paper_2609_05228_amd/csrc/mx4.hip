@@ -276,7 +276,8 @@ template <class Low, class High, int MATS> void launch_shapes(const Mx4Args &m, 
 unsigned convert_grid(uint32_t total) { return std::min<uint32_t>((total + 15) / 16, 16 * kCUs); }
 
 template <typename F> hipError_t launch_convert(const Mx4Convert &a, hipStream_t s, F kernel) {
-  if (a.total > 0) kernel<<<convert_grid(a.total), 256, 0, s>>>(a);
+  if (a.total == 0) return hipSuccess;
+  kernel<<<convert_grid(a.total), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
