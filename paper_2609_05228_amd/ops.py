@@ -127,17 +127,29 @@ def _scale_bytes(K):
 
 def _mx4_of(name, q, dims):
     """K of an Mx4 with `dims` dimensions (None: any)."""
-    _need(isinstance(q, Mx4), f"{name} must be an Mx4")
-    _need(isinstance(q.codes, torch.Tensor) and isinstance(q.scales, torch.Tensor)
-          and q.codes.dim() >= 1 and (dims is None or q.codes.dim() == dims),
-          f"{name} must hold tensors" + ("" if dims is None else f" of {dims} dimensions"))
-    return 2 * q.codes.shape[-1]
+    if not isinstance(q, Mx4):
+        raise ValueError(f"{name} must be an Mx4")
+    codes = q.codes
+    if not (isinstance(codes, torch.Tensor) and isinstance(q.scales, torch.Tensor)):
+        raise ValueError(f"{name} must hold tensors")
+    if codes.dim() != dims if dims is not None else codes.dim() < 1:
+        raise ValueError(f"{name} must hold tensors of {'1 dimension or more' if dims is None else f'{dims} dimensions'}")
+    return 2 * codes.shape[-1]
 
 
-def _mx4_named(name, q, shape):
-    """What `_check_all` has to find for an Mx4 of numbers of that shape."""
-    return [(f"{name}.codes", q.codes, (*shape[:-1], shape[-1] // 2), torch.uint8),
-            (f"{name}.scales", q.scales, (*shape[:-1], _scale_bytes(shape[-1])), torch.uint8)]
+# names of the tensors of an Mx4 argument, for `_check_all`
+_PARTS = {n: (n + ".codes", n + ".scales") for n in ("x", "q", "w", "w_gate", "w_up")}
+
+
+def _mx4_named(name, q, lead, K):
+    """What `_check_all` has to find for an Mx4 of numbers [*lead, K]."""
+    codes, scales = _PARTS[name]
+    return ((codes, q.codes, (*lead, K // 2), torch.uint8), (scales, q.scales, (*lead, _scale_bytes(K)), torch.uint8))
+
+
+def _whole_blocks(K):
+    if K <= 0 or K % _BLOCK != 0:
+        raise ValueError(f"the last dimension, {K}, is not a multiple of {_BLOCK}")
 
 
 def mx4_quantize(x):
@@ -146,7 +158,7 @@ def mx4_quantize(x):
     to the even code, above 6 to 6).  A block that holds a NaN or an infinity stands for NaN.  Returns an `Mx4`."""
     _need(isinstance(x, torch.Tensor) and x.dim() >= 1, "x must be a tensor of 1 dimension or more")
     dtype, K = _dtype_of("x", x, x.dim()), x.shape[-1]
-    _need(K > 0 and K % _BLOCK == 0, f"the last dimension, {K}, is not a multiple of {_BLOCK}")
+    _whole_blocks(K)
     dev = x.device
     _sizes(K)
     _check_all(dev, dtype, [("x", x, x.shape, None)])
@@ -160,12 +172,13 @@ def mx4_quantize(x):
 def mx4_dequantize(q, dtype=torch.bfloat16):
     """The numbers [..., K] that an `Mx4` stands for, exactly, as bf16 or fp32."""
     K = _mx4_of("q", q, None)
-    _need(dtype in _DT, f"unsupported dtype {dtype}")
-    _need(K > 0 and K % _BLOCK == 0, f"the last dimension, {K}, is not a multiple of {_BLOCK}")
-    dev, shape = q.codes.device, (*q.codes.shape[:-1], K)
+    if dtype not in _DT:
+        raise ValueError(f"unsupported dtype {dtype}")
+    _whole_blocks(K)
+    dev, lead = q.codes.device, q.codes.shape[:-1]
     _sizes(K)
-    _check_all(dev, torch.uint8, _mx4_named("q", q, shape))
-    out = q.codes.new_empty(shape, dtype=dtype)
+    _check_all(dev, torch.uint8, _mx4_named("q", q, lead, K))
+    out = q.codes.new_empty((*lead, K), dtype=dtype)
     _enqueue(dev, _lib.lib().ace_mx4_dequantize, out.numel() // K, K, _DT[dtype], q.codes.data_ptr(), q.scales.data_ptr(),
              out.data_ptr())
     return out
@@ -177,17 +190,20 @@ def _mx4_call(x, weights, offsets, out, act, names):
     N, M = weights[0].codes.shape[:2]
     if isinstance(x, Mx4):
         _mx4_of("x", x, 2)
-        S, lead = x.codes.shape[0], x.codes
-        named = _mx4_named("x", x, (S, K))
+        lead, scales = x
+        S = lead.shape[0]
+        named = [*_mx4_named("x", x, (S,), K)]
     else:
-        _need(_dtype_of("x", x, 2) is torch.bfloat16, "x: bf16 or Mx4 with weights in 4 bits")
-        S, lead = x.shape[0], x
+        if _dtype_of("x", x, 2) is not torch.bfloat16:
+            raise ValueError("x: bf16 or Mx4 with weights in 4 bits")
+        S, lead, scales = x.shape[0], x, None
         named = [("x", x, (S, K), torch.bfloat16)]
-    _need(K % _BLOCK == 0, f"K = {K} is not a multiple of {_BLOCK}")
+    _whole_blocks(K)
     size = _sizes(S, N, M, K)
     for name, w in zip(names, weights):
-        _mx4_of(name, w, 3)
-        named += _mx4_named(name, w, (N, M, K))
+        if w is not weights[0]:
+            _mx4_of(name, w, 3)
+        named += _mx4_named(name, w, (N, M), K)
     named.append(("offsets", offsets, (N + 1,), torch.int32))
     flags = 0
     if out is not None:
@@ -202,9 +218,8 @@ def _mx4_call(x, weights, offsets, out, act, names):
     gated = len(weights) == 2
     n = lib.ace_grouped_mx4_workspace_size(desc, gated)
     ws = _scratch(n, dev)
-    xs = x.scales.data_ptr() if isinstance(x, Mx4) else None
     w = [_lib.Mx4Ptr(q.codes.data_ptr(), q.scales.data_ptr()) for q in weights]
-    _enqueue(dev, lib.ace_grouped_gated_mx4 if gated else lib.ace_grouped_matmul_mx4, desc, lead.data_ptr(), xs, *w,
+    _enqueue(dev, lib.ace_grouped_gated_mx4 if gated else lib.ace_grouped_matmul_mx4, desc, lead.data_ptr(), _ptr(scales), *w,
              offsets.data_ptr(), out.data_ptr(), _ptr(ws), n)
     return out
 
