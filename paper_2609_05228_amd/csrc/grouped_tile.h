@@ -596,7 +596,7 @@ struct Share {
 struct Part {
   int k0, len;
 };
-template <int BK> __device__ __forceinline__ Part part_of(int klen, int s, int splits) {
+template <int BK> __host__ __device__ __forceinline__ Part part_of(int klen, int s, int splits) {
   if (splits == 1) return {0, klen};
   const int nk = (klen + BK - 1) / BK, each = nk / splits, more = nk % splits;
   const int b = s * each + min(s, more), n = each + (s < more);

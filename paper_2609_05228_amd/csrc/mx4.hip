@@ -125,17 +125,19 @@ __device__ __forceinline__ void mx4_rows(const Mx4Args &m, uint8_t *smem) {
     const Part k = KS > 1 ? part_of<128>(klen, wave, KS) : part_of<128>(klen, it.split, g.splits);
     GatedRef<S> t;
     if constexpr (ROWS4) {
-      t.a.codes[0] = static_cast<const uint8_t *>(g.x) + static_cast<size_t>(it.row0) * code_row + k.k0 / 2;
-      t.a.scales[0] = m.x_scales + static_cast<size_t>(it.row0) * scale_row + k.k0 / kMx4Block;
+      t.a.codes[0] = static_cast<const uint8_t *>(g.x) + static_cast<size_t>(it.row0) * code_row;
+      t.a.scales[0] = m.x_scales + static_cast<size_t>(it.row0) * scale_row;
+      t.a.k0 = k.k0;
     } else {
       t.a.p[0] = static_cast<const bf16_t *>(g.x) + static_cast<size_t>(it.row0) * g.K + k.k0;
     }
     const size_t row = static_cast<size_t>(max(it.group, 0)) * g.M + f0;
-    t.b.codes[0] = static_cast<const uint8_t *>(g.w_gate) + row * code_row + k.k0 / 2;
-    t.b.scales[0] = m.gate_scales + row * scale_row + k.k0 / kMx4Block;
+    t.b.codes[0] = static_cast<const uint8_t *>(g.w_gate) + row * code_row;
+    t.b.scales[0] = m.gate_scales + row * scale_row;
+    t.b.k0 = k.k0;
     if constexpr (MATS == 2) {
-      t.b.codes[1] = static_cast<const uint8_t *>(g.w_up) + row * code_row + k.k0 / 2;
-      t.b.scales[1] = m.up_scales + row * scale_row + k.k0 / kMx4Block;
+      t.b.codes[1] = static_cast<const uint8_t *>(g.w_up) + row * code_row;
+      t.b.scales[1] = m.up_scales + row * scale_row;
     }
     t.at = static_cast<size_t>(it.row0) * g.M + f0;
     t.out = static_cast<bf16_t *>(g.a) + t.at;

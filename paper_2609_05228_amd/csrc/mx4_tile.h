@@ -29,15 +29,18 @@ constexpr int kMx4Panel = 512;  // of a panel of scales
 
 __host__ __device__ constexpr uint32_t mx4_scale_row(int K) { return static_cast<uint32_t>((K + 127) / 128) * 4u; }
 
+// Where an operand lies: its first rows from their first k, of which the reduction starts at k0
 template <int MATS> struct Mx4Mats {
   const uint8_t *codes[MATS], *scales[MATS];
+  int k0;  // whole stages
 };
 
 // BLK 16-row blocks in 4 bits.  With two matrices block b is block b / 2 of matrix b % 2; in LDS all of the first one's come
 // first.  A unit is a block, 1 KB: copy lane i brings a 16-byte chunk of row i / 4 to byte 16 i, chunk c of row r in slot
 // c ^ (r / 2 % 4), which reads at the full rate (twice that of r / 4).  Waves that have no unit left copy zeros into a
 // place behind the rest, so that every wave waits for equal counts.  A panel is 64 rows a copy, 16 bytes a lane (its rows
-// are padded to 4 bytes only, so the addresses are multiples of 4).
+// are padded to 4 bytes only, so the addresses are multiples of 4).  Where less than that is left of a row a copy brings the
+// start of the next one, so the descriptors end with the last row, which k0 brings nearer to where they start.
 template <int BLK, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
   using Src = Mx4Mats<MATS>;
   static constexpr int BK = kMx4Stage;
@@ -55,15 +58,16 @@ template <int BLK, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
   int klen, chunk_k;
   uint32_t voff[NU], poff[NP];
 
-  __device__ __forceinline__ void init(const Src &src, int ld, int valid, int k, int wave, int lane) {
+  __host__ __device__ __forceinline__ void init(const Src &src, int ld, int valid, int k, int wave, int lane) {
     klen = k;
     code_row = static_cast<uint32_t>(ld) / 2;
     scale_row = mx4_scale_row(ld);
-    code_span = static_cast<uint32_t>(valid) * code_row;
-    scale_span = static_cast<uint32_t>(valid) * scale_row;
+    const uint32_t codes0 = static_cast<uint32_t>(src.k0) / 2, scales0 = static_cast<uint32_t>(src.k0) / kMx4Block;
+    code_span = static_cast<uint32_t>(valid) * code_row - codes0;
+    scale_span = static_cast<uint32_t>(valid) * scale_row - scales0;
     // offsets, not choices between pointers: those would be indexes into the arrays at run time and put them in memory
-    codes = src.codes[0];
-    codes2 = src.codes[MATS - 1];  // a lone wave's second half of units
+    codes = src.codes[0] + codes0;
+    codes2 = src.codes[MATS - 1] + codes0;  // a lone wave's second half of units
     if (MATS == 2 && W > 1) codes += (src.codes[MATS - 1] - src.codes[0]) * (wave * NU >= UNITS / MATS);
     const int r = lane >> 2, chunk = (lane & 3) ^ swap(r);
     chunk_k = kMx4Block * chunk;
@@ -76,23 +80,27 @@ template <int BLK, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
     for (int t = 0; t < NP; ++t) {
       const int i = wave * NP + t, p = i % GROUPS * 64 + lane;
       poff[t] = p < ROWS ? static_cast<uint32_t>(block_row<PAIR>(p >> 4, p & 15)) * scale_row : kOutside;
-      scales[t] = src.scales[0];
+      scales[t] = src.scales[0] + scales0;
       if (MATS == 2) scales[t] += (src.scales[MATS - 1] - src.scales[0]) * (i >= GROUPS);
     }
   }
-  static __device__ __forceinline__ int swap(int r) { return (r >> 1) & 3; }
+  static __host__ __device__ __forceinline__ int swap(int r) { return (r >> 1) & 3; }
+  // of a stage: bytes that its codes, and the panel that holds its scales, lie behind the part's first ones
+  static __host__ __device__ __forceinline__ uint32_t codes_at(int s) { return static_cast<uint32_t>(s) * (BK / 2); }
+  static __host__ __device__ __forceinline__ uint32_t panel_at(int s) { return static_cast<uint32_t>(s / PANEL_STAGES) * 16u; }
+  __host__ __device__ __forceinline__ bool in_stage(int s) const { return chunk_k < klen - s * BK; }
 
   // the copies of stage s, which is within k, and of its panel where there is a place for it
   __device__ __forceinline__ void issue(int s, uint32_t lds, uint32_t panel, int wave, bool) const {
     if (panel) {
-      const uint32_t at = static_cast<uint32_t>(s / PANEL_STAGES) * 16u;
+      const uint32_t at = panel_at(s);
 #pragma unroll
       for (int t = 0; t < NP; ++t)
         if (wave * NP + t < MATS * GROUPS)
           dma16_buf(make_rsrc(scales[t] + at, scale_span - at), poff[t], panel + (wave * NP + t) * kUnitBytes);
     }
-    const bool in = chunk_k < klen - s * BK;
-    const uint32_t at = static_cast<uint32_t>(s) * (BK / 2);
+    const bool in = in_stage(s);
+    const uint32_t at = codes_at(s);
     const i32x4_rsrc first = make_rsrc(codes + at, code_span - at);
     const i32x4_rsrc second = MATS == 2 && W == 1 ? make_rsrc(codes2 + at, code_span - at) : first;
 #pragma unroll
@@ -105,14 +113,14 @@ template <int BLK, bool PAIR, int W, int MATS = 1> struct Mx4Operand {
   }
 
   // the lane's codes: k 32 g .. 32 g + 31 of row r of block blk, (r, g) = (lane % 16, lane / 16)
-  static __device__ __forceinline__ i32x4_t read(const uint8_t *s, int blk, int lane) {
+  static __host__ __device__ __forceinline__ i32x4_t read(const uint8_t *s, int blk, int lane) {
     const int r = lane & 15, g = lane >> 4;
     return *reinterpret_cast<const i32x4_t *>(s + (blk % MATS * (BLK / MATS) + blk / MATS) * kUnitBytes + r * 64 +
                                               ((g ^ swap(r)) << 4));
   }
   // their scale, for the stage from k on of klen: one that is not of a block within klen (whose codes are zeros) may
   // be anything, and is 0 here
-  static __device__ __forceinline__ int read_scale(const uint8_t *panel, int blk, int lane, int k, int klen) {
+  static __host__ __device__ __forceinline__ int read_scale(const uint8_t *panel, int blk, int lane, int k, int klen) {
     const int b = lane >> 4;  // of the stage's blocks
     const int row = blk % MATS * (GROUPS * 64) + blk / MATS * 16 + (lane & 15);
     const int v = panel[row * 16 + (k % kMx4Panel / kMx4Block + b)];
