@@ -5,31 +5,35 @@
 
 namespace ace {
 
-// exp(-z^2 / 2) for 0 <= z <= 20 to about 2^-23: the hardware base-2 exponential, with what z^2 and its
-// product with log2(e) / 2 lose to rounding put back to first order
-__device__ __forceinline__ float half_square_exp(float z) {
-  constexpr float c = 0.72134752f, c_rest = 8.3e-9f;  // log2(e) / 2 = c + c_rest
+// z^2 / 2 log2(e) = -(e + rest) for 0 <= z <= 20 to 4e-12: what z^2 and its product with log2(e) / 2 lose to rounding, in rest
+struct HalfSquare {
+  float e, rest;
+};
+__host__ __device__ __forceinline__ HalfSquare half_square(float z) {
+  constexpr float c = 0.72134752f, c_rest = 9.6298150e-9f;  // log2(e) / 2 = c + c_rest
   const float h = z * z, l = fmaf(z, z, -h), e = -c * h;
-  const float rest = -fmaf(c, h, e) - c * l - c_rest * h;
-  return __builtin_amdgcn_exp2f(e) * fmaf(rest, 0.69314718f, 1.f);
+  return {e, -fmaf(c, h, e) - c * l - c_rest * h};
+}
+
+// exp(-z^2 / 2) for 0 <= z <= 20, to the roundings of the hardware base-2 exponential and of two operations; where it
+// is below the least normal number (z > 13.2) it may be 0
+__device__ __forceinline__ float half_square_exp(float z) {
+  const HalfSquare v = half_square(z);
+  return __builtin_amdgcn_exp2f(v.e) * fmaf(v.rest, 0.69314718f, 1.f);
 }
 
 // Phi(-z) e^(z^2 / 2) for z >= 0, which falls smoothly from 1/2 as 1 / (sqrt(2 pi) z): t P(t) with t = 1 / (1 + 0.32 z)
-// and P a polynomial fitted to the least relative error (3.3e-8 over all z >= 0; 3e-7 with fp32 arithmetic)
-__device__ __forceinline__ float normal_tail(float z) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.32f, z, 1.f));
-  float p = -0.0210784f;
-  p = fmaf(p, t, 0.095408306f);
-  p = fmaf(p, t, -0.14670941f);
-  p = fmaf(p, t, 0.06532997f);
-  p = fmaf(p, t, -0.009378675f);
-  p = fmaf(p, t, 0.058654312f);
-  p = fmaf(p, t, 0.087829046f);
-  p = fmaf(p, t, 0.11462236f);
-  p = fmaf(p, t, 0.12766095f);
-  p = fmaf(p, t, 0.12766153f);
+// and P a polynomial fitted to the least relative error (4.5e-8 over all z >= 0 with the coefficients as they are; 3.3e-7
+// with fp32 arithmetic)
+constexpr float kTail[10] = {-0.0210784f, 0.095408306f, -0.14670941f, 0.06532997f, -0.009378675f,
+                             0.058654312f, 0.087829046f, 0.11462236f, 0.12766095f, 0.12766153f};
+template <typename R> __host__ __device__ __forceinline__ R tail_of(R t) {
+  R p = kTail[0];
+#pragma unroll
+  for (int i = 1; i < 10; ++i) p = fma(p, t, static_cast<R>(kTail[i]));
   return p * t;
 }
+__device__ __forceinline__ float normal_tail(float z) { return tail_of(__builtin_amdgcn_rcpf(fmaf(0.32f, z, 1.f))); }
 
 // act(g), and with SLOPE act'(g).  SiLU of bf16 results: hardware exponential and reciprocal (see silu_for_bf16).
 template <typename T, int ACT> struct Activation {
