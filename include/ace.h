@@ -361,7 +361,8 @@ ace_status ace_mx4_dequantize(int64_t rows, int32_t K, int32_t dtype, const uint
  *   ace_grouped_matmul_mx4  y[r] = w[e] x[r]
  *   ace_grouped_gated_mx4   a[r] = act(w_gate[e] x[r]) * (w_up[e] x[r])
  * w, w_gate, w_up: [N, M, K] numbers, i.e. N * M rows of the format.  x [S, K]: bf16 (x_scales NULL), multiplied with
- * the weights' exact values, or 4-bit codes with x_scales.  y and a are bf16.  Sums are fp32.
+ * the weights as ace_mx4_dequantize gives them in bf16 (exact below 2^128; scales 253 and 254 reach past that, and such
+ * weights are infinite), or 4-bit codes with x_scales (exact for every scale).  y and a are bf16.  Sums are fp32.
  * Rows of no group, limits and S = 0 as for ace_grouped_matmul; M is a multiple of 8, K of 32.
  *   workspace  DEVICE scratch of ace_grouped_mx4_workspace_size(desc, gated) bytes, 256-byte aligned (may be NULL when
  *              that is 0).

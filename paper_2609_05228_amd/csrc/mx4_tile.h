@@ -176,8 +176,9 @@ template <int BLK, int W> struct Mx4Rows {
   }
 };
 
-// 8 numbers of a block as bf16, which holds every one of them exactly: dword j of its codes, times 2^(s - 127) in `scale`,
-// of which the conversion takes the exponent alone (s = 255 gives NaN)
+// 8 numbers of a block as bf16, which holds every one below 2^128 exactly, subnormal ones among them (the others, which only
+// scales 253 and 254 reach, become infinite): dword j of its codes, times 2^(s - 127) in `scale`, of which the conversion
+// takes the exponent alone (s = 255 gives NaN)
 __device__ __forceinline__ bf16x8_t mx4_to_bf16(uint32_t codes, float scale) {
   typedef __bf16 bf16x2_v __attribute__((ext_vector_type(2)));
   typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -190,7 +191,7 @@ __device__ __forceinline__ bf16x8_t mx4_to_bf16(uint32_t codes, float scale) {
 }
 
 // Tiles of bf16 results (see DenseTile) on 4-bit weights: rows in bf16 (ROWS4 = false) by bf16 matrix instructions on
-// the weights' exact values, or rows in 4 bits too, by the scaled instruction
+// the weights in bf16 (see mx4_to_bf16), or rows in 4 bits too, by the scaled instruction
 template <bool ROWS4_, int MB_, int NB_, int WR_, int WC_, int DA_, int DB_, int MATS> struct Mx4Tile {
   using T = bf16_t;
   static constexpr bool ROWS4 = ROWS4_;

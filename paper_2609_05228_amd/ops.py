@@ -170,7 +170,8 @@ def mx4_quantize(x):
 
 
 def mx4_dequantize(q, dtype=torch.bfloat16):
-    """The numbers [..., K] that an `Mx4` stands for, exactly, as bf16 or fp32."""
+    """The numbers [..., K] that an `Mx4` stands for, as bf16 or fp32: exactly, infinite from 2^128 on, which scales of
+    253 and 254 reach."""
     K = _mx4_of("q", q, None)
     if dtype not in _DT:
         raise ValueError(f"unsupported dtype {dtype}")
@@ -240,7 +241,8 @@ def grouped_matmul(x, w, offsets, *, out=None):
     out      [S, M] or None.  Rows of no group stay as they are in `out`; a fresh result
              holds zeros there.
     K and M are multiples of 8 (fp32: 4).  Returns y [S, M].
-    w may be an `Mx4` of [N, M, K]; then x is bf16 or an `Mx4` of [S, K], y and out are bf16, and there is no gradient."""
+    w may be an `Mx4` of [N, M, K]; then x is bf16 or an `Mx4` of [S, K], y and out are bf16, and there is no gradient.
+    bf16 rows meet the weights as `mx4_dequantize` gives them."""
     if isinstance(w, Mx4):
         return _mx4_call(x, (w,), offsets, out, 0, ("w",))
     _dtype_of("x", x, 2)
