@@ -34,26 +34,32 @@ def _need(ok, msg):
 def _check_all(dev, dtype, named):
     """(name, tensor, shape, dtype or None for the call's): shapes, types, layout, device."""
     grad = torch.is_grad_enabled()
-    # asked for each tensor inside a forward-mode level only: that takes as long as the other checks
-    if getattr(forward_ad, "_current_level", 0) >= 0:
+    try:
+        # asked for each tensor inside a forward-mode level only: that takes as long as the other checks
+        if getattr(forward_ad, "_current_level", 0) >= 0:
+            for name, t, _, _ in named:
+                if forward_ad.unpack_dual(t).tangent is not None:
+                    raise ValueError(f"{name} has a forward-mode tangent, which the call would lose")
+        for name, t, shape, dt in named:
+            if (t.shape == shape and t.dtype is (dt or dtype) and t.device == dev and t.is_contiguous()
+                    and not (grad and t.requires_grad)):
+                continue
+            if t.shape != shape:
+                raise ValueError(f"{name}: shape {tuple(t.shape)} != {tuple(shape)}")
+            if t.dtype != (dt or dtype):
+                raise ValueError(f"{name}: dtype {t.dtype} != {dt or dtype}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+            if t.device != dev:
+                raise ValueError(f"{name} is on {t.device}, expected {dev}")
+            raise ValueError(f"{name} requires a gradient, and no graph is recorded: call under torch.no_grad() (gradients of "
+                             "grouped_matmul, grouped_gated and block_norm: the *_grad functions; adapter_add has none, nor do "
+                             "weights in 4 bits)")
+    except (AttributeError, TypeError):  # caught, not asked for each tensor: that takes as long as the other checks
         for name, t, _, _ in named:
-            if forward_ad.unpack_dual(t).tangent is not None:
-                raise ValueError(f"{name} has a forward-mode tangent, which the call would lose")
-    for name, t, shape, dt in named:
-        if (t.shape == shape and t.dtype is (dt or dtype) and t.device == dev and t.is_contiguous()
-                and not (grad and t.requires_grad)):
-            continue
-        if t.shape != shape:
-            raise ValueError(f"{name}: shape {tuple(t.shape)} != {tuple(shape)}")
-        if t.dtype != (dt or dtype):
-            raise ValueError(f"{name}: dtype {t.dtype} != {dt or dtype}")
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        if t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, expected {dev}")
-        raise ValueError(f"{name} requires a gradient, and no graph is recorded: call under torch.no_grad() (gradients of "
-                         "grouped_matmul, grouped_gated and block_norm: the *_grad functions; adapter_add has none, nor do "
-                         "weights in 4 bits)")
+            if not isinstance(t, torch.Tensor):
+                raise ValueError(f"{name} must be a tensor") from None
+        raise
     if dev.type != "cuda":
         raise ValueError(f"the tensors are on {dev}: a GPU is needed")
 
@@ -64,6 +70,15 @@ def _dtype_of(name, t, dims):
     if t.dtype not in _DT:
         raise ValueError(f"{name}: unsupported dtype {t.dtype}")
     return t.dtype
+
+
+def _pair(name, v, what):
+    """The two that v, asked for as `what`, is made of."""
+    try:
+        first, second = v
+    except (TypeError, ValueError):
+        raise ValueError(f"{name}: {what} is needed") from None
+    return first, second
 
 
 def _sizes(*n):
@@ -277,7 +292,7 @@ def grouped_matmul_grad_w(dy, x, offsets, *, out=None):
 
 
 def _activation(name):
-    if name not in _lib.ACTIVATIONS:
+    if not isinstance(name, str) or name not in _lib.ACTIVATIONS:
         raise ValueError(f"activation {name!r} is none of {', '.join(_lib.ACTIVATIONS)}")
     return _lib.ACTIVATIONS[name]
 
@@ -300,7 +315,7 @@ def grouped_gated(x, w_gate, w_up, offsets, *, activation="silu", keep=False, ou
              (the `offsets` of `moe_forward`'s plan; [0, S] for one block that takes every row)
     activation  "silu", or "gelu" with the normal distribution's integral (not its tanh approximation)
     keep     also return g and u, for `grouped_gated_grad`
-    out      None, or tensors in the shape of the result.  Rows of no group stay as they are in them; a fresh
+    out      None, or tensors in the shape of the result (with keep (a, (g, u))).  Rows of no group stay as they are in them; a fresh
              result holds zeros there.
     K and M are multiples of 8 (fp32: 4).  Returns a [S, M], with keep (a, (g, u)).
     Both weights may be an `Mx4` of [N, M, K]; then x is bf16 or an `Mx4` of [S, K], a and out are bf16, and there is
@@ -317,9 +332,13 @@ def grouped_gated(x, w_gate, w_up, offsets, *, activation="silu", keep=False, ou
     named = [("x", x, (S, K), None), ("w_gate", w_gate, (N, M, K), None), ("w_up", w_up, (N, M, K), None),
              ("offsets", offsets, (N + 1,), torch.int32)]
     flags = 0
+    a, g, u = out, None, None
     if out is not None:
-        a, (g, u) = out if keep else (out, (None, None))
-        named += [(n, t, (S, M), None) for n, t in (("out", a), ("out's g", g), ("out's u", u)) if t is not None]
+        if keep:
+            a, gu = _pair("out", out, "(a, (g, u))")
+            g, u = _pair("out", gu, "(a, (g, u))")
+            named += [("out's g", g, (S, M), None), ("out's u", u, (S, M), None)]
+        named.append(("out", a, (S, M), None))
     _check_all(dev, dtype, named)
     if out is None:
         a, g, u = (torch.empty((S, M), dtype=dtype, device=dev) if i == 0 or keep else None for i in range(3))
@@ -350,8 +369,8 @@ def grouped_gated_grad(da, x, w_gate, w_up, offsets, *, kept=None, activation="s
     N, M, K = w_gate.shape
     S = da.shape[0]
     dev, size = da.device, _sizes(S, N, M, K)
-    g, u = (None, None) if kept is None else kept
-    _need(x is not None or (g is not None and not weights), "x is required with weights or without kept")
+    g, u = (None, None) if kept is None else _pair("kept", kept, "(g, u)")
+    _need(x is not None or (kept is not None and not weights), "x is required with weights or without kept")
     named = [("da", da, (S, M), None), ("w_gate", w_gate, (N, M, K), None), ("w_up", w_up, (N, M, K), None),
              ("offsets", offsets, (N + 1,), torch.int32)]
     if x is not None:
