@@ -7,8 +7,9 @@
 //
 // Both projections are one tile (grouped_tile.h): its 16-column blocks alternate between
 // the two matrices, so a lane's accumulators hold g and u of the same four features and the
-// activation and the product happen in registers: x is read once, and g and u never leave the
-// chip unless they are kept.  The gradient takes dg and du either from the kept g and u, or in the
+// activation and the product happen in registers: x is read once, and g and u leave the chip only where they are kept,
+// or where too few tiles fill the CUs and the reduction is in parts, whose fp32 sums of both go through the workspace to a
+// second launch (gated_join_kernel).  The gradient takes dg and du either from the kept g and u, or in the
 // epilogue of the same product computed again; both are rounded to the tensors' type there,
 // since the two products behind them run on matrix cores of that type.  dx is one
 // product with a reduction of two segments (dg with w_gate, then du with w_up), summed in the same

@@ -84,7 +84,7 @@ template <bool GX, bool LINES> __global__ __launch_bounds__(512) void grouped_sh
 }
 
 // Weights' gradient: tile = 16 MB rows x 16 NB columns of one group's dw.  MATS = 2: of both matrices of a gated
-// block, whose sums share x (rows[1], out[1] of GroupedArgs; the second matrix's partial sums lie behind the first's).
+// block, whose sums share x (rows2, out2 of GroupedArgs; the second matrix's partial sums lie behind the first's).
 template <typename T, bool LINES, int MATS, int MB, int NB, int WR, int WC, int DA, int DB>
 __global__ __launch_bounds__(WR *WC * 64) void grouped_weights_kernel(GroupedArgs g) {
   constexpr int BM = 16 * MB, BN = 16 * NB;

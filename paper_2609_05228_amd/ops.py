@@ -306,8 +306,9 @@ def _ptr(t):
 
 
 def grouped_gated(x, w_gate, w_up, offsets, *, activation="silu", keep=False, out=None):
-    """The gated feed-forward block of the experts in one kernel: a[r] = act(g[r]) * u[r] with
-    g[r] = w_gate[e] x[r] and u[r] = w_up[e] x[r] for the rows r of group e.
+    """The gated feed-forward block of the experts: a[r] = act(g[r]) * u[r] with g[r] = w_gate[e] x[r] and
+    u[r] = w_up[e] x[r] for the rows r of group e, in one kernel (where a few tiles have a long reduction, in parts and a
+    second launch that adds them up).
 
     x        [S, K] bf16 or fp32 device tensor, rows in group order
     w_gate, w_up  [N, M, K] weights of the groups (nn.Linear layout)
