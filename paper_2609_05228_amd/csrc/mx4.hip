@@ -39,7 +39,8 @@ __device__ __forceinline__ void load8(const bf16_t *p, float (&v)[8]) {
 // A part is 128 numbers of a row (the last may be short), taken by 16 lanes, 8 numbers each: 4 lanes a block, their four
 // scales one dword.  WHOLE: rows are whole parts, so a part's place needs no division.  Bound by memory: 98304 rows of
 // 2048 in bf16 94 us there and 86 back (4.3 and 5.9 TB/s; the results' non-temporal stores leave the caches clean for
-// whoever comes next: 128 us there after a way back without them).  Two or four parts a lane under way: slower (98, 96
+// whoever comes next: 128 us there after a way back without them).  In fp32 a lane's result is two pieces of 16 bytes, each
+// store half lines, and the hint pays all the same: 260 us back and 181 there, 242 and 222 without it.  Two or four parts a lane under way: slower (98, 96
 // and 94, 99).
 template <bool WHOLE> struct Mx4Part {
   size_t x;  // where the lane's numbers start; their codes at half of it
@@ -242,7 +243,17 @@ struct Plan {
 // Which kernel.  Few tiles of 16 rows x 64 columns: those, the reduction over the waves of a workgroup, against parts of the
 // reduction and a launch that adds them (kernel times: 8 rows in 128 groups of 768 x 2048 8.6 us against 12.8, 64 rows
 // in 64 groups 16.8 against 20.5, in one of 2048 x 4096 11.4 against 15.0).  More of them: 16 x 256 tiles up to 16 rows a
-// group (256 rows in 128 groups: 30 us against 34 in the small ones), 64 x 128 up to 96, then the large shapes.
+// group, 64 x 128 up to 96, then the large shapes.  Kernel times of each without parts, groups of 768 x 2048, bf16 rows plain
+// and gated, rows in 4 bits plain and gated:
+//   rows, groups    few                     16 x 256                64 x 128               large
+//       8, 128      8.8   9.3   8.2   8.5  18.0  18.0 16.2  16.1   19.8  19.9 16.4  16.2  26.8  30.7 22.9 23.0
+//      64,  64     17.2  27.2  15.8  24.6  18.2  23.8 16.8  21.2   21.5  34.3 17.8  28.2  26.3  54.7 23.4 39.8
+//     256, 128     29.2  56.0  26.9  51.3  25.1  44.0 23.5  42.9   34.8  60.6 29.0  48.9  48.3  83.1 41.4 60.3
+//    2048, 128     41.2  86.4  36.3  76.6  35.0  59.9 31.7  55.7   36.2  63.3 29.6  51.0  54.0  94.5 42.1 62.9
+//    8192, 128    114.1 248.2  99.2 213.9  67.7 136.7 52.9 113.3   60.0 108.8 44.8  81.7  66.5 106.2 46.8 68.8
+//   12288, 128    160.0 355.7 138.4 304.8  99.2 194.8 74.6 154.9   70.6 136.5 50.7 100.3  74.3 120.0 49.5 72.6
+//   16384, 128    206.5 454.8 180.7 393.6 122.1 248.2 91.5 196.9   92.3 166.1 66.2 117.8  80.7 129.9 52.9 76.8
+// The rules are the plain products'; the gated block would gain by the large shapes from 64 rows a group on.
 Plan plan_mx4(const Mx4Args &m) {
   const GatedArgs &g = m.g;
   const int mats = m.gated ? 2 : 1, cols = mats * g.M;
