@@ -319,8 +319,8 @@ def grouped_gated(x, w_gate, w_up, offsets, *, activation="silu", keep=False, ou
     out      None, or tensors in the shape of the result (with keep (a, (g, u))).  Rows of no group stay as they are in them; a fresh
              result holds zeros there.
     K and M are multiples of 8 (fp32: 4).  Returns a [S, M], with keep (a, (g, u)).
-    Both weights may be an `Mx4` of [N, M, K]; then x is bf16 or an `Mx4` of [S, K], a and out are bf16, and there is
-    no gradient, so nothing to keep."""
+    Both weights may be an `Mx4` of [N, M, K]; then x is bf16 or an `Mx4` of [S, K] (see `grouped_matmul`), a and out are
+    bf16, and there is no gradient, so nothing to keep."""
     if isinstance(w_gate, Mx4) or isinstance(w_up, Mx4):
         _need(not keep, "keep: weights in 4 bits have no gradient")
         return _mx4_call(x, (w_gate, w_up), offsets, out, _activation(activation), ("w_gate", "w_up"))
